@@ -54,7 +54,8 @@ typedef enum {
   PIVOT_ERR_HIP = 4           /* a HIP launch failed; see pivot_last_error() */
 } pivot_status;
 
-typedef enum { PIVOT_DT_BF16 = 0, PIVOT_DT_FP8_E4M3 = 1 } pivot_dtype;
+/* PIVOT_DT_FP32: the norm's input type only. */
+typedef enum { PIVOT_DT_BF16 = 0, PIVOT_DT_FP8_E4M3 = 1, PIVOT_DT_FP32 = 2 } pivot_dtype;
 
 typedef enum { PIVOT_REUSE = 0, PIVOT_REFINE = 1 } pivot_mode;
 
@@ -367,8 +368,197 @@ pivot_status pivot_topk_rows_ws(int32_t n_rows, const float* scores, int64_t ld,
 pivot_status pivot_encode_e4m3(const float* x, uint8_t* out, int64_t n, void* stream);
 
 /*
+ * ---- Operators around the index calls ----
+ *
+ * What a layer with token-level sparse attention runs before and after the
+ * index calls: the norm that makes fp8 rows, the attention over the index sets
+ * in its latent (MQA) form with a cache held in 4 bits, and the eviction of
+ * tokens that the attention gave little weight.  The conventions above hold:
+ * the caller owns every buffer, nothing is allocated or synchronised, every
+ * argument is checked before the first launch.
+ */
+
+/*
+ * Root-mean-square norm with the residual's addition and E4M3FN output, for
+ * rows r < n_rows of `dim` values (1 .. 32768):
+ *   h = x + residual                         (fp32; residual NULL: h = x)
+ *   y = h * rsqrt(mean(h^2) + eps) * weight   (fp32, of the unrounded h)
+ *   per group of the row: scale = max|y| / 448 (1 if that is 0),
+ *                         codes = E4M3FN of y / scale, nearest even
+ * dtype (x, residual, weight, residual_out): PIVOT_DT_BF16 or PIVOT_DT_FP32,
+ * else PIVOT_ERR_UNSUPPORTED.
+ *   x, residual   dev, rows ld_x / ld_residual values apart (>= dim)
+ *   weight        dev [dim]
+ *   group         0: one scale per row; 128: one per 128 values (the last group
+ *                 may be shorter)
+ *   residual_out  dev [n_rows, dim] or NULL: h rounded to dtype; may be x or
+ *                 residual themselves (rows not padded)
+ *   codes         dev [n_rows, dim]
+ *   scale         dev fp32 [n_rows, group ? ceil(dim / 128) : 1]
+ * Pointers need only their elements' alignment.  A row with a NaN or an
+ * infinity has NaN codes where y is NaN.
+ */
+pivot_status pivot_rmsnorm_fp8(int32_t dtype, int32_t n_rows, int32_t dim, const void* x, int64_t ld_x,
+                               const void* residual, int64_t ld_residual, const void* weight, float eps, int32_t group,
+                               void* residual_out, uint8_t* codes, float* scale, void* stream);
+
+/*
+ * Where token s of sequence b of a batch lives in row arrays of `rows` rows
+ * (1 .. 2^31 - 1):
+ *   block_table NULL: row b * seq_stride + s
+ *   block_table dev int32 [B, max_pages]: row block_table[b * max_pages + s /
+ *     page_size] * page_size + s % page_size; page_size is a power of two in
+ *     [16, 65536], rows a multiple of it; entries outside the pool are clamped
+ *     into it (no access leaves it, the result is then meaningless).
+ */
+typedef struct {
+  const int32_t* block_table;
+  int32_t max_pages;
+  int32_t page_size;
+  int64_t rows;
+  int64_t seq_stride;
+} pivot_row_map;
+
+/*
+ * A latent cache in 4 bits, 400 bytes a token.  A token's row is 512 latent
+ * values in OCP MXFP4 and 64 position values in bf16:
+ *   codes   dev [rows, 256]  E2M1 codes (sign, 2 exponent bits, 1 mantissa bit:
+ *                            0, 0.5, 1, 1.5, 2, 3, 4, 6), the even value of a
+ *                            byte in its low half
+ *   scales  dev [rows, 16]   E8M0: 2^(byte - 127) of each 32 values, 255 = NaN
+ *   rope    dev [rows, 64]   bf16
+ * All three 16-byte aligned.  One row serves all heads: keys are the whole row,
+ * values its latent part.
+ */
+#define PIVOT_CACHE4_LATENT 512
+#define PIVOT_CACHE4_ROPE 64
+typedef struct {
+  void* codes;
+  void* scales;
+  void* rope;
+  pivot_row_map map;
+} pivot_cache4;
+
+/*
+ * Quantise new tokens into the cache.  Sequence b gets n_new rows, or rows
+ * cu[b] .. cu[b+1]-1 (host [B+1], cu[0] = 0), of the packed latent (dev bf16,
+ * rows ld_latent >= 512 values apart) and rope (dev bf16, ld_rope >= 64); they
+ * become its positions pos0[b] (host [B]), pos0[b] + 1, ...
+ * The scale of 32 values is the smallest power of two 2^e (e >= -127) with
+ * max|x| / 2^e <= 6, their codes the nearest E2M1 values to x / 2^e, ties to
+ * even; 32 zeros have scale byte 0, values with an infinity or a NaN among
+ * them byte 255 and codes 0 (they read as NaN).
+ */
+pivot_status pivot_cache4_write(const pivot_cache4* c, int32_t batch, int32_t n_new, const int32_t* cu,
+                                const int32_t* pos0, const void* latent, int64_t ld_latent, const void* rope,
+                                int64_t ld_rope, void* stream);
+
+/*
+ * Read rows back: out (dev bf16 [B, n, 576], 16-byte aligned) receives the
+ * values (exact in bf16) of positions idx (dev int32 [B, n]); a negative
+ * position, or one past what the map can hold, gives a row of zeros.
+ */
+pivot_status pivot_cache4_read(const pivot_cache4* c, int32_t batch, int32_t n, const int32_t* idx, void* out,
+                               void* stream);
+
+/*
+ * Attention of n_q queries per sequence (or packed runs cu_q, as in
+ * pivot_layout) over the cache, `heads` (1 .. 128, else UNSUPPORTED) heads a
+ * query.  With c_s, r_s the latent and position part of cached token s:
+ *   z[r,h,s] = scale * q[r,h] . (c_s, r_s)
+ *   out[r,h] = sum_s softmax(z[r,h])[s] c_s     lse[r,h] = log sum_s exp(z[r,h,s])
+ *   acc[b,s] += sum over the sequence's rows r and heads h of softmax(z[r,h])[s]
+ *   q     dev bf16, row r head h at r * q_row_stride + h * q_head_stride, 576
+ *         values (latent part first); strides are multiples of 8, q is 16-byte
+ *         aligned
+ *   idx   dev int32 [rows, topk] as the index calls write it: a row attends to
+ *         its entries in [0, its position] (others, the -1 padding among them,
+ *         are skipped; entries of one row are distinct).  NULL: to every
+ *         position up to its own
+ *   out   dev bf16 [rows, heads, 512], 16-byte aligned
+ *   lse   dev fp32 [rows, heads], or NULL
+ *   acc   dev fp32 [B, acc_stride], or NULL; acc_stride >= every n_k[b]
+ * Row i of sequence b is at position q_pos0[b] + i; q_pos0[b] + n_q <= n_k[b].
+ * A row with nothing to attend to, or only scores of -infinity, has out = 0 and
+ * lse = -infinity and adds nothing.  A row that attends to a token with a NaN,
+ * or whose query holds an infinity or a NaN, is NaN; tokens it does not attend
+ * to never reach it.  Scores and sums are fp32 (the products are exact), the
+ * weights are rounded to bf16 for the product with the values.  The same call
+ * gives the same bits.
+ * Workspace: pivot_cache4_attend_workspace_size(a) bytes (device, 256-byte
+ * aligned; 0 for invalid shapes or none needed; reads the host arrays only).
+ */
+#define PIVOT_ATTEND_MAX_HEADS 128
+typedef struct {
+  int32_t heads;
+  int32_t batch;
+  int32_t n_q;
+  const int32_t* cu_q;      /* host [B+1], or NULL */
+  const int32_t* q_pos0;    /* host [B] */
+  const int32_t* n_k;       /* host [B] */
+  const void* q;
+  int64_t q_row_stride, q_head_stride;
+  pivot_cache4 cache;
+  const int32_t* idx;
+  int32_t topk;
+  float scale;
+  void* out;
+  float* lse;
+  float* acc;
+  int64_t acc_stride;
+  void* workspace;
+  size_t workspace_bytes;
+  void* stream;
+} pivot_attend_args;
+size_t pivot_cache4_attend_workspace_size(const pivot_attend_args* a);
+pivot_status pivot_cache4_attend(const pivot_attend_args* a);
+
+/*
+ * Eviction by accumulated attention weight.  Of sequence b's n_k[b] tokens
+ * (host [B]) the first `sink`, the last `recent` and the largest acc of the
+ * others stay, `keep` in all (sink + recent <= keep; all tokens when n_k[b] <=
+ * keep).  Equal weights: the lower position stays; NaN ranks above every number
+ * (with the sign bit set: below).
+ *   acc       dev fp32 [B, acc_stride]
+ *   out_keep  dev int32 [B, keep]: the kept positions, ascending, then -1;
+ *             min(n_k[b], keep) of them, so the host knows the new lengths
+ *   out_acc   dev fp32 [B, keep] or NULL: their acc, then 0
+ *   arrays    n_arrays (0 .. 8) row arrays that move along (the cache's three,
+ *             the indexer's keys and key scales, ...): row out_keep[b][j] of
+ *             src under `from` becomes row j of dst under `to`; row_bytes is a
+ *             multiple of 4, the pointers are 4-byte aligned.  No row that is
+ *             written may be one that is read: dst is another array, or the
+ *             same one with `to` naming other pages (pages shared with other
+ *             sequences stay as they are).
+ * Workspace as above, pivot_evict_workspace_size(a) bytes.
+ */
+#define PIVOT_EVICT_MAX_ARRAYS 8
+typedef struct {
+  const void* src;
+  void* dst;
+  int32_t row_bytes;
+} pivot_move;
+typedef struct {
+  int32_t batch;
+  const int32_t* n_k;       /* host [B] */
+  const float* acc;
+  int64_t acc_stride;
+  int32_t keep, sink, recent;
+  int32_t* out_keep;
+  float* out_acc;
+  int32_t n_arrays;
+  pivot_move arrays[PIVOT_EVICT_MAX_ARRAYS];
+  pivot_row_map from, to;
+  void* workspace;
+  size_t workspace_bytes;
+  void* stream;
+} pivot_evict_args;
+size_t pivot_evict_workspace_size(const pivot_evict_args* a);
+pivot_status pivot_evict(const pivot_evict_args* a);
+
+/*
  * Kernel timing.  Between pivot_profile_begin() and pivot_profile_end() every
- * kernel the library launches is bracketed by two HIP events recorded on the
+ * kernel that the index calls and their stages launch is bracketed by two HIP events recorded on the
  * launch's stream.  pivot_profile_end() waits for those events and returns,
  * per kernel kind, the number of launches and the summed event-to-event time;
  * it then stops recording.  Event objects are host-side resources created on

@@ -18,7 +18,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpivot.so")
 
 PIVOT_OK, PIVOT_ERR_INVALID_ARG, PIVOT_ERR_UNSUPPORTED, PIVOT_ERR_WORKSPACE, PIVOT_ERR_HIP = range(5)
-PIVOT_DT_BF16, PIVOT_DT_FP8_E4M3 = 0, 1
+PIVOT_DT_BF16, PIVOT_DT_FP8_E4M3, PIVOT_DT_FP32 = 0, 1, 2
 PIVOT_REUSE, PIVOT_REFINE = 0, 1
 PIVOT_DENSE = -1
 PIVOT_MAX_KEYS = 1 << 27
@@ -27,6 +27,8 @@ PIVOT_WINDOW_SHARED, PIVOT_WINDOW_PER_QUERY = 0, 1
 PIVOT_AGG_MEAN, PIVOT_AGG_FIRST, PIVOT_AGG_LAST = 0, 1, 2
 PIVOT_REFINE_AUTO, PIVOT_REFINE_FUSED, PIVOT_REFINE_SPLIT = 0, 1, 2
 H, D = 64, 128
+PIVOT_CACHE4_LATENT, PIVOT_CACHE4_ROPE = 512, 64
+PIVOT_ATTEND_MAX_HEADS, PIVOT_EVICT_MAX_ARRAYS = 128, 8
 
 EXPORTED = ["pivot_workspace_size", "pivot_dense_index", "pivot_group_index", "pivot_cand_width",
             "pivot_group_workspace_size", "pivot_group_index_opts", "pivot_dense_index_layout",
@@ -35,6 +37,8 @@ EXPORTED = ["pivot_workspace_size", "pivot_dense_index", "pivot_group_index", "p
             "pivot_topk_rows_bf16",
             "pivot_encode_e4m3", "pivot_profile_begin", "pivot_profile_begin_kinds", "pivot_index_layers",
             "pivot_group_index_noalloc",
+            "pivot_rmsnorm_fp8", "pivot_cache4_write", "pivot_cache4_read", "pivot_cache4_attend",
+            "pivot_cache4_attend_workspace_size", "pivot_evict", "pivot_evict_workspace_size",
             "pivot_profile_end", "pivot_status_string", "pivot_last_error", "pivot_version"]
 KERNELS = ["proxy", "score", "select", "refine", "fill", "lin", "copy"]
 
@@ -74,6 +78,45 @@ class pivot_layout(ctypes.Structure):
     _fields_ = [
         ("cu_q", ctypes.POINTER(ctypes.c_int32)), ("block_table", ctypes.c_void_p),
         ("max_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("pool_keys", ctypes.c_int64),
+    ]
+
+
+class pivot_row_map(ctypes.Structure):
+    _fields_ = [
+        ("block_table", ctypes.c_void_p), ("max_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+        ("rows", ctypes.c_int64), ("seq_stride", ctypes.c_int64),
+    ]
+
+
+class pivot_cache4(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rope", ctypes.c_void_p),
+                ("map", pivot_row_map)]
+
+
+class pivot_attend_args(ctypes.Structure):
+    _fields_ = [
+        ("heads", ctypes.c_int32), ("batch", ctypes.c_int32), ("n_q", ctypes.c_int32),
+        ("cu_q", ctypes.POINTER(ctypes.c_int32)), ("q_pos0", ctypes.POINTER(ctypes.c_int32)),
+        ("n_k", ctypes.POINTER(ctypes.c_int32)),
+        ("q", ctypes.c_void_p), ("q_row_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64),
+        ("cache", pivot_cache4), ("idx", ctypes.c_void_p), ("topk", ctypes.c_int32), ("scale", ctypes.c_float),
+        ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("acc", ctypes.c_void_p), ("acc_stride", ctypes.c_int64),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t), ("stream", ctypes.c_void_p),
+    ]
+
+
+class pivot_move(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("row_bytes", ctypes.c_int32)]
+
+
+class pivot_evict_args(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("n_k", ctypes.POINTER(ctypes.c_int32)), ("acc", ctypes.c_void_p),
+        ("acc_stride", ctypes.c_int64), ("keep", ctypes.c_int32), ("sink", ctypes.c_int32),
+        ("recent", ctypes.c_int32), ("out_keep", ctypes.c_void_p), ("out_acc", ctypes.c_void_p),
+        ("n_arrays", ctypes.c_int32), ("arrays", pivot_move * PIVOT_EVICT_MAX_ARRAYS),
+        ("from_", pivot_row_map), ("to", pivot_row_map),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t), ("stream", ctypes.c_void_p),
     ]
 
 
@@ -156,6 +199,23 @@ def lib():
         L.pivot_topk_rows_ws.argtypes = [I32, P, I64, I64, I32, I32, P, P, ctypes.c_size_t, P]
         L.pivot_encode_e4m3.restype = I32
         L.pivot_encode_e4m3.argtypes = [P, P, I64, P]
+        F32 = ctypes.c_float
+        PI = ctypes.POINTER(I32)
+        C4 = ctypes.POINTER(pivot_cache4)
+        L.pivot_rmsnorm_fp8.restype = I32
+        L.pivot_rmsnorm_fp8.argtypes = [I32, I32, I32, P, I64, P, I64, P, F32, I32, P, P, P, P]
+        L.pivot_cache4_write.restype = I32
+        L.pivot_cache4_write.argtypes = [C4, I32, I32, PI, PI, P, I64, P, I64, P]
+        L.pivot_cache4_read.restype = I32
+        L.pivot_cache4_read.argtypes = [C4, I32, I32, P, P, P]
+        L.pivot_cache4_attend_workspace_size.restype = ctypes.c_size_t
+        L.pivot_cache4_attend_workspace_size.argtypes = [ctypes.POINTER(pivot_attend_args)]
+        L.pivot_cache4_attend.restype = I32
+        L.pivot_cache4_attend.argtypes = [ctypes.POINTER(pivot_attend_args)]
+        L.pivot_evict_workspace_size.restype = ctypes.c_size_t
+        L.pivot_evict_workspace_size.argtypes = [ctypes.POINTER(pivot_evict_args)]
+        L.pivot_evict.restype = I32
+        L.pivot_evict.argtypes = [ctypes.POINTER(pivot_evict_args)]
         L.pivot_profile_begin.restype = I32
         L.pivot_profile_begin.argtypes = []
         L.pivot_profile_begin_kinds.restype = I32
@@ -535,3 +595,244 @@ def pivot_encode_e4m3(x, out=None, stream=None):
     out = torch.empty(x.shape, dtype=torch.uint8, device=x.device) if out is None else out
     _check(lib().pivot_encode_e4m3(_ptr(x), _ptr(out), x.numel(), _stream(stream)), "pivot_encode_e4m3")
     return out
+
+
+# ---- operators around the index calls ----
+
+def _host_ints(v, batch=None):
+    """A ctypes int32 array of host integers (one repeated for the batch, or a sequence)."""
+    if isinstance(v, int):
+        v = [v] * batch
+    return (ctypes.c_int32 * len(v))(*v)
+
+
+def _rows_of(t, width, what):
+    """The row stride of a 2-D (or contiguous deeper) tensor of `width` values a row."""
+    if t.shape[-1] != width or t.stride(-1) != 1:
+        raise ValueError(f"{what} must have rows of {width} adjacent values")
+    if t.dim() == 2:
+        return t.stride(0) if t.shape[0] > 1 else width
+    if not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous beyond two dimensions")
+    return width
+
+
+def _float_code(t) -> int:
+    if t.dtype == torch.bfloat16:
+        return PIVOT_DT_BF16
+    if t.dtype == torch.float32:
+        return PIVOT_DT_FP32
+    raise ValueError("x must be bfloat16 or float32")
+
+
+def _expect(t, dtype, shape, what):
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
+    return t
+
+
+def pivot_rmsnorm_fp8(x, weight, eps=1e-6, residual=None, group=0, residual_out=None, codes=None, scale=None,
+                      stream=None):
+    """RMS norm of x + residual ([..., dim], bf16 or fp32) with E4M3FN output:
+    (codes uint8 [..., dim], scale fp32 [..., groups], x + residual in x's type).
+    group 0: one scale per row; 128: one per 128 values.  Without a residual the
+    third result is None."""
+    dim = x.shape[-1]
+    code = _float_code(x)
+    ld_x = _rows_of(x, dim, "x")
+    ld_r = 0
+    if residual is not None:
+        if residual.dtype != x.dtype or residual.shape != x.shape:
+            raise ValueError("residual must have x's type and shape")
+        ld_r = _rows_of(residual, dim, "residual")
+        residual_out = (torch.empty(x.shape, dtype=x.dtype, device=x.device) if residual_out is None
+                        else _expect(residual_out, x.dtype, x.shape, "residual_out"))
+    elif residual_out is not None:
+        raise ValueError("residual_out needs a residual")
+    _expect(weight, x.dtype, (dim,), "weight")
+    rows = x.numel() // max(dim, 1)
+    shape = tuple(x.shape[:-1]) + (-(-dim // group) if group else 1,)
+    codes = (torch.empty(x.shape, dtype=torch.uint8, device=x.device) if codes is None
+             else _expect(codes, torch.uint8, x.shape, "codes"))
+    scale = (torch.empty(shape, dtype=torch.float32, device=x.device) if scale is None
+             else _expect(scale, torch.float32, shape, "scale"))
+    _check(lib().pivot_rmsnorm_fp8(code, rows, dim, _ptr(x), ld_x, _ptr(residual), ld_r, _ptr(weight), eps, group,
+                                   _ptr(residual_out), _ptr(codes), _ptr(scale), _stream(stream)), "pivot_rmsnorm_fp8")
+    return codes, scale, residual_out
+
+
+def make_row_map(seq_stride=0, rows=0, block_table=None, page_size=0) -> pivot_row_map:
+    """Where tokens live in row arrays of `rows` rows: seq_stride rows a sequence,
+    or pages of a pool by block_table (dev int32 [B, max_pages])."""
+    m = pivot_row_map()
+    m.rows, m.seq_stride = int(rows), int(seq_stride)
+    if block_table is not None:
+        if block_table.dtype != torch.int32 or block_table.dim() != 2 or not block_table.is_contiguous():
+            raise ValueError("block_table must be a contiguous int32 [B, max_pages] tensor")
+        m.block_table = block_table.data_ptr()
+        m.max_pages, m.page_size = block_table.shape[1], int(page_size)
+        m._bt = block_table
+    return m
+
+
+def make_cache4(codes, scales, rope, row_map) -> pivot_cache4:
+    """A 4-bit latent cache over codes uint8 [rows, 256], scales uint8 [rows, 16]
+    and rope bf16 [rows, 64]; the tensors have to outlive the struct's use."""
+    n = codes.shape[0]
+    _expect(codes, torch.uint8, (n, PIVOT_CACHE4_LATENT // 2), "codes")
+    _expect(scales, torch.uint8, (n, PIVOT_CACHE4_LATENT // 32), "scales")
+    _expect(rope, torch.bfloat16, (n, PIVOT_CACHE4_ROPE), "rope")
+    if row_map.rows > n:
+        raise ValueError(f"the row map names {row_map.rows} rows, the cache holds {n}")
+    c = pivot_cache4()
+    c.codes, c.scales, c.rope = codes.data_ptr(), scales.data_ptr(), rope.data_ptr()
+    c.map = row_map
+    c._keep = (codes, scales, rope, row_map)
+    return c
+
+
+def _check_batch(row_map, batch, what="block_table"):
+    bt = getattr(row_map, "_bt", None)
+    if bt is not None and bt.shape[0] < batch:
+        raise ValueError(f"{what} has {bt.shape[0]} sequences, the call {batch}")
+
+
+def pivot_cache4_write(latent, rope, cache, pos0, n_new=None, cu=None, stream=None):
+    """Quantise packed tokens (latent [T, 512], rope [T, 64], bf16; rows may be
+    strided) into the cache: n_new for each of len(pos0) sequences, or the runs
+    of cu (host ints [B+1]), from position pos0[b] on."""
+    if latent.dtype != torch.bfloat16 or rope.dtype != torch.bfloat16:
+        raise ValueError("latent and rope must be bfloat16")
+    batch = len(pos0)
+    _check_batch(cache._keep[3], batch)
+    rows = cu[-1] if cu is not None else int(n_new) * batch
+    if latent.numel() != rows * PIVOT_CACHE4_LATENT or rope.numel() != rows * PIVOT_CACHE4_ROPE:
+        raise ValueError(f"latent and rope must hold {rows} rows")
+    if cu is not None and len(cu) != batch + 1:
+        raise ValueError("cu needs len(pos0) + 1 entries")
+    _check(lib().pivot_cache4_write(ctypes.byref(cache), batch, 0 if cu is not None else int(n_new),
+                                    None if cu is None else _host_ints(cu), _host_ints(pos0), _ptr(latent),
+                                    _rows_of(latent, PIVOT_CACHE4_LATENT, "latent"), _ptr(rope),
+                                    _rows_of(rope, PIVOT_CACHE4_ROPE, "rope"), _stream(stream)),
+           "pivot_cache4_write")
+
+
+def pivot_cache4_read(cache, idx, out=None, stream=None):
+    """The values of positions idx (int32 [B, n]) as bf16 [B, n, 576]; negative ones read as zeros."""
+    if idx.dtype != torch.int32 or idx.dim() != 2 or not idx.is_contiguous():
+        raise ValueError("idx must be a contiguous int32 [B, n] tensor")
+    _check_batch(cache._keep[3], idx.shape[0])
+    shape = tuple(idx.shape) + (PIVOT_CACHE4_LATENT + PIVOT_CACHE4_ROPE,)
+    out = (torch.empty(shape, dtype=torch.bfloat16, device=idx.device) if out is None
+           else _expect(out, torch.bfloat16, shape, "out"))
+    _check(lib().pivot_cache4_read(ctypes.byref(cache), idx.shape[0], idx.shape[1], _ptr(idx), _ptr(out),
+                                   _stream(stream)), "pivot_cache4_read")
+    return out
+
+
+def pivot_cache4_attend(q, cache, q_pos0, n_k, scale, idx=None, cu_q=None, acc=None, out=None, lse=None, ws=None,
+                        stream=None):
+    """Attention of q (bf16 [B, n_q, heads, 576], or [rows, heads, 576] with the
+    runs cu_q) over the 4-bit cache: (out bf16 [..., heads, 512], lse fp32
+    [..., heads]).  idx: int32 [..., topk] index sets, or None for every position
+    up to the query's own; acc: fp32 [B, >= max n_k], each token's softmax weight
+    is added to it.  Rows and heads of q may be strided."""
+    lead = q.shape[:-2]
+    heads, dim = q.shape[-2:]
+    if q.dtype != torch.bfloat16 or dim != PIVOT_CACHE4_LATENT + PIVOT_CACHE4_ROPE or q.stride(-1) != 1:
+        raise ValueError("q must be bfloat16 with heads of 576 adjacent values")
+    batch = len(n_k)
+    if len(q_pos0) != batch:
+        raise ValueError("q_pos0 and n_k must have one entry per sequence")
+    if cu_q is None:
+        if q.dim() != 4 or q.shape[0] != batch:
+            raise ValueError("q must be [B, n_q, heads, 576]")
+        if batch > 1 and q.shape[1] > 0 and q.stride(0) != q.shape[1] * q.stride(1):
+            raise ValueError("the sequences of q must follow each other at its row stride")
+        row_stride, n_rows = (q.stride(1) if q.shape[1] > 1 else q.stride(0)), batch * q.shape[1]
+    else:
+        if q.dim() != 3 or len(cu_q) != batch + 1 or cu_q[-1] != q.shape[0]:
+            raise ValueError("q must be [rows, heads, 576] with rows = cu_q[-1] and len(cu_q) = B + 1")
+        row_stride, n_rows = q.stride(0), q.shape[0]
+    head_stride = q.stride(-2) if heads > 1 else dim
+    if n_rows <= 1:
+        row_stride = max(row_stride, (heads - 1) * head_stride + dim)
+    _check_batch(cache._keep[3], batch)
+    a = pivot_attend_args()
+    a.heads, a.batch, a.n_q = heads, batch, 0 if cu_q is not None else q.shape[1]
+    keep = [_host_ints(q_pos0), _host_ints(n_k)]
+    PI = ctypes.POINTER(ctypes.c_int32)
+    a.q_pos0, a.n_k = ctypes.cast(keep[0], PI), ctypes.cast(keep[1], PI)
+    if cu_q is not None:
+        keep.append(_host_ints(cu_q))
+        a.cu_q = ctypes.cast(keep[2], PI)
+    a.q, a.q_row_stride, a.q_head_stride = q.data_ptr(), row_stride, head_stride
+    a.cache = cache
+    if idx is not None:
+        if idx.dtype != torch.int32 or idx.shape[:-1] != lead or not idx.is_contiguous():
+            raise ValueError("idx must be a contiguous int32 tensor with one row of entries per query")
+        a.idx, a.topk = idx.data_ptr(), idx.shape[-1]
+    a.scale = scale
+    shape = tuple(lead) + (heads,)
+    out = (torch.empty(shape + (PIVOT_CACHE4_LATENT,), dtype=torch.bfloat16, device=q.device) if out is None
+           else _expect(out, torch.bfloat16, shape + (PIVOT_CACHE4_LATENT,), "out"))
+    lse = (torch.empty(shape, dtype=torch.float32, device=q.device) if lse is None
+           else _expect(lse, torch.float32, shape, "lse"))
+    a.out, a.lse = out.data_ptr(), lse.data_ptr()
+    if acc is not None:
+        if acc.dtype != torch.float32 or acc.dim() != 2 or acc.shape[0] < batch or not acc.is_contiguous():
+            raise ValueError("acc must be a contiguous float32 [B, tokens] tensor")
+        a.acc, a.acc_stride = acc.data_ptr(), acc.shape[1]
+    a.stream = _stream(stream)
+    L = lib()
+    need = L.pivot_cache4_attend_workspace_size(ctypes.byref(a))
+    if need:
+        buf = ws if ws is not None else workspace(need, q.device, stream)
+        a.workspace, a.workspace_bytes = buf.data_ptr(), buf.numel() * buf.element_size()
+    _check(L.pivot_cache4_attend(ctypes.byref(a)), "pivot_cache4_attend")
+    return out, lse
+
+
+def pivot_evict(acc, n_k, keep, arrays, from_map, to_map, sink=0, recent=0, out_keep=None, out_acc=None, ws=None,
+                stream=None):
+    """Keep the first `sink`, the last `recent` and the tokens of largest acc (fp32
+    [B, >= max n_k]), `keep` in all, and move every (src, dst) row array of
+    `arrays` (one row a token along the first dimension) with them, from from_map
+    to to_map.  Returns (kept positions int32 [B, keep], ascending, -1 past
+    min(n_k[b], keep), their acc fp32 [B, keep])."""
+    batch = len(n_k)
+    if acc.dtype != torch.float32 or acc.dim() != 2 or acc.shape[0] < batch or not acc.is_contiguous():
+        raise ValueError("acc must be a contiguous float32 [B, tokens] tensor")
+    if len(arrays) > PIVOT_EVICT_MAX_ARRAYS:
+        raise ValueError(f"at most {PIVOT_EVICT_MAX_ARRAYS} arrays move in one call")
+    out_keep = (torch.empty((batch, keep), dtype=torch.int32, device=acc.device) if out_keep is None
+                else _expect(out_keep, torch.int32, (batch, keep), "out_keep"))
+    out_acc = (torch.empty((batch, keep), dtype=torch.float32, device=acc.device) if out_acc is None
+               else _expect(out_acc, torch.float32, (batch, keep), "out_acc"))
+    a = pivot_evict_args()
+    nk = _host_ints(n_k)
+    a.batch, a.n_k = batch, ctypes.cast(nk, ctypes.POINTER(ctypes.c_int32))
+    a.acc, a.acc_stride = acc.data_ptr(), acc.shape[1]
+    a.keep, a.sink, a.recent = keep, sink, recent
+    a.out_keep, a.out_acc = out_keep.data_ptr(), out_acc.data_ptr()
+    a.n_arrays = len(arrays)
+    if arrays:
+        a.from_, a.to = from_map, to_map
+        _check_batch(from_map, batch, "from_map's block_table")
+        _check_batch(to_map, batch, "to_map's block_table")
+    for i, (src, dst) in enumerate(arrays):
+        if not src.is_contiguous() or not dst.is_contiguous() or src.dtype != dst.dtype or src.shape[1:] != dst.shape[1:]:
+            raise ValueError(f"array {i}: src and dst must be contiguous, of one type and row shape")
+        if from_map.rows > src.shape[0] or to_map.rows > dst.shape[0]:
+            raise ValueError(f"array {i} has fewer rows than its row map")
+        m = a.arrays[i]
+        m.src, m.dst = src.data_ptr(), dst.data_ptr()
+        m.row_bytes = src.element_size() * (src.numel() // max(src.shape[0], 1))
+    a.stream = _stream(stream)
+    L = lib()
+    need = L.pivot_evict_workspace_size(ctypes.byref(a))
+    if need:
+        buf = ws if ws is not None else workspace(need, acc.device, stream)
+        a.workspace, a.workspace_bytes = buf.data_ptr(), buf.numel() * buf.element_size()
+    _check(L.pivot_evict(ctypes.byref(a)), "pivot_evict")
+    return out_keep, out_acc

@@ -13,7 +13,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libpivot.so")
 BUILD_DIR = os.path.join(HERE, "_build")
 
-SOURCES = ["api.hip", "proxy.hip", "score.hip", "select.hip", "refine.hip"]
+SOURCES = ["api.hip", "proxy.hip", "score.hip", "select.hip", "refine.hip",
+           "api_ops.hip", "norm.hip", "cache4.hip", "attend.hip", "evict.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

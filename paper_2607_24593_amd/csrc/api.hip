@@ -11,6 +11,7 @@
 #include "launch.h"
 #include "mfma_tile.h"
 #include "pivot.h"
+#include "status.h"
 
 using namespace pivot;
 
@@ -20,8 +21,10 @@ using namespace pivot;
 static __device__ __align__(256) uint8_t scratch[PIVOT_NOALLOC_SCRATCH_BYTES];
 
 namespace {
-
 thread_local char g_err[512] = "";
+}
+
+namespace pivot {
 
 pivot_status fail(pivot_status s, const char* fmt, ...) {
   va_list ap;
@@ -35,6 +38,10 @@ pivot_status hip_check(hipError_t e, const char* what) {
   if (e == hipSuccess) return PIVOT_OK;
   return fail(PIVOT_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
+
+}  // namespace pivot
+
+namespace {
 
 // ---- optional per-kernel event timing (pivot_profile_begin / _end) ----
 struct ProfRecord {
