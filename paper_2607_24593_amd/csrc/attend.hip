@@ -8,6 +8,8 @@
 // lse = -infinity and adds nothing to acc.
 //
 // Scores are kept in base 2 (z log2 e), statistics and sums in fp32.
+#include <utility>
+
 #include "cache4.h"
 #include "dpp.h"
 #include "ops.h"
@@ -30,94 +32,662 @@ struct ScoreMap {
   int64_t base[kMaxSeq];
 };
 
-__device__ __forceinline__ float block_max(float v, float* red, int tid) {
-  v = wave_reduce(v, [](float a, float b) { return fmaxf(a, b); });
-  __syncthreads();
-  if ((tid & 63) == 0) red[tid >> 6] = v;
-  __syncthreads();
-  return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
+
+#define LDS(type, p) ((__attribute__((address_space(3))) type*)(p))
+
+// Sixteen (or four) bytes of every lane from memory into LDS at byte address dst
+// + 16 (4) * lane, dst the same in all lanes of the wave.  Written out, because
+// the compiler waits for all such loads before any read of LDS that it cannot
+// tell apart from their target; the tile loop waits for them itself, before the
+// barrier that hands the tile over.
+__device__ __forceinline__ void load_lds16(const void* src, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(src) : "memory");
 }
-__device__ __forceinline__ float block_sum(float v, float* red, int tid) {
-  v = wave_reduce(v, [](float a, float b) { return a + b; });
-  __syncthreads();
-  if ((tid & 63) == 0) red[tid >> 6] = v;
-  __syncthreads();
-  return (red[0] + red[1]) + (red[2] + red[3]);
+__device__ __forceinline__ void load_lds4(const void* src, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(dst), "v"(src) : "memory");
 }
 
-// One workgroup per (query row, head): a thread scores one key of a chunk of
-// 256, then owns two of the 512 output values over the chunk's keys.
-__global__ __launch_bounds__(256) void attend_kernel(AttendArgs a, RunTable t, ScoreMap sm) {
-  __shared__ float q[kAttnDim];
-  __shared__ float p[256];
-  __shared__ int64_t krow[256];
-  __shared__ float red[4];
-  const int tid = threadIdx.x, head = blockIdx.x, r = blockIdx.y;
-  const int b = run_of(t, r), i = r - t.row0[b];
-  const int pos = t.pos0[b] + i;
-  const uint16_t* qp = a.q + r * a.q_row + head * a.q_head;
-  for (int e = tid; e < kAttnDim; e += 256) q[e] = __uint_as_float((uint32_t)qp[e] << 16);
-  const float c = a.scale * kLog2e;
-  const int n = a.idx ? a.topk : pos + 1;
-  const int unit_rows = a.idx ? a.heads : t.n_rows[b] * a.heads;
-  const int unit_row = a.idx ? head : i * a.heads + head;
-  const int padded = a.idx ? (a.topk + kTileKeys - 1) / kTileKeys * kTileKeys
-                           : (t.pos0[b] + t.n_rows[b] + kTileKeys - 1) / kTileKeys * kTileKeys;
-  const int64_t base = a.idx ? (int64_t)r * unit_rows * padded : sm.base[b];
-  float m = -INFINITY, l = 0.f, o0 = 0.f, o1 = 0.f;
-  for (int k0 = 0; k0 < (sm.s2 ? padded : n); k0 += 256) {
-    const int k = k0 + tid;
-    int key = -1;
-    if (k < n) key = a.idx ? a.idx[(int64_t)r * a.topk + k] : k;
-    if (key > pos) key = -1;
-    float s = -INFINITY;
-    int64_t row = 0;
-    if (key >= 0) {
-      row = a.map.row(b, key);
-      float dot = 0.f;
-      for (int j = 0; j < kLatent / 8; ++j) {
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(a.cache.codes + row * kCodeBytes + 4 * j);
-        const uint4 v = decode8(w, scale_operand(a.cache.scales[row * kScaleBytes + j / 4]));
-        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+// x *= f for a value in the accumulation registers.  Written out: as plain code
+// the compiler moves the whole output into vector registers ahead of the test
+// whether it is to be scaled, in every tile.  The callers leave the waits between
+// these and the matrix products around them.
+__device__ __forceinline__ void scale_acc(float& x, float f) {
+  float v;
+  asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(x));
+  v *= f;
+  asm volatile("v_accvgpr_write_b32 %0, %1" : "=a"(x) : "v"(v));
+}
+
+// f(0), f(1), ..., f(N - 1) with the index a constant
+template <class F, int... I>
+__device__ __forceinline__ void unroll(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void unroll(F&& f) {
+  unroll(f, std::make_integer_sequence<int, N>{});
+}
+// Pieces [0, PIECES) of other work, spread over the steps of a loop of STEPS:
+// those that belong after step S.
+template <int STEPS, int PIECES, int S, class F>
+__device__ __forceinline__ void pieces_after(F&& piece) {
+  constexpr int lo = S * PIECES / STEPS, hi = (S + 1) * PIECES / STEPS;
+  unroll<hi - lo>([&](auto i) { piece(std::integral_constant<int, lo + i>{}); });
+}
+
+// The largest / the sum of a value over the four lane groups of 16 lanes.
+__device__ __forceinline__ float groups_max(float x) {
+  auto e = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(e[0]), __uint_as_float(e[1]));
+  e = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(e[0]), __uint_as_float(e[1]));
+}
+__device__ __forceinline__ float groups_sum(float x) {
+  auto e = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(e[0]) + __uint_as_float(e[1]);
+  e = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(e[0]) + __uint_as_float(e[1]);
+}
+
+// Sixteen query rows as the second operand of the 16x16x32 score products: lane
+// (row r, group g) has values 32 k + 8 g .. + 7 of product k.
+struct QueryFrag {
+  v4i v[kAttnDim / 32];
+
+  __device__ __forceinline__ void load(const uint16_t* row, int lane) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          dot = fmaf(q[8 * j + 2 * e], __uint_as_float(u[e] << 16), dot);
-          dot = fmaf(q[8 * j + 2 * e + 1], __uint_as_float(u[e] & 0xFFFF0000u), dot);
+    for (int k = 0; k < kAttnDim / 32; ++k) v[k] = *reinterpret_cast<const v4i*>(row + 32 * k + 8 * (lane >> 4));
+  }
+};
+
+// LDS.  As loaded, a wave's 1024 bytes (4 keys' codes, 8 keys' position values)
+// are a group, the groups 1088 bytes apart; the 16-byte chunks of a row change
+// places by two bits of the key.  Together the two put one chunk of 16 keys,
+// which a score operand reads at once, into 16 different bank groups.
+constexpr int kGroup = 1024 + 64;
+constexpr int kCodesBytes = kTileKeys / 4 * kGroup, kRopeBytes = kTileKeys / 8 * kGroup;
+// The widened latent values are rows of 64 chunks of 8 values, chunk c of key k
+// at c ^ swizzle(k): conflict free for a chunk of 16 consecutive keys (scores)
+// as for 4 neighbouring chunks of keys 4 n .. 4 n + 3 (the transposed reads).
+constexpr int kValueBytes = kTileKeys * 2 * kLatent;
+__device__ __forceinline__ int swizzle(int key) { return (key & 3) << 2 | (key >> 2 & 3); }
+// Weights: rows of 32 high parts, then 32 low parts.
+constexpr int kWeightStride = 4 * kTileKeys + 16;
+
+// What one launch's workgroups are: units (query rows of an index-set call,
+// else sequences) x splits of the unit's keys x tiles of 16 RG rows.
+struct Work {
+  int units, splits, tiles_per_split, row_tiles;
+  float4* part_o;
+  float2* part_ml;  // reference, sum
+};
+
+// A workgroup attends 16 RG rows (heads of one query; in a prefix call heads of
+// consecutive queries of a sequence) to one split of their keys, 32 at a time.
+// Four stages, each on a tile of its own between two barriers:
+//   load    the tile's rows into LDS;
+//   widen   codes to bf16 in LDS (8 keys a wave), exact;
+//   score   transposed, keys x rows: a lane has 4 keys of a row, so maxima and
+//           sums need two lane swaps.  The reference m only moves when a score
+//           passes it by more than 32 (the weights, their sums and the output have
+//           fp32's range, so none comes near its end), and the output is hardly
+//           ever rescaled.  A weight goes to LDS as two bf16, 16 bits
+//           of it: one bf16 would round it by up to 2^-8, as much as the output's
+//           own rounding, and fp16 would lose the small ones;
+//   output  transposed, values x rows: a wave has 128 of the 512 values for all
+//           rows, and the values are read transposed once per tile.
+// Score waves have 32 rows x 16 keys (RG = 4), or 16 x 16 (2, and 1 with two of
+// the four waves).
+//
+// One wave per SIMD holds its query (144 registers for 32 rows) and output (128),
+// so nothing but its own instructions hides a latency.  Operands are therefore
+// read from LDS some steps ahead, and the vector work of the other stages is
+// cut into pieces that are issued between the matrix products, which run on
+// their own once issued.  Scheduling barriers keep the compiler from sorting
+// the two apart again.
+template <int RG>
+__global__ __launch_bounds__(256, 1) void attend_kernel(AttendArgs a, RunTable t, ScoreMap sm, Work wk) {
+  constexpr int ROWS = 16 * RG;
+  constexpr int KT = kTileKeys;
+  constexpr int NRT = RG == 4 ? 2 : 1;         // row tiles of 16 per wave
+  constexpr int CT = RG == 1 ? 1 : RG / 2;     // output column tiles (of 32 rows, or of 16)
+  constexpr int NQ = RG == 1 ? 8 : 16 * CT;    // output registers per lane / 4
+  constexpr int WB = ROWS * kWeightStride;
+  __shared__ __attribute__((aligned(16))) uint8_t s_val[3 * kValueBytes];
+  __shared__ __attribute__((aligned(16))) uint8_t s_codes[2 * kCodesBytes];
+  __shared__ __attribute__((aligned(16))) uint8_t s_scale[2 * 4 * 256];  // 8 keys a wave, twice
+  __shared__ __attribute__((aligned(16))) uint8_t s_rope[3 * kRopeBytes];
+  __shared__ __attribute__((aligned(16))) int s_pos[3 * KT];
+  __shared__ __attribute__((aligned(16))) uint8_t s_w[2 * WB];
+  __shared__ __attribute__((aligned(16))) float s_nan[2 * KT];              // NaN for a key with a NaN block, else 0
+  __shared__ __attribute__((aligned(16))) float s_scalef[KT * kScaleBytes];  // the scales as conversion operands
+  __shared__ float s_alpha[2][ROWS], s_max[2][ROWS], s_sum[2][ROWS];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // consecutive work items share an XCD (workgroups go to the 8 XCDs in turn)
+  const int total = wk.units * wk.splits * wk.row_tiles;
+  const int xcd = blockIdx.x & 7, per = total >> 3, rem = total & 7;
+  const int item = xcd * per + min(xcd, rem) + (int)(blockIdx.x >> 3);
+  const int rt = item % wk.row_tiles, split = item / wk.row_tiles % wk.splits, unit = item / wk.row_tiles / wk.splits;
+  const bool sets = a.idx != nullptr;
+  const int b = sets ? run_of(t, unit) : unit;
+  const int unit_rows = sets ? a.heads : t.n_rows[b] * a.heads;
+  const int first = rt * ROWS;
+  if (first >= unit_rows) return;
+  const int rows = min(ROWS, unit_rows - first);
+  const int i_first = sets ? unit - t.row0[b] : 0;                       // the unit's first query in its sequence
+  const int pos_last = t.pos0[b] + (sets ? i_first : (first + rows - 1) / a.heads);
+  // kept scores cover the unit's keys for every row
+  const int n = sets ? a.topk : sm.s2 ? t.pos0[b] + t.n_rows[b] : pos_last + 1;
+  const int all_tiles = (n + KT - 1) / KT;
+  const int t0 = split * wk.tiles_per_split, t1 = min(all_tiles, t0 + wk.tiles_per_split);
+  const int64_t part = ((int64_t)unit * wk.row_tiles + rt) * wk.splits + split;
+  if (t0 >= t1 && wk.splits > 1) {
+    if (tid < ROWS) wk.part_ml[part * ROWS + tid] = {-INFINITY, 0.f};
+    return;
+  }
+
+  const int kt = RG == 1 ? w : w >> 1;             // the wave's 16 keys of a tile,
+  const int row0 = RG == 1 ? 0 : 16 * NRT * (w & 1);  // and its first row of scores
+  const bool scoring = RG != 1 || w < 2;
+
+  // Keys 8 w + (lane & 7) of a tile, found in three steps a tile apart, so that
+  // no step waits for its load: the set's entry; the page of its position; the
+  // cache row.
+  const int32_t* idx = sets ? a.idx + (int64_t)unit * a.topk : nullptr;
+  const int32_t* pages = a.map.pages ? a.map.pages + (int64_t)b * a.map.max_pages : nullptr;
+  auto fetch = [&](int ln, int tile) {
+    const int k = min(tile * KT + 8 * w + (ln & 7), n - 1);
+    return sets ? idx[k] : k;
+  };
+  // pos: the position whose row is loaded (0 for keys that do not count), at: the one that masks the key
+  auto place = [&](int ln, int tile, int entry, int& pos, int& at) {
+    const bool ok = ((uint32_t)entry <= (uint32_t)pos_last) & (tile < t1) & (tile * KT + 8 * w + (ln & 7) < n);
+    pos = ok ? entry : 0;
+    at = ok ? entry : 0x7FFFFFFF;
+    return pages ? pages[pos >> a.map.shift] : 0;
+  };
+  auto locate = [&](int pos, int page) -> int {
+    if (!pages) return (int)(b * a.map.stride) + pos;
+    return (min(max(page, 0), a.map.n_pages - 1) << a.map.shift) | (pos & ((1 << a.map.shift) - 1));
+  };
+  const uint32_t codes0 = (uint32_t)(uintptr_t)LDS(uint8_t, s_codes), rope0 = (uint32_t)(uintptr_t)LDS(uint8_t, s_rope),
+                 scale0 = (uint32_t)(uintptr_t)LDS(uint8_t, s_scale);
+  const float c = a.scale * kLog2e;
+  QueryFrag q[NRT];
+  int limit[NRT];  // the last position a row attends to; rows past the last one take its query, masked
+#pragma unroll
+  for (int r = 0; r < NRT; ++r) {
+    const int mine = row0 + 16 * r + (lane & 15), flat = first + min(mine, rows - 1);
+    const int i = sets ? 0 : flat / a.heads, head = flat - i * a.heads;
+    limit[r] = mine < rows ? t.pos0[b] + i_first + i : -1;
+    if (scoring) q[r].load(a.q + ((int64_t)t.row0[b] + i_first + i) * a.q_row + (int64_t)head * a.q_head, lane);
+  }
+  float m[NRT], l[NRT];
+#pragma unroll
+  for (int r = 0; r < NRT; ++r) m[r] = -INFINITY, l[r] = 0.f;
+  v16f o[4][CT];
+  v4f o1[8];
+#pragma unroll
+  for (int x = 0; x < 4; ++x)
+#pragma unroll
+    for (int y = 0; y < CT; ++y)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[x][y][i] = 0.f;
+#pragma unroll
+  for (int x = 0; x < 8; ++x) o1[x] = v4f{0.f, 0.f, 0.f, 0.f};
+  float* s2 = nullptr;  // the workgroup's rows in the unit's first tile of kept scores
+  if (sm.s2) {
+    const int64_t padded = (a.topk + KT - 1) / KT * KT;
+    s2 = sm.s2 + (sets ? (int64_t)unit * unit_rows * padded : sm.base[b]) + (int64_t)first * KT;
+  }
+
+  // ---- the stages, in pieces; slot2 / slot3: a tile's place of two / of three
+  int at = 0, pos = 0, page = 0, entry = 0;  // of the next tile to be loaded; the entry of the one after
+  int row = 0;
+  auto load_piece = [&](int ln, int tile, int slot2, int slot3, auto piece) {
+    constexpr int P = piece;
+    if constexpr (P == 0) {
+      row = locate(pos, page);
+    } else if constexpr (P == 1 || P == 2) {
+      const int key = ln >> 4;  // of 4
+      const int64_t r = __shfl(row, 4 * (P - 1) + key, 64);
+      load_lds16(a.cache.codes + r * kCodeBytes + (((ln & 15) ^ key) << 4),
+                 codes0 + slot2 * kCodesBytes + (2 * w + P - 1) * kGroup);
+    } else if constexpr (P == 3) {
+      const int key = ln >> 3;  // of 8
+      const int64_t r = __shfl(row, key, 64);
+      load_lds16(reinterpret_cast<const uint8_t*>(a.cache.rope) + r * (2 * kRope) + (((ln & 7) ^ (key >> 1)) << 4),
+                 rope0 + slot3 * kRopeBytes + w * kGroup);
+    } else if constexpr (P == 4) {
+      const int64_t r = __shfl(row, ln >> 2 & 7, 64);
+      load_lds4(a.cache.scales + r * kScaleBytes + 4 * (ln & 3), scale0 + (4 * slot2 + w) * 256);
+      s_pos[slot3 * KT + 8 * w + (ln & 7)] = at;
+    } else if constexpr (P == 5) {
+      page = place(ln, tile + 1, entry, pos, at);
+    } else {
+      entry = fetch(ln, tile + 2);
+    }
+  };
+  constexpr int LOADS = 7;
+
+  // lane l: the scales of four blocks (l / 8 modulo 4) of the wave's key l & 7
+  uint32_t scale4 = 0;
+  auto scale_piece = [&](int ln, int slot2, auto piece) {
+    constexpr int P = piece;
+    const int key = ln & 7, part4 = ln >> 3 & 3;
+    if constexpr (P == 0) {
+      scale4 = *reinterpret_cast<const uint32_t*>(s_scale + (4 * slot2 + w) * 256 + key * kScaleBytes + part4 * 4);
+    } else if constexpr (P == 1) {
+      uint4 f;
+      uint32_t* p = &f.x;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        // a NaN block makes the key's scores NaN through s_nan; as a value it must
+        // not reach the rows that do not attend to the key (0 * NaN)
+        const int byte = scale4 >> (8 * i) & 255u;
+        p[i] = (uint32_t)(byte & ((byte - 255) >> 31)) << 23;
+      }
+      *reinterpret_cast<uint4*>(&s_scalef[(8 * w + key) * kScaleBytes + part4 * 4]) = f;
+    } else {
+      const uint32_t n = ~scale4;  // a zero byte of it is a byte of 255
+      const uint64_t any = __builtin_amdgcn_ballot_w64(((n - 0x01010101u) & ~n & 0x80808080u) != 0);
+      const uint32_t of = (uint32_t)any;  // lanes 0 .. 31 have every block
+      const uint32_t keys = of | of >> 8 | of >> 16 | of >> 24;
+      s_nan[slot2 * KT + 8 * w + key] = keys >> key & 1 ? __builtin_nanf("") : 0.f;
+    }
+  };
+  constexpr int SCALES = 3;
+
+  // one key at a time, 8 values a lane
+  uint32_t word[2];
+  float wscale[2];
+  auto widen_piece = [&](int ln, int slot2, int slot3, auto piece) {
+    constexpr int j = piece / 2;
+    if constexpr (piece % 2 == 0) {
+      word[j & 1] = *reinterpret_cast<const uint32_t*>(s_codes + slot2 * kCodesBytes + 2 * w * kGroup +
+                                                       ((4 * ln) ^ ((j & 3) << 4)) + j / 4 * kGroup + (j & 3) * kCodeBytes);
+      wscale[j & 1] = s_scalef[8 * w * kScaleBytes + (ln >> 2) + j * kScaleBytes];
+    } else {
+      *reinterpret_cast<uint4*>(s_val + slot3 * kValueBytes + (8 * w + j) * 2 * kLatent +
+                                (16 * ln ^ (swizzle(8 * w + j) << 4))) = decode8(word[j & 1], wscale[j & 1]);
+    }
+  };
+  constexpr int WIDENS = 16;
+
+  // scores of the wave's rows and keys, operands read DEPTH products ahead
+  v4f s[NRT];
+  auto score = [&](int ln, int slot3, auto after) {
+    constexpr int STEPS = kAttnDim / 32, DEPTH = 5;
+    const int key = ln & 15, g = ln >> 4;
+    const uint8_t* val = s_val + slot3 * kValueBytes + (16 * kt + key) * 2 * kLatent;
+    const uint32_t at0 = (uint32_t)((g ^ swizzle(key)) << 4);
+    const uint8_t* rope = s_rope + slot3 * kRopeBytes + (key >> 3) * kGroup + (key & 7) * 2 * kRope +
+                          ((g ^ ((key >> 1) & 3)) << 4) + 2 * kt * kGroup;
+    v4i x[STEPS];
+    auto read = [&](auto k) {
+      x[k] = *reinterpret_cast<const v4i*>(k < kLatent / 32 ? val + (at0 ^ ((k & 3) << 6)) + (k >> 2) * 256
+                                                            : rope + 64 * (k - kLatent / 32));
+    };
+    unroll<DEPTH>(read);
+#pragma unroll
+    for (int r = 0; r < NRT; ++r) s[r] = v4f{0.f, 0.f, 0.f, 0.f};
+    unroll<STEPS>([&](auto k) {
+      if constexpr (k + DEPTH < STEPS) read(std::integral_constant<int, k + DEPTH>{});
+#pragma unroll
+      for (int r = 0; r < NRT; ++r)
+        s[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, x[k]), __builtin_bit_cast(v8bf, q[r].v[k]),
+                                                       s[r], 0, 0, 0);
+      after(k, std::integral_constant<int, STEPS>{});
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+
+  // maxima of the wave's scores to s_max; tile: the unit's tile, for the kept scores
+  auto maxima = [&](int ln, int tile, int slot2, int slot3) {
+    const int key = ln & 15, g = ln >> 4, k4 = 16 * kt + 4 * g;
+    const v4i key_at = *reinterpret_cast<const v4i*>(&s_pos[slot3 * KT + k4]);
+    const v4f bad = *reinterpret_cast<const v4f*>(&s_nan[slot2 * KT + k4]);
+#pragma unroll
+    for (int r = 0; r < NRT; ++r) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s[r][i] = key_at[i] <= limit[r] ? fmaf(s[r][i], c, bad[i]) : -INFINITY;
+        top = fmaxf(top, s[r][i]);
+      }
+      if (s2 && tile < t1 && row0 + 16 * r + key < rows)
+        *reinterpret_cast<v4f*>(s2 + (int64_t)tile * unit_rows * KT + ((row0 + 16 * r + key) * KT + k4)) = s[r];
+      top = groups_max(top);
+      s_max[kt][row0 + 16 * r + key] = top;
+    }
+  };
+  // the scores' weights to s_w[slot2]
+  float ref[NRT], alpha[NRT], e[NRT][4];
+  v4bf hi[NRT];
+  auto weigh_piece = [&](int ln, int slot2, auto piece) {
+    constexpr int r = piece / 5, P = piece % 5;
+    const int key = ln & 15, g = ln >> 4, mine = row0 + 16 * r + key;
+    if constexpr (P == 0) {
+      const float top = fmaxf(s_max[0][mine], s_max[1][mine]);
+      const bool move = top > m[r] + 32.f;
+      const float next = move ? top : m[r];
+      alpha[r] = move ? __builtin_amdgcn_exp2f(m[r] - next) : 1.f;
+      ref[r] = next == -INFINITY ? 0.f : next;
+      m[r] = next;
+    } else if constexpr (P == 1 || P == 2) {
+#pragma unroll
+      for (int i = 2 * P - 2; i < 2 * P; ++i) e[r][i] = __builtin_amdgcn_exp2f(s[r][i] - ref[r]);
+    } else if constexpr (P == 3) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) hi[r][i] = (__bf16)e[r][i];
+      l[r] = fmaf(l[r], alpha[r], (e[r][0] + e[r][1]) + (e[r][2] + e[r][3]));
+      s_alpha[slot2][mine] = alpha[r];
+    } else {
+      v4bf lo;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) lo[i] = (__bf16)(e[r][i] - (float)hi[r][i]);
+      uint8_t* to = s_w + slot2 * WB + mine * kWeightStride + 32 * kt + 8 * g;
+      *reinterpret_cast<v4bf*>(to) = hi[r];
+      *reinterpret_cast<v4bf*>(to + 2 * KT) = lo;
+    }
+  };
+  constexpr int WEIGHS = 5 * NRT;
+
+  auto output = [&](int ln, int slot3, int slot2, auto after) {
+    const uint8_t* wgt = s_w + slot2 * WB;
+    const int g = ln >> 4, quad = (ln & 15) >> 2;
+    // RG = 1: keys 8 g + 4 r + quad, chunks 16 w + 2 x + (ln & 3) / 2; else keys
+    // 16 k + 8 h + 4 r + quad, chunks 16 w + 4 x + 2 (g & 1) + (ln & 3) / 2
+    constexpr int VS = RG == 1 ? 8 : 8, AHEAD = 2;  // reads of values; read two ahead
+    const int h = ln >> 5;
+    const uint8_t* base = s_val + slot3 * kValueBytes + (8 * (RG == 1 ? g : h) + quad) * 2 * kLatent + 256 * w + 8 * (ln & 1);
+    const uint32_t at0 = RG == 1 ? (uint32_t)((((ln & 3) >> 1) ^ (4 * quad + (2 * g & 3))) << 4)
+                                 : (uint32_t)((4 * quad + ((2 * (g & 1) + ((ln & 3) >> 1)) ^ (2 * h))) << 4);
+    v4s v0[VS], v1[VS];
+    auto read = [&](auto x) {
+      const uint8_t* from = base + (RG == 1 ? 0 : x / 4 * 16 * 2 * kLatent);
+      const uint32_t d = RG == 1 ? (uint32_t)(x << 5) : (uint32_t)(x % 4 << 6);
+      v0[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, from + (at0 ^ d)));
+      v1[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, from + (at0 ^ d ^ 16) + 4 * 2 * kLatent));
+    };
+    v8bf wt[2][2][CT];  // [k][high, low][row tile]
+    auto read_weights = [&](int k) {
+#pragma unroll
+      for (int y = 0; y < CT; ++y) {
+        const uint8_t* wp = RG == 1 ? wgt + (ln & 15) * kWeightStride + 16 * g
+                                    : wgt + (32 * y + (ln & 31)) * kWeightStride + 32 * k + 16 * h;
+        wt[k][0][y] = __builtin_bit_cast(v8bf, *reinterpret_cast<const v4i*>(wp));
+        wt[k][1][y] = __builtin_bit_cast(v8bf, *reinterpret_cast<const v4i*>(wp + 2 * KT));
+      }
+    };
+    read_weights(0);
+    unroll<AHEAD>(read);
+    if constexpr (RG == 1) {
+      const float al = s_alpha[slot2][ln & 15];
+      if (__any(al != 1.f)) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float v = o1[x][i];
+            scale_acc(v, al);
+            o1[x][i] = v;
+          }
+        asm volatile("s_nop 7\n\ts_nop 7" ::: "memory");
+      }
+    } else {
+#pragma unroll
+      for (int y = 0; y < CT; ++y) {
+        const float al = s_alpha[slot2][32 * y + (ln & 31)];
+        if (__any(al != 1.f)) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              float v = o[x][y][i];
+              scale_acc(v, al);
+              o[x][y][i] = v;
+            }
+          asm volatile("s_nop 7\n\ts_nop 7" ::: "memory");
         }
       }
-      for (int e = 0; e < kRope; ++e)
-        dot = fmaf(q[kLatent + e], __uint_as_float((uint32_t)a.cache.rope[row * kRope + e] << 16), dot);
-      s = dot * c;
     }
-    if (sm.s2 && k < padded)
-      sm.s2[base + ((int64_t)(k / kTileKeys) * unit_rows + unit_row) * kTileKeys + k % kTileKeys] = s;
-    const float top = fmaxf(m, block_max(s, red, tid));
-    const float ref = top == -INFINITY ? 0.f : top;
-    const float alpha = exp2f(m - ref);
-    m = top;
-    const float e = exp2f(s - ref);
-    p[tid] = e;
-    krow[tid] = row;
-    l = l * alpha + block_sum(e, red, tid);
-    o0 *= alpha;
-    o1 *= alpha;
-    const int count = min(256, n - k0);
-    for (int j = 0; j < count; ++j) {
-      if (p[j] == 0.f) continue;
-      const uint32_t w = a.cache.codes[krow[j] * kCodeBytes + tid];
-      const uint4 v = decode8(w, scale_operand(a.cache.scales[krow[j] * kScaleBytes + tid / 16]));
-      o0 = fmaf(p[j], __uint_as_float(v.x << 16), o0);
-      o1 = fmaf(p[j], __uint_as_float(v.x & 0xFFFF0000u), o1);
+    __builtin_amdgcn_sched_barrier(0);
+    unroll<VS>([&](auto x) {
+      if constexpr (x + AHEAD < VS) read(std::integral_constant<int, x + AHEAD>{});
+      if constexpr (RG != 1 && x == 1) read_weights(1);
+      const v8bf v = __builtin_bit_cast(v8bf, __builtin_shufflevector(v0[x], v1[x], 0, 1, 2, 3, 4, 5, 6, 7));
+      constexpr int k = RG == 1 ? 0 : x / 4;
+      unroll<2 * CT>([&](auto u) {  // high parts of the row tiles, then low ones
+        constexpr int part = u / CT, y = u % CT;
+        if constexpr (RG == 1) {
+          o1[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, wt[0][part][0], o1[x], 0, 0, 0);
+        } else {
+          o[x % 4][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, wt[k][part][y], o[x % 4][y], 0, 0, 0);
+        }
+        after(std::integral_constant<int, x * 2 * CT + u>{}, std::integral_constant<int, VS * 2 * CT>{});
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    });
+  };
+  auto nothing = [](auto, auto) {};
+
+  const int count = t1 - t0;
+  if (count > 0) {
+    // tiles 0 .. 2 loaded, 0 and 1 widened, 0 scored
+    const int entry0 = fetch(lane, t0);
+    entry = fetch(lane, t0 + 1);
+    page = place(lane, t0, entry0, pos, at);
+    unroll<LOADS>([&](auto p) { load_piece(lane, t0, 0, 0, p); });
+    unroll<LOADS>([&](auto p) { load_piece(lane, t0 + 1, 1, 1, p); });
+    // the query is in registers before the loop (its waits would fall inside it)
+#pragma unroll
+    for (int r = 0; r < NRT; ++r)
+#pragma unroll
+      for (int k = 0; k < kAttnDim / 32; k += 2) asm volatile("s_waitcnt vmcnt(0)" : "+v"(q[r].v[k]), "+v"(q[r].v[k + 1]));
+    asm volatile("s_waitcnt vmcnt(0)" : "+v"(entry), "+v"(page)::"memory");
+    __syncthreads();
+    auto widen_all = [&](int slot) {
+      unroll<SCALES>([&](auto p) { scale_piece(lane, slot, p); });
+      unroll<WIDENS>([&](auto p) { widen_piece(lane, slot, slot, p); });
+    };
+    widen_all(0);
+    __syncthreads();
+    unroll<LOADS>([&](auto p) { load_piece(lane, t0 + 2, 0, 2, p); });
+    if (scoring) {
+      score(lane, 0, nothing);
+      maxima(lane, t0, 0, 0);
     }
     __syncthreads();
+    if (scoring) unroll<WEIGHS>([&](auto p) { weigh_piece(lane, 0, p); });
+    widen_all(1);
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  const int64_t orow = (int64_t)r * a.heads + head;
-  *reinterpret_cast<uint32_t*>(a.out + orow * kLatent + 2 * tid) =
-      (uint32_t)bf16_rne(o0 * inv) | ((uint32_t)bf16_rne(o1 * inv) << 16);
-  if (tid == 0) {
-    if (a.lse) a.lse[orow] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
-    if (sm.stat) sm.stat[orow] = {m == -INFINITY ? 0.f : m, inv};
+  // Iteration i: tile i + 3 is loaded, i + 2 widened, i + 1 scored, i put out
+  // (past the last tile masked ones, of row 0).
+  int slot3 = 0;
+  for (int i = 0; i < count; ++i) {
+    int ln = lane;  // addresses are made anew for every tile rather than kept in registers
+    asm volatile("" : "+v"(ln));
+    const int next3 = slot3 == 2 ? 0 : slot3 + 1, after3 = next3 == 2 ? 0 : next3 + 1;  // of i + 1, i + 2
+    // every load is done, the entry and the page too (named here, so that the
+    // compiler waits for them nowhere else)
+    asm volatile("s_waitcnt vmcnt(0)" : "+v"(entry), "+v"(page)::"memory");
+    __syncthreads();
+    const auto during_score = [&](auto step, auto steps) {
+      pieces_after<steps, LOADS + SCALES, step>([&](auto p) {
+        if constexpr (p < LOADS) load_piece(ln, t0 + i + 3, (i + 1) & 1, slot3, p);
+        else scale_piece(ln, i & 1, std::integral_constant<int, p - LOADS>{});
+      });
+    };
+    if (scoring) {
+      score(ln, next3, during_score);
+      maxima(ln, t0 + i + 1, (i + 1) & 1, next3);
+    } else {
+      unroll<LOADS + SCALES>([&](auto p) { during_score(p, std::integral_constant<int, LOADS + SCALES>{}); });
+    }
+    __syncthreads();
+    if (scoring) {
+      output(ln, slot3, i & 1, [&](auto step, auto steps) {
+        pieces_after<steps, WIDENS + WEIGHS, step>([&](auto p) {
+          // weights first: two pieces of them for three of widening
+          if constexpr (p < WEIGHS) weigh_piece(ln, (i + 1) & 1, p);
+          else widen_piece(ln, i & 1, after3, std::integral_constant<int, p - WEIGHS>{});
+        });
+      });
+    } else {
+      output(ln, slot3, i & 1, [&](auto step, auto steps) {
+        pieces_after<steps, WIDENS, step>([&](auto p) { widen_piece(ln, i & 1, after3, p); });
+      });
+    }
+    slot3 = next3;
+  }
+  // no load into LDS may outlive the workgroup
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+
+  // the rows' statistics
+  const int g = lane >> 4;
+  __syncthreads();
+  if (scoring) {
+#pragma unroll
+    for (int r = 0; r < NRT; ++r) {
+      l[r] = groups_sum(l[r]);
+      if (g == 0) {
+        const int mine = row0 + 16 * r + lane;
+        s_sum[kt][mine] = l[r];
+        s_max[0][mine] = m[r];  // both waves of the rows hold the same
+      }
+    }
+  }
+  __syncthreads();
+  if (wk.splits > 1) {
+    if (tid < ROWS) wk.part_ml[part * ROWS + tid] = {s_max[0][tid], s_sum[0][tid] + s_sum[1][tid]};
+    // the registers as they lie: the joining kernel has the same lanes
+    float4* po = wk.part_o + part * NQ * 256 + tid;
+    if constexpr (RG == 1) {
+#pragma unroll
+      for (int x = 0; x < 8; ++x) po[x * 256] = float4{o1[x][0], o1[x][1], o1[x][2], o1[x][3]};
+    } else {
+#pragma unroll
+      for (int y = 0; y < CT; ++y)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            po[((4 * y + x) * 4 + i) * 256] =
+                float4{o[x][y][4 * i], o[x][y][4 * i + 1], o[x][y][4 * i + 2], o[x][y][4 * i + 3]};
+    }
+    return;
+  }
+  const int64_t orow = ((int64_t)t.row0[b] + i_first) * a.heads + first;
+  if (tid < rows) {
+    const float sum = s_sum[0][tid] + s_sum[1][tid], top = s_max[0][tid];
+    if (a.lse) a.lse[orow + tid] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+    if (sm.stat) sm.stat[orow + tid] = {top == -INFINITY ? 0.f : top, sum == 0.f ? 0.f : 1.f / sum};
+  }
+  // 32 rows (16) at a time through LDS, so that whole rows are written
+  constexpr int OS = 2 * kLatent + 16, OR = RG == 1 ? 16 : 32;
+#pragma unroll
+  for (int y = 0; y < CT; ++y) {
+    const int row = 32 * y + (RG == 1 ? lane & 15 : lane & 31);
+    const float sum = s_sum[0][row] + s_sum[1][row], inv = sum == 0.f ? 0.f : 1.f / sum;
+    uint8_t* to = s_val + (row - 32 * y) * OS;
+    if constexpr (RG == 1) {
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        v4bf v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (__bf16)(o1[x][i] * inv);
+        *reinterpret_cast<v4bf*>(to + 2 * (128 * w + 16 * x + 4 * g)) = v;
+      }
+    } else {
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          v4bf v;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = (__bf16)(o[x][y][4 * j + i] * inv);
+          *reinterpret_cast<v4bf*>(to + 2 * (128 * w + 32 * x + 8 * j + 4 * (lane >> 5))) = v;
+        }
+    }
+    __syncthreads();
+    for (int r = w; r < OR && 32 * y + r < rows; r += 4)
+      *reinterpret_cast<uint4*>(a.out + (orow + 32 * y + r) * kLatent + 8 * lane) =
+          *reinterpret_cast<const uint4*>(s_val + r * OS + 16 * lane);
+    if (y + 1 < CT) __syncthreads();
+  }
+}
+
+// Joins the splits of a row tile: blockIdx.x a chunk of the lanes' registers,
+// blockIdx.y the row tile.
+template <int RG>
+constexpr int kJoinQuads = RG == 1 ? 2 : 4;
+template <int RG>
+__global__ __launch_bounds__(256) void join_kernel(AttendArgs a, RunTable t, ScoreMap sm, Work wk) {
+  constexpr int ROWS = 16 * RG;
+  constexpr int CT = RG == 1 ? 1 : RG / 2;
+  constexpr int NQ = RG == 1 ? 8 : 16 * CT;
+  constexpr int JQ = kJoinQuads<RG>;
+  extern __shared__ float s_w[];  // [splits][ROWS]
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int unit = blockIdx.y / wk.row_tiles, rt = blockIdx.y % wk.row_tiles;
+  const bool sets = a.idx != nullptr;
+  const int b = sets ? run_of(t, unit) : unit;
+  const int unit_rows = sets ? a.heads : t.n_rows[b] * a.heads;
+  const int first = rt * ROWS;
+  if (first >= unit_rows) return;
+  const int rows = min(ROWS, unit_rows - first);
+  const int64_t orow = ((int64_t)t.row0[b] + (sets ? unit - t.row0[b] : 0)) * a.heads + first;
+  const int64_t part = (int64_t)blockIdx.y * wk.splits;
+  const float2* ml = wk.part_ml + part * ROWS;
+  if (tid < ROWS) {
+    float top = -INFINITY;
+    for (int s = 0; s < wk.splits; ++s) top = fmaxf(top, ml[s * ROWS + tid].x);
+    const float ref = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+    for (int s = 0; s < wk.splits; ++s) {
+      const float2 v = ml[s * ROWS + tid];
+      const float e = __builtin_amdgcn_exp2f(v.x - ref);
+      s_w[s * ROWS + tid] = e;
+      sum = fmaf(e, v.y, sum);
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    for (int s = 0; s < wk.splits; ++s) s_w[s * ROWS + tid] *= inv;
+    if (blockIdx.x == 0 && tid < rows) {
+      if (a.lse) a.lse[orow + tid] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+      if (sm.stat) sm.stat[orow + tid] = {ref, inv};
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < JQ; ++j) {
+    const int quad = blockIdx.x * JQ + j;
+    const int row = RG == 1 ? lane & 15 : 32 * (quad / 16) + (lane & 31);
+    const int dv = RG == 1 ? 128 * w + 16 * quad + 4 * (lane >> 4)
+                           : 128 * w + 32 * (quad / 4 % 4) + 8 * (quad % 4) + 4 * (lane >> 5);
+    const float4* po = wk.part_o + part * NQ * 256 + quad * 256 + tid;
+    float4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < wk.splits; ++s) {
+      const float e = s_w[s * ROWS + row];
+      if (e == 0.f) continue;  // an empty split wrote no output
+      const float4 v = po[(int64_t)s * NQ * 256];
+      sum.x = fmaf(e, v.x, sum.x);
+      sum.y = fmaf(e, v.y, sum.y);
+      sum.z = fmaf(e, v.z, sum.z);
+      sum.w = fmaf(e, v.w, sum.w);
+    }
+    if (row < rows) {
+      const v4bf v = {(__bf16)sum.x, (__bf16)sum.y, (__bf16)sum.z, (__bf16)sum.w};
+      *reinterpret_cast<v4bf*>(a.out + (orow + row) * kLatent + dv) = v;
+    }
   }
 }
 
@@ -188,33 +758,81 @@ __global__ __launch_bounds__(256) void slot_add_kernel(AttendArgs a, RunTable t,
 size_t round256(size_t x) { return (x + 255) / 256 * 256; }
 
 struct Plan {
-  size_t scores, stats, slots;
+  size_t scores, stats, slots, part_o, part_ml;
   int padded;
   int64_t base[kMaxSeq];
   int rows, max_n;
-  size_t bytes() const { return round256(scores) + round256(stats) + round256(slots); }
+  int rg;       // row groups of 16 per workgroup
+  Work wk;
+  size_t bytes() const {
+    return round256(scores) + round256(stats) + round256(slots) + round256(part_o) + round256(part_ml);
+  }
 };
+
+constexpr int kTargetWgs = 256;  // one per CU
+constexpr int kMaxSplits = 128;
 
 Plan plan_of(const AttendArgs& a, const RunTable& t) {
   Plan p{};
-  int64_t words = 0;
+  int64_t words = 0, unit_tiles = 0;
+  int max_rows = 0;
+  p.padded = (a.topk + kTileKeys - 1) / kTileKeys * kTileKeys;
   for (int b = 0; b < t.n; ++b) {
     const int n = t.pos0[b] + t.n_rows[b];
     p.base[b] = words;
     if (t.n_rows[b]) {
       words += (int64_t)((n + kTileKeys - 1) / kTileKeys) * kTileKeys * t.n_rows[b] * a.heads;
       if (n > p.max_n) p.max_n = n;
+      if (t.n_rows[b] > max_rows) max_rows = t.n_rows[b];
     }
     p.rows += t.n_rows[b];
   }
-  p.padded = (a.topk + kTileKeys - 1) / kTileKeys * kTileKeys;
+  if (p.rows == 0) return p;
   if (a.idx) words = (int64_t)p.rows * p.padded * a.heads;
   if (a.acc) {
     p.scores = (size_t)words * 4;
     p.stats = (size_t)p.rows * a.heads * sizeof(float2);
     p.slots = a.idx ? (size_t)p.rows * p.padded * 4 : 0;
   }
+  const int64_t unit_rows = a.idx ? a.heads : (int64_t)max_rows * a.heads;
+  p.rg = unit_rows > 32 ? 4 : unit_rows > 16 ? 2 : 1;
+  const int R = 16 * p.rg;
+  p.wk.units = a.idx ? p.rows : t.n;
+  p.wk.row_tiles = (int)((unit_rows + R - 1) / R);
+  const int max_tiles = a.idx ? p.padded / kTileKeys : (p.max_n + kTileKeys - 1) / kTileKeys;
+  // tiles of all row tiles: what the workgroups share out evenly
+  if (a.idx) {
+    unit_tiles = (int64_t)p.rows * p.wk.row_tiles * max_tiles;
+  } else {
+    for (int b = 0; b < t.n; ++b)
+      unit_tiles += ((int64_t)t.n_rows[b] * a.heads + R - 1) / R * ((t.pos0[b] + t.n_rows[b] + kTileKeys - 1) / kTileKeys);
+  }
+  int64_t each = (unit_tiles + kTargetWgs - 1) / kTargetWgs;
+  if (each < 2) each = 2;
+  if ((max_tiles + each - 1) / each > kMaxSplits) each = (max_tiles + kMaxSplits - 1) / kMaxSplits;
+  p.wk.splits = (int)((max_tiles + each - 1) / each);
+  if (p.wk.splits < 1) p.wk.splits = 1;
+  p.wk.tiles_per_split = (int)each;
+  if (p.wk.splits > 1) {
+    const int64_t parts = (int64_t)p.wk.units * p.wk.row_tiles * p.wk.splits;
+    p.part_o = (size_t)parts * R * kLatent * 4;
+    p.part_ml = (size_t)parts * R * sizeof(float2);
+  } else {
+    p.wk.tiles_per_split = max_tiles > 0 ? max_tiles : 1;
+  }
   return p;
+}
+
+template <int RG>
+hipError_t launch_rows(const AttendArgs& a, const RunTable& t, const ScoreMap& sm, const Work& wk, hipStream_t stream) {
+  const unsigned grid = (unsigned)(wk.units * wk.splits * wk.row_tiles);
+  hipLaunchKernelGGL(attend_kernel<RG>, dim3(grid), dim3(256), 0, stream, a, t, sm, wk);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || wk.splits == 1) return e;
+  constexpr int NQ = RG == 1 ? 8 : 8 * RG;
+  hipLaunchKernelGGL(join_kernel<RG>, dim3(NQ / kJoinQuads<RG>, (unsigned)(wk.units * wk.row_tiles)), dim3(256),
+                     (size_t)wk.splits * 16 * RG * 4, stream, a, t, sm, wk);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -222,19 +840,22 @@ Plan plan_of(const AttendArgs& a, const RunTable& t) {
 size_t attend_workspace(const AttendArgs& a, const RunTable& t) { return plan_of(a, t).bytes(); }
 
 hipError_t launch_attend(const AttendArgs& a, const RunTable& t, hipStream_t stream) {
-  const Plan p = plan_of(a, t);
+  Plan p = plan_of(a, t);
   if (p.rows == 0) return hipSuccess;
   ScoreMap sm{};
-  float* slots = nullptr;
+  uint8_t* ws = (uint8_t*)a.workspace;
   if (a.acc) {
-    uint8_t* ws = (uint8_t*)a.workspace;
     sm.s2 = (float*)ws;
     sm.stat = (float2*)(ws + round256(p.scores));
-    slots = (float*)(ws + round256(p.scores) + round256(p.stats));
     for (int b = 0; b < t.n; ++b) sm.base[b] = p.base[b];
   }
-  hipLaunchKernelGGL(attend_kernel, dim3((unsigned)a.heads, (unsigned)p.rows), dim3(256), 0, stream, a, t, sm);
-  hipError_t e = hipGetLastError();
+  float* slots = (float*)(ws + round256(p.scores) + round256(p.stats));
+  uint8_t* parts = ws + round256(p.scores) + round256(p.stats) + round256(p.slots);
+  p.wk.part_o = (float4*)parts;
+  p.wk.part_ml = (float2*)(parts + round256(p.part_o));
+  hipError_t e = p.rg == 4   ? launch_rows<4>(a, t, sm, p.wk, stream)
+                 : p.rg == 2 ? launch_rows<2>(a, t, sm, p.wk, stream)
+                             : launch_rows<1>(a, t, sm, p.wk, stream);
   if (e != hipSuccess || !a.acc || (a.idx && a.topk == 0)) return e;
   if (!a.idx) {
     const unsigned tiles = (unsigned)((p.max_n + kTileKeys - 1) / kTileKeys);
