@@ -53,17 +53,6 @@ __device__ __forceinline__ void load_lds4(const void* src, uint32_t dst) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(dst), "v"(src) : "memory");
 }
 
-// x *= f for a value in the accumulation registers.  Written out: as plain code
-// the compiler moves the whole output into vector registers ahead of the test
-// whether it is to be scaled, in every tile.  The callers leave the waits between
-// these and the matrix products around them.
-__device__ __forceinline__ void scale_acc(float& x, float f) {
-  float v;
-  asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(x));
-  v *= f;
-  asm volatile("v_accvgpr_write_b32 %0, %1" : "=a"(x) : "v"(v));
-}
-
 // f(0), f(1), ..., f(N - 1) with the index a constant
 template <class F, int... I>
 __device__ __forceinline__ void unroll(F&& f, std::integer_sequence<int, I...>) {
@@ -95,30 +84,21 @@ __device__ __forceinline__ float groups_sum(float x) {
   return __uint_as_float(e[0]) + __uint_as_float(e[1]);
 }
 
-// Sixteen query rows as the second operand of the 16x16x32 score products: lane
-// (row r, group g) has values 32 k + 8 g .. + 7 of product k.
-struct QueryFrag {
-  v4i v[kAttnDim / 32];
-
-  __device__ __forceinline__ void load(const uint16_t* row, int lane) {
-#pragma unroll
-    for (int k = 0; k < kAttnDim / 32; ++k) v[k] = *reinterpret_cast<const v4i*>(row + 32 * k + 8 * (lane >> 4));
-  }
-};
-
-// LDS.  As loaded, a wave's 1024 bytes (4 keys' codes, 8 keys' position values)
-// are a group, the groups 1088 bytes apart; the 16-byte chunks of a row change
-// places by two bits of the key.  Together the two put one chunk of 16 keys,
-// which a score operand reads at once, into 16 different bank groups.
+// LDS.  As loaded, 1024 bytes of one wave's load (4 keys' codes, 8 keys' position
+// values) are a group, the groups 1088 bytes apart; the 16-byte chunks of a row
+// change places by two bits of the key.  Together the two put one chunk of 16
+// keys, which a score operand reads at once, into 16 different bank groups.
 constexpr int kGroup = 1024 + 64;
 constexpr int kCodesBytes = kTileKeys / 4 * kGroup, kRopeBytes = kTileKeys / 8 * kGroup;
+constexpr int kScalesBytes = kTileKeys / 8 * 256;  // 8 keys' scales twice, as 64 lanes load them
 // The widened latent values are rows of 64 chunks of 8 values, chunk c of key k
-// at c ^ swizzle(k): conflict free for a chunk of 16 consecutive keys (scores)
-// as for 4 neighbouring chunks of keys 4 n .. 4 n + 3 (the transposed reads).
+// at c ^ swizzle(k): 4 neighbouring chunks of keys 4 n .. 4 n + 3, which a
+// transposed read takes, lie in different banks.
 constexpr int kValueBytes = kTileKeys * 2 * kLatent;
 __device__ __forceinline__ int swizzle(int key) { return (key & 3) << 2 | (key >> 2 & 3); }
 // Weights: rows of 32 high parts, then 32 low parts.
 constexpr int kWeightStride = 4 * kTileKeys + 16;
+constexpr int kWaves = 8;
 
 // What one launch's workgroups are: units (query rows of an index-set call,
 // else sequences) x splits of the unit's keys x tiles of 16 RG rows.
@@ -128,46 +108,54 @@ struct Work {
   float2* part_ml;  // reference, sum
 };
 
-// A workgroup attends 16 RG rows (heads of one query; in a prefix call heads of
-// consecutive queries of a sequence) to one split of their keys, 32 at a time.
-// Four stages, each on a tile of its own between two barriers:
-//   load    the tile's rows into LDS;
-//   widen   codes to bf16 in LDS (8 keys a wave), exact;
-//   score   transposed, keys x rows: a lane has 4 keys of a row, so maxima and
-//           sums need two lane swaps.  The reference m only moves when a score
-//           passes it by more than 32 (the weights, their sums and the output have
-//           fp32's range, so none comes near its end), and the output is hardly
-//           ever rescaled.  A weight goes to LDS as two bf16, 16 bits
-//           of it: one bf16 would round it by up to 2^-8, as much as the output's
-//           own rounding, and fp16 would lose the small ones;
-//   output  transposed, values x rows: a wave has 128 of the 512 values for all
-//           rows, and the values are read transposed once per tile.
-// Score waves have 32 rows x 16 keys (RG = 4), or 16 x 16 (2, and 1 with two of
-// the four waves).
-//
-// One wave per SIMD holds its query (144 registers for 32 rows) and output (128),
-// so nothing but its own instructions hides a latency.  Operands are therefore
-// read from LDS some steps ahead, and the vector work of the other stages is
-// cut into pieces that are issued between the matrix products, which run on
-// their own once issued.  Scheduling barriers keep the compiler from sorting
-// the two apart again.
+// A workgroup of 8 waves attends 16 RG rows (heads of one query; in a prefix call
+// heads of consecutive queries of a sequence) to one split of their keys, 32 at
+// a time, in four stages:
+//   load    the tile's rows into LDS, a tile ahead;
+//   score   transposed, keys x rows, the codes widened to bf16 in registers
+//           (exact: a code has two significant bits); a lane has 4 keys of a row,
+//           so maxima and sums need two lane swaps.  The reference m of a row only
+//           moves when a score passes it by more than 32 (weights, sums and output
+//           have fp32's range, so none comes near its end), and the output is
+//           hardly ever rescaled.  A weight goes to LDS as two bf16, 16 bits of
+//           it: one bf16 would round it by up to 2^-8, as much as the output's own
+//           rounding, and fp16 would lose the small ones;
+//   widen   codes to bf16 in LDS, 4 keys a wave;
+//   output  transposed, values x rows: a wave has 64 of the 512 values for all
+//           rows, and the values are read transposed from LDS once per tile.
+// RG = 8: a wave scores its 16 rows against all 32 keys; the stages of an
+// iteration (output of tile i; score and widen of i + 1; load of i + 2) need
+// nothing of each other, so one barrier per tile is enough, and the two waves of
+// a SIMD take them in different orders: one widens codes for its scores while the
+// other's output keeps the matrix core busy.  RG <= 4: a wave scores 16 rows
+// against 16 keys, and the waves that share rows exchange their maxima at a second
+// barrier, before which the values of tile i are widened (one buffer does) and
+// after which they are used.
+// Operands are read from LDS some steps ahead, and the vector work of other
+// stages is cut into pieces issued between the output's matrix products, which
+// run on their own once issued; scheduling barriers keep the two from being
+// sorted apart.
 template <int RG>
-__global__ __launch_bounds__(256, 1) void attend_kernel(AttendArgs a, RunTable t, ScoreMap sm, Work wk) {
+__global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, RunTable t, ScoreMap sm,
+                                                                              Work wk) {
+  constexpr bool ONE = RG == 8;                // one barrier per tile
   constexpr int ROWS = 16 * RG;
   constexpr int KT = kTileKeys;
-  constexpr int NRT = RG == 4 ? 2 : 1;         // row tiles of 16 per wave
+  constexpr int NKT = ONE ? 2 : 1;             // key tiles of 16 per wave
+  constexpr int KG = ONE ? 1 : 2;              // waves that share a row group's keys
+  constexpr int SCORERS = RG * KG;             // waves that score
   constexpr int CT = RG == 1 ? 1 : RG / 2;     // output column tiles (of 32 rows, or of 16)
-  constexpr int NQ = RG == 1 ? 8 : 16 * CT;    // output registers per lane / 4
+  constexpr int NQ = RG == 1 ? 4 : 8 * CT;     // output registers per lane / 4
+  constexpr int NS = ONE ? 2 : 3;              // tiles' codes held
+  constexpr int NV = ONE ? 2 : 1;              // tiles' values held
   constexpr int WB = ROWS * kWeightStride;
-  __shared__ __attribute__((aligned(16))) uint8_t s_val[3 * kValueBytes];
-  __shared__ __attribute__((aligned(16))) uint8_t s_codes[2 * kCodesBytes];
-  __shared__ __attribute__((aligned(16))) uint8_t s_scale[2 * 4 * 256];  // 8 keys a wave, twice
-  __shared__ __attribute__((aligned(16))) uint8_t s_rope[3 * kRopeBytes];
-  __shared__ __attribute__((aligned(16))) int s_pos[3 * KT];
+  __shared__ __attribute__((aligned(16))) uint8_t s_val[NV * kValueBytes + (NV == 1 ? 512 : 0)];
+  __shared__ __attribute__((aligned(16))) uint8_t s_codes[NS * kCodesBytes];
+  __shared__ __attribute__((aligned(16))) uint8_t s_rope[NS * kRopeBytes];
+  __shared__ __attribute__((aligned(16))) uint8_t s_scale[NS * kScalesBytes];
+  __shared__ __attribute__((aligned(16))) int s_pos[NS * KT];
   __shared__ __attribute__((aligned(16))) uint8_t s_w[2 * WB];
-  __shared__ __attribute__((aligned(16))) float s_nan[2 * KT];              // NaN for a key with a NaN block, else 0
-  __shared__ __attribute__((aligned(16))) float s_scalef[KT * kScaleBytes];  // the scales as conversion operands
-  __shared__ float s_alpha[2][ROWS], s_max[2][ROWS], s_sum[2][ROWS];
+  __shared__ float s_alpha[2][ROWS], s_max[KG][ROWS], s_sum[KG][ROWS];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -194,22 +182,25 @@ __global__ __launch_bounds__(256, 1) void attend_kernel(AttendArgs a, RunTable t
     return;
   }
 
-  const int kt = RG == 1 ? w : w >> 1;             // the wave's 16 keys of a tile,
-  const int row0 = RG == 1 ? 0 : 16 * NRT * (w & 1);  // and its first row of scores
-  const bool scoring = RG != 1 || w < 2;
+  const int kt = ONE ? 0 : w / RG;             // the wave's (first) 16 keys of a tile,
+  const int row0 = ONE ? 16 * w : 16 * (w % RG);  // and its rows of scores
+  const bool scoring = SCORERS == kWaves || w < SCORERS;
 
-  // Keys 8 w + (lane & 7) of a tile, found in three steps a tile apart, so that
-  // no step waits for its load: the set's entry; the page of its position; the
-  // cache row.
+  // Keys 8 (w mod 4) + (lane & 7) of a tile, found in three steps a tile apart,
+  // so that no step waits for its load: the set's entry; the page of its
+  // position; the cache row.  Waves 0 .. 3 load position values and scales of
+  // these keys, waves 4 .. 7 their codes.
   const int32_t* idx = sets ? a.idx + (int64_t)unit * a.topk : nullptr;
   const int32_t* pages = a.map.pages ? a.map.pages + (int64_t)b * a.map.max_pages : nullptr;
+  const int w4 = w & 3;
+  const bool code_wave = w >= 4;
   auto fetch = [&](int ln, int tile) {
-    const int k = min(tile * KT + 8 * w + (ln & 7), n - 1);
+    const int k = min(tile * KT + 8 * w4 + (ln & 7), n - 1);
     return sets ? idx[k] : k;
   };
   // pos: the position whose row is loaded (0 for keys that do not count), at: the one that masks the key
   auto place = [&](int ln, int tile, int entry, int& pos, int& at) {
-    const bool ok = ((uint32_t)entry <= (uint32_t)pos_last) & (tile < t1) & (tile * KT + 8 * w + (ln & 7) < n);
+    const bool ok = ((uint32_t)entry <= (uint32_t)pos_last) & (tile < t1) & (tile * KT + 8 * w4 + (ln & 7) < n);
     pos = ok ? entry : 0;
     at = ok ? entry : 0x7FFFFFFF;
     return pages ? pages[pos >> a.map.shift] : 0;
@@ -220,406 +211,408 @@ __global__ __launch_bounds__(256, 1) void attend_kernel(AttendArgs a, RunTable t
   };
   const uint32_t codes0 = (uint32_t)(uintptr_t)LDS(uint8_t, s_codes), rope0 = (uint32_t)(uintptr_t)LDS(uint8_t, s_rope),
                  scale0 = (uint32_t)(uintptr_t)LDS(uint8_t, s_scale);
+  int at = 0, pos = 0, page = 0, entry = 0;  // of the next tile to be loaded; the entry of the one after
+  int row = 0;
+  auto load_piece = [&](int ln, int tile, int slot, auto piece) {
+    constexpr int P = piece;
+    if constexpr (P == 0) {
+      row = locate(pos, page);
+    } else if constexpr (P == 1) {  // 8 keys' position values, or 4 keys' codes
+      const int key = ln >> (code_wave ? 4 : 3);
+      const int64_t r = __shfl(row, key, 64);
+      const uint8_t* base = code_wave ? a.cache.codes : reinterpret_cast<const uint8_t*>(a.cache.rope);
+      const int chunk = code_wave ? (ln & 15) ^ key : (ln & 7) ^ (key >> 1);
+      load_lds16(base + (r << (code_wave ? 8 : 7)) + (chunk << 4),
+                 code_wave ? codes0 + slot * kCodesBytes + 2 * w4 * kGroup : rope0 + slot * kRopeBytes + w4 * kGroup);
+    } else if constexpr (P == 2) {
+      if (code_wave) {
+        const int key = ln >> 4;
+        const int64_t r = __shfl(row, 4 + key, 64);
+        load_lds16(a.cache.codes + r * kCodeBytes + (((ln & 15) ^ key) << 4),
+                   codes0 + slot * kCodesBytes + (2 * w4 + 1) * kGroup);
+      } else {
+        const int64_t r = __shfl(row, ln >> 2 & 7, 64);
+        load_lds4(a.cache.scales + r * kScaleBytes + 4 * (ln & 3), scale0 + slot * kScalesBytes + w4 * 256);
+        s_pos[slot * KT + 8 * w4 + (ln & 7)] = at;
+      }
+    } else if constexpr (P == 3) {
+      page = place(ln, tile + 1, entry, pos, at);
+    } else {
+      entry = fetch(ln, tile + 2);
+    }
+  };
+  constexpr int LOADS = 5;
+
   const float c = a.scale * kLog2e;
-  QueryFrag q[NRT];
-  int limit[NRT];  // the last position a row attends to; rows past the last one take its query, masked
-#pragma unroll
-  for (int r = 0; r < NRT; ++r) {
-    const int mine = row0 + 16 * r + (lane & 15), flat = first + min(mine, rows - 1);
+  // The wave's query rows as the second operand of the score products: lane (row
+  // r, group g) has values 8 u .. + 7 of block 4 g + t in product 4 t + u, then
+  // 8 g .. + 7 of each 32 position values.
+  v4i q[kAttnDim / 32];
+  // the last position the lane's row attends to; rows past the last one take its query, masked
+  int limit;
+  {
+    const int mine = row0 + (lane & 15), flat = first + min(mine, rows - 1), g = lane >> 4;
     const int i = sets ? 0 : flat / a.heads, head = flat - i * a.heads;
-    limit[r] = mine < rows ? t.pos0[b] + i_first + i : -1;
-    if (scoring) q[r].load(a.q + ((int64_t)t.row0[b] + i_first + i) * a.q_row + (int64_t)head * a.q_head, lane);
+    limit = mine < rows ? t.pos0[b] + i_first + i : -1;
+    const uint16_t* from = a.q + ((int64_t)t.row0[b] + i_first + i) * a.q_row + (int64_t)head * a.q_head;
+    if (scoring) {
+#pragma unroll
+      for (int k = 0; k < kLatent / 32; ++k)
+        q[k] = *reinterpret_cast<const v4i*>(from + 32 * (4 * g + k / 4) + 8 * (k % 4));
+#pragma unroll
+      for (int k = 0; k < kRope / 32; ++k)
+        q[kLatent / 32 + k] = *reinterpret_cast<const v4i*>(from + kLatent + 32 * k + 8 * g);
+    }
   }
-  float m[NRT], l[NRT];
+  float m = -INFINITY, l = 0.f;
+  v16f o[2][CT];
+  v4f o1[4];
 #pragma unroll
-  for (int r = 0; r < NRT; ++r) m[r] = -INFINITY, l[r] = 0.f;
-  v16f o[4][CT];
-  v4f o1[8];
-#pragma unroll
-  for (int x = 0; x < 4; ++x)
+  for (int x = 0; x < 2; ++x)
 #pragma unroll
     for (int y = 0; y < CT; ++y)
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[x][y][i] = 0.f;
 #pragma unroll
-  for (int x = 0; x < 8; ++x) o1[x] = v4f{0.f, 0.f, 0.f, 0.f};
+  for (int x = 0; x < 4; ++x) o1[x] = v4f{0.f, 0.f, 0.f, 0.f};
   float* s2 = nullptr;  // the workgroup's rows in the unit's first tile of kept scores
   if (sm.s2) {
     const int64_t padded = (a.topk + KT - 1) / KT * KT;
     s2 = sm.s2 + (sets ? (int64_t)unit * unit_rows * padded : sm.base[b]) + (int64_t)first * KT;
   }
 
-  // ---- the stages, in pieces; slot2 / slot3: a tile's place of two / of three
-  int at = 0, pos = 0, page = 0, entry = 0;  // of the next tile to be loaded; the entry of the one after
-  int row = 0;
-  auto load_piece = [&](int ln, int tile, int slot2, int slot3, auto piece) {
-    constexpr int P = piece;
-    if constexpr (P == 0) {
-      row = locate(pos, page);
-    } else if constexpr (P == 1 || P == 2) {
-      const int key = ln >> 4;  // of 4
-      const int64_t r = __shfl(row, 4 * (P - 1) + key, 64);
-      load_lds16(a.cache.codes + r * kCodeBytes + (((ln & 15) ^ key) << 4),
-                 codes0 + slot2 * kCodesBytes + (2 * w + P - 1) * kGroup);
-    } else if constexpr (P == 3) {
-      const int key = ln >> 3;  // of 8
-      const int64_t r = __shfl(row, key, 64);
-      load_lds16(reinterpret_cast<const uint8_t*>(a.cache.rope) + r * (2 * kRope) + (((ln & 7) ^ (key >> 1)) << 4),
-                 rope0 + slot3 * kRopeBytes + w * kGroup);
-    } else if constexpr (P == 4) {
-      const int64_t r = __shfl(row, ln >> 2 & 7, 64);
-      load_lds4(a.cache.scales + r * kScaleBytes + 4 * (ln & 3), scale0 + (4 * slot2 + w) * 256);
-      s_pos[slot3 * KT + 8 * w + (ln & 7)] = at;
-    } else if constexpr (P == 5) {
-      page = place(ln, tile + 1, entry, pos, at);
-    } else {
-      entry = fetch(ln, tile + 2);
-    }
-  };
-  constexpr int LOADS = 7;
-
-  // lane l: the scales of four blocks (l / 8 modulo 4) of the wave's key l & 7
-  uint32_t scale4 = 0;
-  auto scale_piece = [&](int ln, int slot2, auto piece) {
-    constexpr int P = piece;
-    const int key = ln & 7, part4 = ln >> 3 & 3;
-    if constexpr (P == 0) {
-      scale4 = *reinterpret_cast<const uint32_t*>(s_scale + (4 * slot2 + w) * 256 + key * kScaleBytes + part4 * 4);
-    } else if constexpr (P == 1) {
-      uint4 f;
-      uint32_t* p = &f.x;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        // a NaN block makes the key's scores NaN through s_nan; as a value it must
-        // not reach the rows that do not attend to the key (0 * NaN)
-        const int byte = scale4 >> (8 * i) & 255u;
-        p[i] = (uint32_t)(byte & ((byte - 255) >> 31)) << 23;
-      }
-      *reinterpret_cast<uint4*>(&s_scalef[(8 * w + key) * kScaleBytes + part4 * 4]) = f;
-    } else {
-      const uint32_t n = ~scale4;  // a zero byte of it is a byte of 255
-      const uint64_t any = __builtin_amdgcn_ballot_w64(((n - 0x01010101u) & ~n & 0x80808080u) != 0);
-      const uint32_t of = (uint32_t)any;  // lanes 0 .. 31 have every block
-      const uint32_t keys = of | of >> 8 | of >> 16 | of >> 24;
-      s_nan[slot2 * KT + 8 * w + key] = keys >> key & 1 ? __builtin_nanf("") : 0.f;
-    }
-  };
-  constexpr int SCALES = 3;
-
-  // one key at a time, 8 values a lane
+  // ---- the other stages
+  // one of the wave's 4 keys, 8 values a lane: read, then widened
   uint32_t word[2];
-  float wscale[2];
-  auto widen_piece = [&](int ln, int slot2, int slot3, auto piece) {
+  int byte[2];
+  auto widen_piece = [&](int ln, int slot, int vslot, auto piece) {
     constexpr int j = piece / 2;
     if constexpr (piece % 2 == 0) {
-      word[j & 1] = *reinterpret_cast<const uint32_t*>(s_codes + slot2 * kCodesBytes + 2 * w * kGroup +
-                                                       ((4 * ln) ^ ((j & 3) << 4)) + j / 4 * kGroup + (j & 3) * kCodeBytes);
-      wscale[j & 1] = s_scalef[8 * w * kScaleBytes + (ln >> 2) + j * kScaleBytes];
+      word[j & 1] = *reinterpret_cast<const uint32_t*>(s_codes + slot * kCodesBytes + w * kGroup + ((4 * ln) ^ (j << 4)) +
+                                                       j * kCodeBytes);
+      byte[j & 1] = s_scale[slot * kScalesBytes + (w >> 1) * 256 + (4 * (w & 1) + j) * kScaleBytes + (ln >> 2)];
     } else {
-      *reinterpret_cast<uint4*>(s_val + slot3 * kValueBytes + (8 * w + j) * 2 * kLatent +
-                                (16 * ln ^ (swizzle(8 * w + j) << 4))) = decode8(word[j & 1], wscale[j & 1]);
+      // a NaN block makes the key's scores NaN; as a value it must not reach the
+      // rows that do not attend to the key (0 * NaN)
+      const int e = byte[j & 1] & ((byte[j & 1] - 255) >> 31);
+      *reinterpret_cast<uint4*>(s_val + vslot * kValueBytes + (4 * w + j) * 2 * kLatent +
+                                (16 * ln ^ (swizzle(4 * w + j) << 4))) = decode8(word[j & 1], scale_operand(e));
     }
   };
-  constexpr int WIDENS = 16;
+  constexpr int WIDENS = 8;
 
-  // scores of the wave's rows and keys, operands read DEPTH products ahead
-  v4f s[NRT];
-  auto score = [&](int ln, int slot3, auto after) {
-    constexpr int STEPS = kAttnDim / 32, DEPTH = 5;
+  // scores of the wave's rows and keys, operands read ahead
+  v4f s[NKT];
+  auto score = [&](int ln, int slot) {
+    constexpr int STEPS = 4 * NKT, DEPTH = 2;  // a step: 128 values of 16 keys
     const int key = ln & 15, g = ln >> 4;
-    const uint8_t* val = s_val + slot3 * kValueBytes + (16 * kt + key) * 2 * kLatent;
-    const uint32_t at0 = (uint32_t)((g ^ swizzle(key)) << 4);
-    const uint8_t* rope = s_rope + slot3 * kRopeBytes + (key >> 3) * kGroup + (key & 7) * 2 * kRope +
+    const uint8_t* codes = s_codes + slot * kCodesBytes + 4 * kt * kGroup;
+    const uint32_t at0 = (uint32_t)((key >> 2) * kGroup + (key & 3) * kCodeBytes + 64 * g + ((key & 3) << 4));
+    const uint8_t* rope = s_rope + slot * kRopeBytes + (key >> 3) * kGroup + (key & 7) * 2 * kRope +
                           ((g ^ ((key >> 1) & 3)) << 4) + 2 * kt * kGroup;
+    const uint8_t* scale = s_scale + slot * kScalesBytes + (key >> 3) * 256 + (key & 7) * kScaleBytes + 4 * g + 2 * kt * 256;
     v4i x[STEPS];
-    auto read = [&](auto k) {
-      x[k] = *reinterpret_cast<const v4i*>(k < kLatent / 32 ? val + (at0 ^ ((k & 3) << 6)) + (k >> 2) * 256
-                                                            : rope + 64 * (k - kLatent / 32));
+    uint32_t sk[NKT];
+    v4i xr[NKT][2];
+    auto read = [&](auto i) {
+      constexpr int j = i / 4, tt = i % 4;
+      if constexpr (tt == 0) sk[j] = *reinterpret_cast<const uint32_t*>(scale + 2 * j * 256);
+      x[i] = *reinterpret_cast<const v4i*>(codes + (at0 ^ (tt << 4)) + 4 * j * kGroup);
     };
     unroll<DEPTH>(read);
 #pragma unroll
-    for (int r = 0; r < NRT; ++r) s[r] = v4f{0.f, 0.f, 0.f, 0.f};
-    unroll<STEPS>([&](auto k) {
-      if constexpr (k + DEPTH < STEPS) read(std::integral_constant<int, k + DEPTH>{});
+    for (int j = 0; j < NKT; ++j) s[j] = v4f{0.f, 0.f, 0.f, 0.f};
+    unroll<STEPS>([&](auto i) {
+      constexpr int j = i / 4, tt = i % 4;
+      if constexpr (i + DEPTH < STEPS) read(std::integral_constant<int, i + DEPTH>{});
+      if constexpr (tt == 2) {
+        xr[j][0] = *reinterpret_cast<const v4i*>(rope + 2 * j * kGroup);
+        xr[j][1] = *reinterpret_cast<const v4i*>(rope + 2 * j * kGroup + 64);
+      }
+      const float e = scale_operand(sk[j] >> (8 * tt) & 255u);
 #pragma unroll
-      for (int r = 0; r < NRT; ++r)
-        s[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, x[k]), __builtin_bit_cast(v8bf, q[r].v[k]),
-                                                       s[r], 0, 0, 0);
-      after(k, std::integral_constant<int, STEPS>{});
+      for (int u = 0; u < 4; ++u) {
+        const v8bf k8 = __builtin_bit_cast(v8bf, decode8((uint32_t)x[i][u], e));
+        s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, __builtin_bit_cast(v8bf, q[4 * tt + u]), s[j], 0, 0, 0);
+      }
+      if constexpr (tt == 3) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, xr[j][k]),
+                                                         __builtin_bit_cast(v8bf, q[kLatent / 32 + k]), s[j], 0, 0, 0);
+      }
       __builtin_amdgcn_sched_barrier(0);
     });
   };
 
-  // maxima of the wave's scores to s_max; tile: the unit's tile, for the kept scores
-  auto maxima = [&](int ln, int tile, int slot2, int slot3) {
-    const int key = ln & 15, g = ln >> 4, k4 = 16 * kt + 4 * g;
-    const v4i key_at = *reinterpret_cast<const v4i*>(&s_pos[slot3 * KT + k4]);
-    const v4f bad = *reinterpret_cast<const v4f*>(&s_nan[slot2 * KT + k4]);
+  // the scores in base 2, masked, and the row's largest; tile: the unit's tile, for the kept scores
+  float top = 0.f;
+  auto finish_scores = [&](int ln, int tile, int slot) {
+    const int key = ln & 15, g = ln >> 4;
+    top = -INFINITY;
 #pragma unroll
-    for (int r = 0; r < NRT; ++r) {
-      float top = -INFINITY;
+    for (int j = 0; j < NKT; ++j) {
+      const int k4 = 16 * (kt + j) + 4 * g;
+      const v4i key_at = *reinterpret_cast<const v4i*>(&s_pos[slot * KT + k4]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        s[r][i] = key_at[i] <= limit[r] ? fmaf(s[r][i], c, bad[i]) : -INFINITY;
-        top = fmaxf(top, s[r][i]);
+        s[j][i] = key_at[i] <= limit ? s[j][i] * c : -INFINITY;
+        top = fmaxf(top, s[j][i]);
       }
-      if (s2 && tile < t1 && row0 + 16 * r + key < rows)
-        *reinterpret_cast<v4f*>(s2 + (int64_t)tile * unit_rows * KT + ((row0 + 16 * r + key) * KT + k4)) = s[r];
-      top = groups_max(top);
-      s_max[kt][row0 + 16 * r + key] = top;
+      if (s2 && tile < t1 && row0 + key < rows)
+        *reinterpret_cast<v4f*>(s2 + (int64_t)tile * unit_rows * KT + ((row0 + key) * KT + k4)) = s[j];
     }
+    top = groups_max(top);
+    if constexpr (!ONE) s_max[kt][row0 + key] = top;
   };
-  // the scores' weights to s_w[slot2]
-  float ref[NRT], alpha[NRT], e[NRT][4];
-  v4bf hi[NRT];
-  auto weigh_piece = [&](int ln, int slot2, auto piece) {
-    constexpr int r = piece / 5, P = piece % 5;
-    const int key = ln & 15, g = ln >> 4, mine = row0 + 16 * r + key;
-    if constexpr (P == 0) {
-      const float top = fmaxf(s_max[0][mine], s_max[1][mine]);
-      const bool move = top > m[r] + 32.f;
-      const float next = move ? top : m[r];
-      alpha[r] = move ? __builtin_amdgcn_exp2f(m[r] - next) : 1.f;
-      ref[r] = next == -INFINITY ? 0.f : next;
-      m[r] = next;
-    } else if constexpr (P == 1 || P == 2) {
-#pragma unroll
-      for (int i = 2 * P - 2; i < 2 * P; ++i) e[r][i] = __builtin_amdgcn_exp2f(s[r][i] - ref[r]);
-    } else if constexpr (P == 3) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) hi[r][i] = (__bf16)e[r][i];
-      l[r] = fmaf(l[r], alpha[r], (e[r][0] + e[r][1]) + (e[r][2] + e[r][3]));
-      s_alpha[slot2][mine] = alpha[r];
+  // the scores' weights to s_w[wslot]
+  float ref = 0.f, alpha = 1.f, e[NKT][4];
+  v4bf hi[NKT];
+  auto weigh_piece = [&](int ln, int wslot, auto piece) {
+    const int key = ln & 15, g = ln >> 4, mine = row0 + key;
+    if constexpr (piece == 0) {
+      if constexpr (!ONE) top = fmaxf(s_max[0][mine], s_max[1][mine]);
+      const bool move = top > m + 32.f;
+      const float next = move ? top : m;
+      alpha = move ? __builtin_amdgcn_exp2f(m - next) : 1.f;
+      ref = next == -INFINITY ? 0.f : next;
+      m = next;
+      s_alpha[wslot][mine] = alpha;
+      l *= alpha;
     } else {
-      v4bf lo;
+      constexpr int j = (piece - 1) / 3, P = (piece - 1) % 3;
+      if constexpr (P == 0) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) lo[i] = (__bf16)(e[r][i] - (float)hi[r][i]);
-      uint8_t* to = s_w + slot2 * WB + mine * kWeightStride + 32 * kt + 8 * g;
-      *reinterpret_cast<v4bf*>(to) = hi[r];
-      *reinterpret_cast<v4bf*>(to + 2 * KT) = lo;
+        for (int i = 0; i < 4; ++i) e[j][i] = __builtin_amdgcn_exp2f(s[j][i] - ref);
+      } else if constexpr (P == 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) hi[j][i] = (__bf16)e[j][i];
+        l += (e[j][0] + e[j][1]) + (e[j][2] + e[j][3]);
+      } else {
+        v4bf lo;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) lo[i] = (__bf16)(e[j][i] - (float)hi[j][i]);
+        uint8_t* to = s_w + wslot * WB + mine * kWeightStride + 32 * (kt + j) + 8 * g;
+        *reinterpret_cast<v4bf*>(to) = hi[j];
+        *reinterpret_cast<v4bf*>(to + 2 * KT) = lo;
+      }
     }
   };
-  constexpr int WEIGHS = 5 * NRT;
+  constexpr int WEIGHS = 1 + 3 * NKT;
 
-  auto output = [&](int ln, int slot3, int slot2, auto after) {
-    const uint8_t* wgt = s_w + slot2 * WB;
-    const int g = ln >> 4, quad = (ln & 15) >> 2;
-    // RG = 1: keys 8 g + 4 r + quad, chunks 16 w + 2 x + (ln & 3) / 2; else keys
-    // 16 k + 8 h + 4 r + quad, chunks 16 w + 4 x + 2 (g & 1) + (ln & 3) / 2
-    constexpr int VS = RG == 1 ? 8 : 8, AHEAD = 2;  // reads of values; read two ahead
-    const int h = ln >> 5;
-    const uint8_t* base = s_val + slot3 * kValueBytes + (8 * (RG == 1 ? g : h) + quad) * 2 * kLatent + 256 * w + 8 * (ln & 1);
-    const uint32_t at0 = RG == 1 ? (uint32_t)((((ln & 3) >> 1) ^ (4 * quad + (2 * g & 3))) << 4)
-                                 : (uint32_t)((4 * quad + ((2 * (g & 1) + ((ln & 3) >> 1)) ^ (2 * h))) << 4);
-    v4s v0[VS], v1[VS];
-    auto read = [&](auto x) {
-      const uint8_t* from = base + (RG == 1 ? 0 : x / 4 * 16 * 2 * kLatent);
-      const uint32_t d = RG == 1 ? (uint32_t)(x << 5) : (uint32_t)(x % 4 << 6);
-      v0[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, from + (at0 ^ d)));
-      v1[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, from + (at0 ^ d ^ 16) + 4 * 2 * kLatent));
-    };
-    v8bf wt[2][2][CT];  // [k][high, low][row tile]
-    auto read_weights = [&](int k) {
-#pragma unroll
-      for (int y = 0; y < CT; ++y) {
-        const uint8_t* wp = RG == 1 ? wgt + (ln & 15) * kWeightStride + 16 * g
-                                    : wgt + (32 * y + (ln & 31)) * kWeightStride + 32 * k + 16 * h;
-        wt[k][0][y] = __builtin_bit_cast(v8bf, *reinterpret_cast<const v4i*>(wp));
-        wt[k][1][y] = __builtin_bit_cast(v8bf, *reinterpret_cast<const v4i*>(wp + 2 * KT));
-      }
-    };
-    read_weights(0);
-    unroll<AHEAD>(read);
+  auto output = [&](int ln, int vslot, int wslot, auto after) {
+    const uint8_t* wgt = s_w + wslot * WB;
+    const int g = ln >> 4, quad = (ln & 15) >> 2, h = ln >> 5;
     if constexpr (RG == 1) {
-      const float al = s_alpha[slot2][ln & 15];
+      // keys 8 g + 4 r + quad, chunks 8 w + 2 x + (ln & 3) / 2
+      const uint8_t* base = s_val + vslot * kValueBytes + (8 * g + quad) * 2 * kLatent + 256 * (w >> 1) + 8 * (ln & 1);
+      const uint32_t at0 = (uint32_t)(((8 * (w & 1) + ((ln & 3) >> 1)) ^ (4 * quad + (2 * g & 3))) << 4);
+      v4s v0[4], v1[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        v0[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, base + (at0 ^ (x << 5))));
+        v1[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, base + (at0 ^ (x << 5) ^ 16) + 4 * 2 * kLatent));
+      }
+      const uint8_t* wp = wgt + (ln & 15) * kWeightStride + 16 * g;
+      const v8bf wt[2] = {__builtin_bit_cast(v8bf, *reinterpret_cast<const v4i*>(wp)),
+                          __builtin_bit_cast(v8bf, *reinterpret_cast<const v4i*>(wp + 2 * KT))};
+      const float al = s_alpha[wslot][ln & 15];
       if (__any(al != 1.f)) {
 #pragma unroll
-        for (int x = 0; x < 8; ++x)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float v = o1[x][i];
-            scale_acc(v, al);
-            o1[x][i] = v;
-          }
-        asm volatile("s_nop 7\n\ts_nop 7" ::: "memory");
+        for (int x = 0; x < 4; ++x) o1[x] *= al;
       }
-    } else {
-#pragma unroll
-      for (int y = 0; y < CT; ++y) {
-        const float al = s_alpha[slot2][32 * y + (ln & 31)];
-        if (__any(al != 1.f)) {
-#pragma unroll
-          for (int x = 0; x < 4; ++x)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              float v = o[x][y][i];
-              scale_acc(v, al);
-              o[x][y][i] = v;
-            }
-          asm volatile("s_nop 7\n\ts_nop 7" ::: "memory");
-        }
-      }
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    unroll<VS>([&](auto x) {
-      if constexpr (x + AHEAD < VS) read(std::integral_constant<int, x + AHEAD>{});
-      if constexpr (RG != 1 && x == 1) read_weights(1);
-      const v8bf v = __builtin_bit_cast(v8bf, __builtin_shufflevector(v0[x], v1[x], 0, 1, 2, 3, 4, 5, 6, 7));
-      constexpr int k = RG == 1 ? 0 : x / 4;
-      unroll<2 * CT>([&](auto u) {  // high parts of the row tiles, then low ones
-        constexpr int part = u / CT, y = u % CT;
-        if constexpr (RG == 1) {
-          o1[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, wt[0][part][0], o1[x], 0, 0, 0);
-        } else {
-          o[x % 4][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, wt[k][part][y], o[x % 4][y], 0, 0, 0);
-        }
-        after(std::integral_constant<int, x * 2 * CT + u>{}, std::integral_constant<int, VS * 2 * CT>{});
+      unroll<8>([&](auto u) {
+        constexpr int x = u % 4;
+        const v8bf v = __builtin_bit_cast(v8bf, __builtin_shufflevector(v0[x], v1[x], 0, 1, 2, 3, 4, 5, 6, 7));
+        o1[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, wt[u / 4], o1[x], 0, 0, 0);
+        after(u, std::integral_constant<int, 8>{});
         __builtin_amdgcn_sched_barrier(0);
       });
-    });
+    } else {
+      // keys 16 k + 8 h + 4 r + quad, chunks 8 w + 4 x + 2 (g & 1) + (ln & 3) / 2
+      const uint8_t* base = s_val + vslot * kValueBytes + (8 * h + quad) * 2 * kLatent + 256 * (w >> 1) + 8 * (ln & 1);
+      const uint32_t at0 = (uint32_t)(((8 * (w & 1) + 2 * (g & 1) + ((ln & 3) >> 1)) ^ (4 * quad + 2 * h)) << 4);
+      constexpr int STEPS = 2 * CT;  // a step: 16 keys, 32 rows
+      v4s v0[2][2], v1[2][2];
+      auto read_values = [&](auto k) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const uint8_t* from = base + k * 16 * 2 * kLatent;
+          v0[k][x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, from + (at0 ^ (x << 6))));
+          v1[k][x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, from + (at0 ^ (x << 6) ^ 16) + 4 * 2 * kLatent));
+        }
+      };
+      v8bf wt[STEPS][2];
+      auto read_weights = [&](auto i) {
+        constexpr int k = i / CT, y = i % CT;
+        const uint8_t* wp = wgt + (32 * y + (ln & 31)) * kWeightStride + 32 * k + 16 * h;
+        wt[i][0] = __builtin_bit_cast(v8bf, *reinterpret_cast<const v4i*>(wp));
+        wt[i][1] = __builtin_bit_cast(v8bf, *reinterpret_cast<const v4i*>(wp + 2 * KT));
+      };
+      read_values(std::integral_constant<int, 0>{});
+      read_weights(std::integral_constant<int, 0>{});
+#pragma unroll
+      for (int y = 0; y < CT; ++y) {
+        const float al = s_alpha[wslot][32 * y + (ln & 31)];
+        if (__any(al != 1.f)) {
+#pragma unroll
+          for (int x = 0; x < 2; ++x) o[x][y] *= al;
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      unroll<STEPS>([&](auto i) {
+        constexpr int k = i / CT, y = i % CT;
+        if constexpr (i + 1 < STEPS) read_weights(std::integral_constant<int, i + 1>{});
+        if constexpr (i == CT) read_values(std::integral_constant<int, 1>{});
+        unroll<4>([&](auto u) {  // both value tiles with the high parts, then with the low ones
+          constexpr int x = u % 2;
+          const v8bf v = __builtin_bit_cast(v8bf, __builtin_shufflevector(v0[k][x], v1[k][x], 0, 1, 2, 3, 4, 5, 6, 7));
+          o[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, wt[i][u / 2], o[x][y], 0, 0, 0);
+          after(std::integral_constant<int, 4 * i + u>{}, std::integral_constant<int, 4 * STEPS>{});
+          __builtin_amdgcn_sched_barrier(0);
+        });
+      });
+    }
   };
-  auto nothing = [](auto, auto) {};
 
   const int count = t1 - t0;
   if (count > 0) {
-    // tiles 0 .. 2 loaded, 0 and 1 widened, 0 scored
     const int entry0 = fetch(lane, t0);
     entry = fetch(lane, t0 + 1);
     page = place(lane, t0, entry0, pos, at);
-    unroll<LOADS>([&](auto p) { load_piece(lane, t0, 0, 0, p); });
-    unroll<LOADS>([&](auto p) { load_piece(lane, t0 + 1, 1, 1, p); });
+    unroll<LOADS>([&](auto p) { load_piece(lane, t0, 0, p); });
+    if constexpr (!ONE) unroll<LOADS>([&](auto p) { load_piece(lane, t0 + 1, 1, p); });
     // the query is in registers before the loop (its waits would fall inside it)
+    if (scoring) {
 #pragma unroll
-    for (int r = 0; r < NRT; ++r)
-#pragma unroll
-      for (int k = 0; k < kAttnDim / 32; k += 2) asm volatile("s_waitcnt vmcnt(0)" : "+v"(q[r].v[k]), "+v"(q[r].v[k + 1]));
+      for (int k = 0; k < kAttnDim / 32; k += 2) asm volatile("s_waitcnt vmcnt(0)" : "+v"(q[k]), "+v"(q[k + 1]));
+    }
     asm volatile("s_waitcnt vmcnt(0)" : "+v"(entry), "+v"(page)::"memory");
     __syncthreads();
-    auto widen_all = [&](int slot) {
-      unroll<SCALES>([&](auto p) { scale_piece(lane, slot, p); });
-      unroll<WIDENS>([&](auto p) { widen_piece(lane, slot, slot, p); });
-    };
-    widen_all(0);
-    __syncthreads();
-    unroll<LOADS>([&](auto p) { load_piece(lane, t0 + 2, 0, 2, p); });
+    if constexpr (ONE) unroll<LOADS>([&](auto p) { load_piece(lane, t0 + 1, 1, p); });
     if (scoring) {
-      score(lane, 0, nothing);
-      maxima(lane, t0, 0, 0);
+      score(lane, 0);
+      finish_scores(lane, t0, 0);
     }
-    __syncthreads();
+    if constexpr (!ONE) __syncthreads();
     if (scoring) unroll<WEIGHS>([&](auto p) { weigh_piece(lane, 0, p); });
-    widen_all(1);
+    if constexpr (ONE) unroll<WIDENS>([&](auto p) { widen_piece(lane, 0, 0, p); });
   }
-  // Iteration i: tile i + 3 is loaded, i + 2 widened, i + 1 scored, i put out
-  // (past the last tile masked ones, of row 0).
-  int slot3 = 0;
+  // Iteration i: tile i + 2 is loaded, i + 1 scored, i put out (past the last
+  // tile masked ones, of row 0).
+  int slot = 0;  // of tile i's codes
   for (int i = 0; i < count; ++i) {
     int ln = lane;  // addresses are made anew for every tile rather than kept in registers
     asm volatile("" : "+v"(ln));
-    const int next3 = slot3 == 2 ? 0 : slot3 + 1, after3 = next3 == 2 ? 0 : next3 + 1;  // of i + 1, i + 2
     // every load is done, the entry and the page too (named here, so that the
     // compiler waits for them nowhere else)
     asm volatile("s_waitcnt vmcnt(0)" : "+v"(entry), "+v"(page)::"memory");
     __syncthreads();
-    const auto during_score = [&](auto step, auto steps) {
-      pieces_after<steps, LOADS + SCALES, step>([&](auto p) {
-        if constexpr (p < LOADS) load_piece(ln, t0 + i + 3, (i + 1) & 1, slot3, p);
-        else scale_piece(ln, i & 1, std::integral_constant<int, p - LOADS>{});
-      });
-    };
-    if (scoring) {
-      score(ln, next3, during_score);
-      maxima(ln, t0 + i + 1, (i + 1) & 1, next3);
-    } else {
-      unroll<LOADS + SCALES>([&](auto p) { during_score(p, std::integral_constant<int, LOADS + SCALES>{}); });
-    }
-    __syncthreads();
-    if (scoring) {
-      output(ln, slot3, i & 1, [&](auto step, auto steps) {
-        pieces_after<steps, WIDENS + WEIGHS, step>([&](auto p) {
-          // weights first: two pieces of them for three of widening
-          if constexpr (p < WEIGHS) weigh_piece(ln, (i + 1) & 1, p);
-          else widen_piece(ln, i & 1, after3, std::integral_constant<int, p - WEIGHS>{});
+    const int next = slot + 1 == NS ? 0 : slot + 1, after_next = next + 1 == NS ? 0 : next + 1;  // of i + 1, i + 2
+    const auto load = [&](auto p) { load_piece(ln, t0 + i + 2, after_next, p); };
+    if constexpr (ONE) {
+      const auto weigh = [&](auto p) { weigh_piece(ln, (i + 1) & 1, p); };
+      const auto widen = [&](auto p) { widen_piece(ln, next, (i + 1) & 1, p); };
+      score(ln, next);
+      finish_scores(ln, t0 + i + 1, next);
+      output(ln, i & 1, i & 1, [&](auto step, auto steps) {
+        pieces_after<steps, WEIGHS + WIDENS + LOADS, step>([&](auto p) {
+          if constexpr (p < LOADS) load(p);
+          else if constexpr (p < LOADS + WEIGHS) weigh(std::integral_constant<int, p - LOADS>{});
+          else widen(std::integral_constant<int, p - LOADS - WEIGHS>{});
         });
       });
     } else {
-      output(ln, slot3, i & 1, [&](auto step, auto steps) {
-        pieces_after<steps, WIDENS, step>([&](auto p) { widen_piece(ln, i & 1, after3, p); });
-      });
+      unroll<LOADS>(load);
+      unroll<WIDENS>([&](auto p) { widen_piece(ln, slot, 0, p); });
+      if (scoring) {
+        score(ln, next);
+        finish_scores(ln, t0 + i + 1, next);
+      }
+      __syncthreads();
+      if (scoring) {
+        output(ln, 0, i & 1, [&](auto step, auto steps) {
+          pieces_after<steps, WEIGHS, step>([&](auto p) { weigh_piece(ln, (i + 1) & 1, p); });
+        });
+      } else {
+        output(ln, 0, i & 1, [](auto, auto) {});
+      }
     }
-    slot3 = next3;
+    slot = next;
   }
   // no load into LDS may outlive the workgroup
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
   // the rows' statistics
-  const int g = lane >> 4;
   __syncthreads();
+  const int g = lane >> 4;
   if (scoring) {
-#pragma unroll
-    for (int r = 0; r < NRT; ++r) {
-      l[r] = groups_sum(l[r]);
-      if (g == 0) {
-        const int mine = row0 + 16 * r + lane;
-        s_sum[kt][mine] = l[r];
-        s_max[0][mine] = m[r];  // both waves of the rows hold the same
-      }
+    l = groups_sum(l);
+    if (g == 0) {
+      s_sum[ONE ? 0 : kt][row0 + lane] = l;
+      s_max[0][row0 + lane] = m;  // the waves of the rows hold the same
     }
   }
   __syncthreads();
+  auto total_of = [&](int row) {
+    float sum = s_sum[0][row];
+    if constexpr (KG > 1) sum += s_sum[1][row];
+    return sum;
+  };
   if (wk.splits > 1) {
-    if (tid < ROWS) wk.part_ml[part * ROWS + tid] = {s_max[0][tid], s_sum[0][tid] + s_sum[1][tid]};
+    if (tid < ROWS) wk.part_ml[part * ROWS + tid] = {s_max[0][tid], total_of(tid)};
     // the registers as they lie: the joining kernel has the same lanes
-    float4* po = wk.part_o + part * NQ * 256 + tid;
+    float4* po = wk.part_o + part * NQ * (64 * kWaves) + tid;
     if constexpr (RG == 1) {
 #pragma unroll
-      for (int x = 0; x < 8; ++x) po[x * 256] = float4{o1[x][0], o1[x][1], o1[x][2], o1[x][3]};
+      for (int x = 0; x < 4; ++x) po[x * 64 * kWaves] = float4{o1[x][0], o1[x][1], o1[x][2], o1[x][3]};
     } else {
 #pragma unroll
       for (int y = 0; y < CT; ++y)
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            po[((4 * y + x) * 4 + i) * 256] =
+            po[((2 * y + x) * 4 + i) * 64 * kWaves] =
                 float4{o[x][y][4 * i], o[x][y][4 * i + 1], o[x][y][4 * i + 2], o[x][y][4 * i + 3]};
     }
     return;
   }
   const int64_t orow = ((int64_t)t.row0[b] + i_first) * a.heads + first;
   if (tid < rows) {
-    const float sum = s_sum[0][tid] + s_sum[1][tid], top = s_max[0][tid];
+    const float sum = total_of(tid), top = s_max[0][tid];
     if (a.lse) a.lse[orow + tid] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
     if (sm.stat) sm.stat[orow + tid] = {top == -INFINITY ? 0.f : top, sum == 0.f ? 0.f : 1.f / sum};
   }
   // 32 rows (16) at a time through LDS, so that whole rows are written
   constexpr int OS = 2 * kLatent + 16, OR = RG == 1 ? 16 : 32;
+  static_assert(OR * OS <= sizeof(s_val), "the rows fit");
 #pragma unroll
   for (int y = 0; y < CT; ++y) {
     const int row = 32 * y + (RG == 1 ? lane & 15 : lane & 31);
-    const float sum = s_sum[0][row] + s_sum[1][row], inv = sum == 0.f ? 0.f : 1.f / sum;
+    const float sum = total_of(row), inv = sum == 0.f ? 0.f : 1.f / sum;
     uint8_t* to = s_val + (row - 32 * y) * OS;
     if constexpr (RG == 1) {
 #pragma unroll
-      for (int x = 0; x < 8; ++x) {
+      for (int x = 0; x < 4; ++x) {
         v4bf v;
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = (__bf16)(o1[x][i] * inv);
-        *reinterpret_cast<v4bf*>(to + 2 * (128 * w + 16 * x + 4 * g)) = v;
+        *reinterpret_cast<v4bf*>(to + 2 * (64 * w + 16 * x + 4 * g)) = v;
       }
     } else {
 #pragma unroll
-      for (int x = 0; x < 4; ++x)
+      for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           v4bf v;
 #pragma unroll
           for (int i = 0; i < 4; ++i) v[i] = (__bf16)(o[x][y][4 * j + i] * inv);
-          *reinterpret_cast<v4bf*>(to + 2 * (128 * w + 32 * x + 8 * j + 4 * (lane >> 5))) = v;
+          *reinterpret_cast<v4bf*>(to + 2 * (64 * w + 32 * x + 8 * j + 4 * (lane >> 5))) = v;
         }
     }
     __syncthreads();
-    for (int r = w; r < OR && 32 * y + r < rows; r += 4)
+    for (int r = w; r < OR && 32 * y + r < rows; r += kWaves)
       *reinterpret_cast<uint4*>(a.out + (orow + 32 * y + r) * kLatent + 8 * lane) =
           *reinterpret_cast<const uint4*>(s_val + r * OS + 16 * lane);
     if (y + 1 < CT) __syncthreads();
@@ -631,10 +624,10 @@ __global__ __launch_bounds__(256, 1) void attend_kernel(AttendArgs a, RunTable t
 template <int RG>
 constexpr int kJoinQuads = RG == 1 ? 2 : 4;
 template <int RG>
-__global__ __launch_bounds__(256) void join_kernel(AttendArgs a, RunTable t, ScoreMap sm, Work wk) {
+__global__ __launch_bounds__(64 * kWaves) void join_kernel(AttendArgs a, RunTable t, ScoreMap sm, Work wk) {
   constexpr int ROWS = 16 * RG;
   constexpr int CT = RG == 1 ? 1 : RG / 2;
-  constexpr int NQ = RG == 1 ? 8 : 16 * CT;
+  constexpr int NQ = RG == 1 ? 4 : 8 * CT;
   constexpr int JQ = kJoinQuads<RG>;
   extern __shared__ float s_w[];  // [splits][ROWS]
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
@@ -670,15 +663,15 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, RunTable t, Sco
 #pragma unroll
   for (int j = 0; j < JQ; ++j) {
     const int quad = blockIdx.x * JQ + j;
-    const int row = RG == 1 ? lane & 15 : 32 * (quad / 16) + (lane & 31);
-    const int dv = RG == 1 ? 128 * w + 16 * quad + 4 * (lane >> 4)
-                           : 128 * w + 32 * (quad / 4 % 4) + 8 * (quad % 4) + 4 * (lane >> 5);
-    const float4* po = wk.part_o + part * NQ * 256 + quad * 256 + tid;
+    const int row = RG == 1 ? lane & 15 : 32 * (quad / 8) + (lane & 31);
+    const int dv = RG == 1 ? 64 * w + 16 * quad + 4 * (lane >> 4)
+                           : 64 * w + 32 * (quad / 4 % 2) + 8 * (quad % 4) + 4 * (lane >> 5);
+    const float4* po = wk.part_o + (part * NQ + quad) * (64 * kWaves) + tid;
     float4 sum = {0.f, 0.f, 0.f, 0.f};
     for (int s = 0; s < wk.splits; ++s) {
       const float e = s_w[s * ROWS + row];
       if (e == 0.f) continue;  // an empty split wrote no output
-      const float4 v = po[(int64_t)s * NQ * 256];
+      const float4 v = po[(int64_t)s * NQ * (64 * kWaves)];
       sum.x = fmaf(e, v.x, sum.x);
       sum.y = fmaf(e, v.y, sum.y);
       sum.z = fmaf(e, v.z, sum.z);
@@ -795,7 +788,7 @@ Plan plan_of(const AttendArgs& a, const RunTable& t) {
     p.slots = a.idx ? (size_t)p.rows * p.padded * 4 : 0;
   }
   const int64_t unit_rows = a.idx ? a.heads : (int64_t)max_rows * a.heads;
-  p.rg = unit_rows > 32 ? 4 : unit_rows > 16 ? 2 : 1;
+  p.rg = unit_rows > 64 ? 8 : unit_rows > 32 ? 4 : unit_rows > 16 ? 2 : 1;
   const int R = 16 * p.rg;
   p.wk.units = a.idx ? p.rows : t.n;
   p.wk.row_tiles = (int)((unit_rows + R - 1) / R);
@@ -807,8 +800,9 @@ Plan plan_of(const AttendArgs& a, const RunTable& t) {
     for (int b = 0; b < t.n; ++b)
       unit_tiles += ((int64_t)t.n_rows[b] * a.heads + R - 1) / R * ((t.pos0[b] + t.n_rows[b] + kTileKeys - 1) / kTileKeys);
   }
+  const int64_t least = p.rg == 8 ? 8 : p.rg == 4 ? 6 : 4;
   int64_t each = (unit_tiles + kTargetWgs - 1) / kTargetWgs;
-  if (each < 2) each = 2;
+  if (each < least) each = least;
   if ((max_tiles + each - 1) / each > kMaxSplits) each = (max_tiles + kMaxSplits - 1) / kMaxSplits;
   p.wk.splits = (int)((max_tiles + each - 1) / each);
   if (p.wk.splits < 1) p.wk.splits = 1;
@@ -826,11 +820,11 @@ Plan plan_of(const AttendArgs& a, const RunTable& t) {
 template <int RG>
 hipError_t launch_rows(const AttendArgs& a, const RunTable& t, const ScoreMap& sm, const Work& wk, hipStream_t stream) {
   const unsigned grid = (unsigned)(wk.units * wk.splits * wk.row_tiles);
-  hipLaunchKernelGGL(attend_kernel<RG>, dim3(grid), dim3(256), 0, stream, a, t, sm, wk);
+  hipLaunchKernelGGL(attend_kernel<RG>, dim3(grid), dim3(64 * kWaves), 0, stream, a, t, sm, wk);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || wk.splits == 1) return e;
-  constexpr int NQ = RG == 1 ? 8 : 8 * RG;
-  hipLaunchKernelGGL(join_kernel<RG>, dim3(NQ / kJoinQuads<RG>, (unsigned)(wk.units * wk.row_tiles)), dim3(256),
+  constexpr int NQ = RG == 1 ? 4 : 4 * RG;
+  hipLaunchKernelGGL(join_kernel<RG>, dim3(NQ / kJoinQuads<RG>, (unsigned)(wk.units * wk.row_tiles)), dim3(64 * kWaves),
                      (size_t)wk.splits * 16 * RG * 4, stream, a, t, sm, wk);
   return hipGetLastError();
 }
@@ -853,7 +847,8 @@ hipError_t launch_attend(const AttendArgs& a, const RunTable& t, hipStream_t str
   uint8_t* parts = ws + round256(p.scores) + round256(p.stats) + round256(p.slots);
   p.wk.part_o = (float4*)parts;
   p.wk.part_ml = (float2*)(parts + round256(p.part_o));
-  hipError_t e = p.rg == 4   ? launch_rows<4>(a, t, sm, p.wk, stream)
+  hipError_t e = p.rg == 8   ? launch_rows<8>(a, t, sm, p.wk, stream)
+                 : p.rg == 4 ? launch_rows<4>(a, t, sm, p.wk, stream)
                  : p.rg == 2 ? launch_rows<2>(a, t, sm, p.wk, stream)
                              : launch_rows<1>(a, t, sm, p.wk, stream);
   if (e != hipSuccess || !a.acc || (a.idx && a.topk == 0)) return e;
