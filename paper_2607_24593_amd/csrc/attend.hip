@@ -98,6 +98,7 @@ constexpr int kValueBytes = kTileKeys * 2 * kLatent;
 __device__ __forceinline__ int swizzle(int key) { return (key & 3) << 2 | (key >> 2 & 3); }
 // Weights: rows of 32 high parts, then 32 low parts.
 constexpr int kWeightStride = 4 * kTileKeys + 16;
+constexpr int kQueryStride = 2 * kRope + 64 + 16;
 constexpr int kWaves = 8;
 
 // What one launch's workgroups are: units (query rows of an index-set call,
@@ -155,6 +156,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
   __shared__ __attribute__((aligned(16))) uint8_t s_scale[NS * kScalesBytes];
   __shared__ __attribute__((aligned(16))) int s_pos[NS * KT];
   __shared__ __attribute__((aligned(16))) uint8_t s_w[2 * WB];
+  // the part of the queries that finds no register: the position values and the
+  // last 32 latent ones
+  __shared__ __attribute__((aligned(16))) uint8_t s_qr[ONE ? ROWS * kQueryStride : 16];
   __shared__ float s_alpha[2][ROWS], s_max[KG][ROWS], s_sum[KG][ROWS];
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -247,7 +251,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
   // The wave's query rows as the second operand of the score products: lane (row
   // r, group g) has values 8 u .. + 7 of block 4 g + t in product 4 t + u, then
   // 8 g .. + 7 of each 32 position values.
-  v4i q[kAttnDim / 32];
+  constexpr int QK = ONE ? kLatent / 32 - 1 : kAttnDim / 32;  // products whose query part stays in registers
+  v4i q[QK];
   // the last position the lane's row attends to; rows past the last one take its query, masked
   int limit;
   {
@@ -257,11 +262,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
     const uint16_t* from = a.q + ((int64_t)t.row0[b] + i_first + i) * a.q_row + (int64_t)head * a.q_head;
     if (scoring) {
 #pragma unroll
-      for (int k = 0; k < kLatent / 32; ++k)
-        q[k] = *reinterpret_cast<const v4i*>(from + 32 * (4 * g + k / 4) + 8 * (k % 4));
+      for (int k = 0; k < kLatent / 32; ++k) {
+        const v4i v = *reinterpret_cast<const v4i*>(from + 32 * (4 * g + k / 4) + 8 * (k % 4));
+        if (k < QK) q[k] = v;
+        else *reinterpret_cast<v4i*>(s_qr + mine * kQueryStride + 2 * kRope + 16 * g) = v;  // its own wave's
+      }
 #pragma unroll
-      for (int k = 0; k < kRope / 32; ++k)
-        q[kLatent / 32 + k] = *reinterpret_cast<const v4i*>(from + kLatent + 32 * k + 8 * g);
+      for (int k = 0; k < kRope / 32; ++k) {
+        const v4i v = *reinterpret_cast<const v4i*>(from + kLatent + 32 * k + 8 * g);
+        if constexpr (ONE) *reinterpret_cast<v4i*>(s_qr + mine * kQueryStride + 64 * k + 16 * g) = v;
+        else q[kLatent / 32 + k] = v;
+      }
     }
   }
   float m = -INFINITY, l = 0.f;
@@ -303,7 +314,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
 
   // scores of the wave's rows and keys, operands read ahead
   v4f s[NKT];
-  auto score = [&](int ln, int slot) {
+  auto score = [&](int ln, int slot, auto between) {
     constexpr int STEPS = 4 * NKT, DEPTH = 2;  // a step: 128 values of 16 keys
     const int key = ln & 15, g = ln >> 4;
     const uint8_t* codes = s_codes + slot * kCodesBytes + 4 * kt * kGroup;
@@ -313,33 +324,44 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
     const uint8_t* scale = s_scale + slot * kScalesBytes + (key >> 3) * 256 + (key & 7) * kScaleBytes + 4 * g + 2 * kt * 256;
     v4i x[STEPS];
     uint32_t sk[NKT];
-    v4i xr[NKT][2];
     auto read = [&](auto i) {
       constexpr int j = i / 4, tt = i % 4;
       if constexpr (tt == 0) sk[j] = *reinterpret_cast<const uint32_t*>(scale + 2 * j * 256);
       x[i] = *reinterpret_cast<const v4i*>(codes + (at0 ^ (tt << 4)) + 4 * j * kGroup);
     };
-    unroll<DEPTH>(read);
+    // the position part first: its operands need not share the registers with the others'
+    {
+      v4i xr[NKT][2], qr[2];
 #pragma unroll
-    for (int j = 0; j < NKT; ++j) s[j] = v4f{0.f, 0.f, 0.f, 0.f};
+      for (int k = 0; k < 2; ++k) {
+#pragma unroll
+        for (int j = 0; j < NKT; ++j) xr[j][k] = *reinterpret_cast<const v4i*>(rope + 2 * j * kGroup + 64 * k);
+        if constexpr (ONE) qr[k] = *reinterpret_cast<const v4i*>(s_qr + (row0 + key) * kQueryStride + 64 * k + 16 * g);
+        else qr[k] = q[kLatent / 32 + k];
+      }
+      between();
+#pragma unroll
+      for (int j = 0; j < NKT; ++j) {
+        s[j] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, xr[j][k]),
+                                                         __builtin_bit_cast(v8bf, qr[k]), s[j], 0, 0, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    unroll<DEPTH>(read);
     unroll<STEPS>([&](auto i) {
       constexpr int j = i / 4, tt = i % 4;
       if constexpr (i + DEPTH < STEPS) read(std::integral_constant<int, i + DEPTH>{});
-      if constexpr (tt == 2) {
-        xr[j][0] = *reinterpret_cast<const v4i*>(rope + 2 * j * kGroup);
-        xr[j][1] = *reinterpret_cast<const v4i*>(rope + 2 * j * kGroup + 64);
-      }
+      v4i last;
+      if constexpr (ONE && tt == 3) last = *reinterpret_cast<const v4i*>(s_qr + (row0 + key) * kQueryStride + 2 * kRope + 16 * g);
       const float e = scale_operand(sk[j] >> (8 * tt) & 255u);
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const v8bf k8 = __builtin_bit_cast(v8bf, decode8((uint32_t)x[i][u], e));
-        s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, __builtin_bit_cast(v8bf, q[4 * tt + u]), s[j], 0, 0, 0);
-      }
-      if constexpr (tt == 3) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-          s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, xr[j][k]),
-                                                         __builtin_bit_cast(v8bf, q[kLatent / 32 + k]), s[j], 0, 0, 0);
+        const v4i qu = 4 * tt + u < QK ? q[4 * tt + u < QK ? 4 * tt + u : 0] : last;
+        s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, __builtin_bit_cast(v8bf, qu), s[j], 0, 0, 0);
       }
       __builtin_amdgcn_sched_barrier(0);
     });
@@ -443,14 +465,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
         }
       };
       v8bf wt[STEPS][2];
-      auto read_weights = [&](auto i) {
+      auto read_weights = [&](auto i, int part) {
         constexpr int k = i / CT, y = i % CT;
         const uint8_t* wp = wgt + (32 * y + (ln & 31)) * kWeightStride + 32 * k + 16 * h;
-        wt[i][0] = __builtin_bit_cast(v8bf, *reinterpret_cast<const v4i*>(wp));
-        wt[i][1] = __builtin_bit_cast(v8bf, *reinterpret_cast<const v4i*>(wp + 2 * KT));
+        wt[i][part] = __builtin_bit_cast(v8bf, *reinterpret_cast<const v4i*>(wp + part * 2 * KT));
       };
       read_values(std::integral_constant<int, 0>{});
-      read_weights(std::integral_constant<int, 0>{});
+      read_weights(std::integral_constant<int, 0>{}, 0);
 #pragma unroll
       for (int y = 0; y < CT; ++y) {
         const float al = s_alpha[wslot][32 * y + (ln & 31)];
@@ -462,12 +483,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
       __builtin_amdgcn_sched_barrier(0);
       unroll<STEPS>([&](auto i) {
         constexpr int k = i / CT, y = i % CT;
-        if constexpr (i + 1 < STEPS) read_weights(std::integral_constant<int, i + 1>{});
         if constexpr (i == CT) read_values(std::integral_constant<int, 1>{});
+        read_weights(i, 1);
         unroll<4>([&](auto u) {  // both value tiles with the high parts, then with the low ones
           constexpr int x = u % 2;
           const v8bf v = __builtin_bit_cast(v8bf, __builtin_shufflevector(v0[k][x], v1[k][x], 0, 1, 2, 3, 4, 5, 6, 7));
           o[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, wt[i][u / 2], o[x][y], 0, 0, 0);
+          if constexpr (u == 1 && i + 1 < STEPS) read_weights(std::integral_constant<int, i + 1>{}, 0);
           after(std::integral_constant<int, 4 * i + u>{}, std::integral_constant<int, 4 * STEPS>{});
           __builtin_amdgcn_sched_barrier(0);
         });
@@ -485,13 +507,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
     // the query is in registers before the loop (its waits would fall inside it)
     if (scoring) {
 #pragma unroll
-      for (int k = 0; k < kAttnDim / 32; k += 2) asm volatile("s_waitcnt vmcnt(0)" : "+v"(q[k]), "+v"(q[k + 1]));
+      for (int k = 0; k < QK; ++k) asm volatile("s_waitcnt vmcnt(0)" : "+v"(q[k]));
     }
     asm volatile("s_waitcnt vmcnt(0)" : "+v"(entry), "+v"(page)::"memory");
     __syncthreads();
     if constexpr (ONE) unroll<LOADS>([&](auto p) { load_piece(lane, t0 + 1, 1, p); });
     if (scoring) {
-      score(lane, 0);
+      score(lane, 0, [] {});
       finish_scores(lane, t0, 0);
     }
     if constexpr (!ONE) __syncthreads();
@@ -513,20 +535,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
     if constexpr (ONE) {
       const auto weigh = [&](auto p) { weigh_piece(ln, (i + 1) & 1, p); };
       const auto widen = [&](auto p) { widen_piece(ln, next, (i + 1) & 1, p); };
-      score(ln, next);
+      score(ln, next, [&] { unroll<LOADS>(load); });
       finish_scores(ln, t0 + i + 1, next);
       output(ln, i & 1, i & 1, [&](auto step, auto steps) {
-        pieces_after<steps, WEIGHS + WIDENS + LOADS, step>([&](auto p) {
-          if constexpr (p < LOADS) load(p);
-          else if constexpr (p < LOADS + WEIGHS) weigh(std::integral_constant<int, p - LOADS>{});
-          else widen(std::integral_constant<int, p - LOADS - WEIGHS>{});
+        pieces_after<steps, WEIGHS + WIDENS, step>([&](auto p) {
+          if constexpr (p < WEIGHS) weigh(p);
+          else widen(std::integral_constant<int, p - WEIGHS>{});
         });
       });
     } else {
       unroll<LOADS>(load);
       unroll<WIDENS>([&](auto p) { widen_piece(ln, slot, 0, p); });
       if (scoring) {
-        score(ln, next);
+        score(ln, next, [] {});
         finish_scores(ln, t0 + i + 1, next);
       }
       __syncthreads();
