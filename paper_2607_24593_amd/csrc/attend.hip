@@ -194,55 +194,66 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
   // so that no step waits for its load: the set's entry; the page of its
   // position; the cache row.  Waves 0 .. 3 load position values and scales of
   // these keys, waves 4 .. 7 their codes.
-  const int32_t* idx = sets ? a.idx + (int64_t)unit * a.topk : nullptr;
-  const int32_t* pages = a.map.pages ? a.map.pages + (int64_t)b * a.map.max_pages : nullptr;
+  // Both loads are made in every call (where there is no set or no page table, of
+  // any readable word): a choice between a load's result and another value would
+  // be made, and waited for, where the load is.
+  const bool paged = a.map.pages != nullptr;
+  const int32_t* any_word = reinterpret_cast<const int32_t*>(a.cache.codes);
+  const int32_t* idx = sets ? a.idx + (int64_t)unit * a.topk : any_word;
+  const int32_t* pages = paged ? a.map.pages + (int64_t)b * a.map.max_pages : any_word;
   const int w4 = w & 3;
   const bool code_wave = w >= 4;
   auto fetch = [&](int ln, int tile) {
     const int k = min(tile * KT + 8 * w4 + (ln & 7), n - 1);
-    return sets ? idx[k] : k;
+    return idx[sets ? k : 0];
   };
-  // pos: the position whose row is loaded (0 for keys that do not count), at: the one that masks the key
+  // of key (ln & 7) of the tile with set entry `entry`: pos: the position whose
+  // row is loaded (0 for keys that do not count), at: the one that masks the key
   auto place = [&](int ln, int tile, int entry, int& pos, int& at) {
-    const bool ok = ((uint32_t)entry <= (uint32_t)pos_last) & (tile < t1) & (tile * KT + 8 * w4 + (ln & 7) < n);
+    const int k = tile * KT + 8 * w4 + (ln & 7);
+    entry = sets ? entry : k;
+    const bool ok = ((uint32_t)entry <= (uint32_t)pos_last) & (tile < t1) & (k < n);
     pos = ok ? entry : 0;
     at = ok ? entry : 0x7FFFFFFF;
-    return pages ? pages[pos >> a.map.shift] : 0;
+    return pages[paged ? pos >> a.map.shift : 0];
   };
   auto locate = [&](int pos, int page) -> int {
-    if (!pages) return (int)(b * a.map.stride) + pos;
+    if (!paged) return (int)(b * a.map.stride) + pos;
     return (min(max(page, 0), a.map.n_pages - 1) << a.map.shift) | (pos & ((1 << a.map.shift) - 1));
   };
   const uint32_t codes0 = (uint32_t)(uintptr_t)LDS(uint8_t, s_codes), rope0 = (uint32_t)(uintptr_t)LDS(uint8_t, s_rope),
                  scale0 = (uint32_t)(uintptr_t)LDS(uint8_t, s_scale);
   int at = 0, pos = 0, page = 0, entry = 0;  // of the next tile to be loaded; the entry of the one after
-  int row = 0;
+  int row1 = 0, row2 = 0, row_at = 0;  // the rows of the lane's two loads; the masking position
   auto load_piece = [&](int ln, int tile, int slot, auto piece) {
     constexpr int P = piece;
     if constexpr (P == 0) {
-      row = locate(pos, page);
-    } else if constexpr (P == 1) {  // 8 keys' position values, or 4 keys' codes
+      const int row = locate(pos, page);
+      row_at = at;
+      row1 = __shfl(row, ln >> (code_wave ? 4 : 3), 64);
+      row2 = __shfl(row, code_wave ? 4 + (ln >> 4) : ln >> 2 & 7, 64);
+    } else if constexpr (P == 1) {  // before this tile's loads, so that it does not wait for them
+      page = place(ln, tile + 1, entry, pos, at);
+    } else if constexpr (P == 2) {
+      entry = fetch(ln, tile + 2);
+    } else if constexpr (P == 3) {  // 8 keys' position values, or 4 keys' codes
       const int key = ln >> (code_wave ? 4 : 3);
-      const int64_t r = __shfl(row, key, 64);
+      const int64_t r = row1;
       const uint8_t* base = code_wave ? a.cache.codes : reinterpret_cast<const uint8_t*>(a.cache.rope);
       const int chunk = code_wave ? (ln & 15) ^ key : (ln & 7) ^ (key >> 1);
       load_lds16(base + (r << (code_wave ? 8 : 7)) + (chunk << 4),
                  code_wave ? codes0 + slot * kCodesBytes + 2 * w4 * kGroup : rope0 + slot * kRopeBytes + w4 * kGroup);
-    } else if constexpr (P == 2) {
+    } else {
       if (code_wave) {
         const int key = ln >> 4;
-        const int64_t r = __shfl(row, 4 + key, 64);
+        const int64_t r = row2;
         load_lds16(a.cache.codes + r * kCodeBytes + (((ln & 15) ^ key) << 4),
                    codes0 + slot * kCodesBytes + (2 * w4 + 1) * kGroup);
       } else {
-        const int64_t r = __shfl(row, ln >> 2 & 7, 64);
+        const int64_t r = row2;
         load_lds4(a.cache.scales + r * kScaleBytes + 4 * (ln & 3), scale0 + slot * kScalesBytes + w4 * 256);
-        s_pos[slot * KT + 8 * w4 + (ln & 7)] = at;
+        s_pos[slot * KT + 8 * w4 + (ln & 7)] = row_at;
       }
-    } else if constexpr (P == 3) {
-      page = place(ln, tile + 1, entry, pos, at);
-    } else {
-      entry = fetch(ln, tile + 2);
     }
   };
   constexpr int LOADS = 5;
@@ -314,21 +325,23 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
 
   // scores of the wave's rows and keys, operands read ahead
   v4f s[NKT];
-  auto score = [&](int ln, int slot, auto between) {
-    constexpr int STEPS = 4 * NKT, DEPTH = 2;  // a step: 128 values of 16 keys
+  auto score = [&](int ln, int slot, auto after) {
+    constexpr int STEPS = 4 * 4 * NKT;  // products; those of the key tiles take turns, so that none waits for the one before
     const int key = ln & 15, g = ln >> 4;
     const uint8_t* codes = s_codes + slot * kCodesBytes + 4 * kt * kGroup;
     const uint32_t at0 = (uint32_t)((key >> 2) * kGroup + (key & 3) * kCodeBytes + 64 * g + ((key & 3) << 4));
     const uint8_t* rope = s_rope + slot * kRopeBytes + (key >> 3) * kGroup + (key & 7) * 2 * kRope +
                           ((g ^ ((key >> 1) & 3)) << 4) + 2 * kt * kGroup;
     const uint8_t* scale = s_scale + slot * kScalesBytes + (key >> 3) * 256 + (key & 7) * kScaleBytes + 4 * g + 2 * kt * 256;
-    v4i x[STEPS];
+    v4i x[4][NKT];  // [128 values][key tile]
     uint32_t sk[NKT];
-    auto read = [&](auto i) {
-      constexpr int j = i / 4, tt = i % 4;
-      if constexpr (tt == 0) sk[j] = *reinterpret_cast<const uint32_t*>(scale + 2 * j * 256);
-      x[i] = *reinterpret_cast<const v4i*>(codes + (at0 ^ (tt << 4)) + 4 * j * kGroup);
+    auto read = [&](auto tt) {
+#pragma unroll
+      for (int j = 0; j < NKT; ++j) x[tt][j] = *reinterpret_cast<const v4i*>(codes + (at0 ^ (tt << 4)) + 4 * j * kGroup);
     };
+#pragma unroll
+    for (int j = 0; j < NKT; ++j) sk[j] = *reinterpret_cast<const uint32_t*>(scale + 2 * j * 256);
+    read(std::integral_constant<int, 0>{});
     // the position part first: its operands need not share the registers with the others'
     {
       v4i xr[NKT][2], qr[2];
@@ -339,30 +352,32 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
         if constexpr (ONE) qr[k] = *reinterpret_cast<const v4i*>(s_qr + (row0 + key) * kQueryStride + 64 * k + 16 * g);
         else qr[k] = q[kLatent / 32 + k];
       }
-      between();
 #pragma unroll
-      for (int j = 0; j < NKT; ++j) {
-        s[j] = v4f{0.f, 0.f, 0.f, 0.f};
+      for (int j = 0; j < NKT; ++j) s[j] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int j = 0; j < NKT; ++j)
           s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, xr[j][k]),
                                                          __builtin_bit_cast(v8bf, qr[k]), s[j], 0, 0, 0);
-      }
       __builtin_amdgcn_sched_barrier(0);
     }
-    unroll<DEPTH>(read);
-    unroll<STEPS>([&](auto i) {
-      constexpr int j = i / 4, tt = i % 4;
-      if constexpr (i + DEPTH < STEPS) read(std::integral_constant<int, i + DEPTH>{});
-      v4i last;
-      if constexpr (ONE && tt == 3) last = *reinterpret_cast<const v4i*>(s_qr + (row0 + key) * kQueryStride + 2 * kRope + 16 * g);
-      const float e = scale_operand(sk[j] >> (8 * tt) & 255u);
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const v8bf k8 = __builtin_bit_cast(v8bf, decode8((uint32_t)x[i][u], e));
-        const v4i qu = 4 * tt + u < QK ? q[4 * tt + u < QK ? 4 * tt + u : 0] : last;
-        s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, __builtin_bit_cast(v8bf, qu), s[j], 0, 0, 0);
-      }
+    v8bf wide[2];  // the widened operand of this product and of the next
+    auto widen = [&](auto v) {
+      constexpr int tt = v / (4 * NKT), u = v / NKT % 4, j = v % NKT;
+      wide[v & 1] = __builtin_bit_cast(v8bf, decode8((uint32_t)x[tt][j][u], scale_operand(sk[j] >> (8 * tt) & 255u)));
+    };
+    widen(std::integral_constant<int, 0>{});
+    v4i last;
+    unroll<STEPS>([&](auto v) {
+      constexpr int tt = v / (4 * NKT), u = v / NKT % 4, j = v % NKT;
+      if constexpr (v % (4 * NKT) == 0 && tt + 1 < 4) read(std::integral_constant<int, tt + 1>{});
+      if constexpr (ONE && v == 3 * 4 * NKT)
+        last = *reinterpret_cast<const v4i*>(s_qr + (row0 + key) * kQueryStride + 2 * kRope + 16 * g);
+      if constexpr (v + 1 < STEPS) widen(std::integral_constant<int, v + 1>{});
+      const v4i qu = 4 * tt + u < QK ? q[4 * tt + u < QK ? 4 * tt + u : 0] : last;
+      s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide[v & 1], __builtin_bit_cast(v8bf, qu), s[j], 0, 0, 0);
+      after(v, std::integral_constant<int, STEPS>{});
       __builtin_amdgcn_sched_barrier(0);
     });
   };
@@ -456,13 +471,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
       const uint32_t at0 = (uint32_t)(((8 * (w & 1) + 2 * (g & 1) + ((ln & 3) >> 1)) ^ (4 * quad + 2 * h)) << 4);
       constexpr int STEPS = 2 * CT;  // a step: 16 keys, 32 rows
       v4s v0[2][2], v1[2][2];
-      auto read_values = [&](auto k) {
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const uint8_t* from = base + k * 16 * 2 * kLatent;
-          v0[k][x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, from + (at0 ^ (x << 6))));
-          v1[k][x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, from + (at0 ^ (x << 6) ^ 16) + 4 * 2 * kLatent));
-        }
+      auto read_value = [&](auto k, int x) {
+        const uint8_t* from = base + k * 16 * 2 * kLatent;
+        v0[k][x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, from + (at0 ^ (x << 6))));
+        v1[k][x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, from + (at0 ^ (x << 6) ^ 16) + 4 * 2 * kLatent));
       };
       v8bf wt[STEPS][2];
       auto read_weights = [&](auto i, int part) {
@@ -470,8 +482,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
         const uint8_t* wp = wgt + (32 * y + (ln & 31)) * kWeightStride + 32 * k + 16 * h;
         wt[i][part] = __builtin_bit_cast(v8bf, *reinterpret_cast<const v4i*>(wp + part * 2 * KT));
       };
-      read_values(std::integral_constant<int, 0>{});
+      read_value(std::integral_constant<int, 0>{}, 0);
+      read_value(std::integral_constant<int, 0>{}, 1);
       read_weights(std::integral_constant<int, 0>{}, 0);
+      read_weights(std::integral_constant<int, 0>{}, 1);
 #pragma unroll
       for (int y = 0; y < CT; ++y) {
         const float al = s_alpha[wslot][32 * y + (ln & 31)];
@@ -483,13 +497,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
       __builtin_amdgcn_sched_barrier(0);
       unroll<STEPS>([&](auto i) {
         constexpr int k = i / CT, y = i % CT;
-        if constexpr (i == CT) read_values(std::integral_constant<int, 1>{});
-        read_weights(i, 1);
         unroll<4>([&](auto u) {  // both value tiles with the high parts, then with the low ones
           constexpr int x = u % 2;
           const v8bf v = __builtin_bit_cast(v8bf, __builtin_shufflevector(v0[k][x], v1[k][x], 0, 1, 2, 3, 4, 5, 6, 7));
           o[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, wt[i][u / 2], o[x][y], 0, 0, 0);
-          if constexpr (u == 1 && i + 1 < STEPS) read_weights(std::integral_constant<int, i + 1>{}, 0);
+          // the next step's operands as registers fall free
+          if constexpr (i + 1 < STEPS && u == 1) read_weights(std::integral_constant<int, i + 1>{}, 0);
+          if constexpr (i + 1 < STEPS && u == 2) read_weights(std::integral_constant<int, i + 1>{}, 1);
+          if constexpr (i + 1 == CT && u >= 2) read_value(std::integral_constant<int, 1>{}, u - 2);
           after(std::integral_constant<int, 4 * i + u>{}, std::integral_constant<int, 4 * STEPS>{});
           __builtin_amdgcn_sched_barrier(0);
         });
@@ -504,20 +519,23 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
     page = place(lane, t0, entry0, pos, at);
     unroll<LOADS>([&](auto p) { load_piece(lane, t0, 0, p); });
     if constexpr (!ONE) unroll<LOADS>([&](auto p) { load_piece(lane, t0 + 1, 1, p); });
-    // the query is in registers before the loop (its waits would fall inside it)
-    if (scoring) {
+  }
+  // the query is in registers before the loop (its waits would fall inside it)
+  if (scoring) {
 #pragma unroll
-      for (int k = 0; k < QK; ++k) asm volatile("s_waitcnt vmcnt(0)" : "+v"(q[k]));
-    }
+    for (int k = 0; k < QK; ++k) asm volatile("s_waitcnt vmcnt(0)" : "+v"(q[k]));
+  }
+  if (count > 0) {
     asm volatile("s_waitcnt vmcnt(0)" : "+v"(entry), "+v"(page)::"memory");
     __syncthreads();
     if constexpr (ONE) unroll<LOADS>([&](auto p) { load_piece(lane, t0 + 1, 1, p); });
-    if (scoring) {
-      score(lane, 0, [] {});
+    const bool now = ONE ? w < 4 : scoring;
+    if (now) {
+      score(lane, 0, [](auto, auto) {});
       finish_scores(lane, t0, 0);
     }
     if constexpr (!ONE) __syncthreads();
-    if (scoring) unroll<WEIGHS>([&](auto p) { weigh_piece(lane, 0, p); });
+    if (now) unroll<WEIGHS>([&](auto p) { weigh_piece(lane, 0, p); });
     if constexpr (ONE) unroll<WIDENS>([&](auto p) { widen_piece(lane, 0, 0, p); });
   }
   // Iteration i: tile i + 2 is loaded, i + 1 scored, i put out (past the last
@@ -527,27 +545,35 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
     int ln = lane;  // addresses are made anew for every tile rather than kept in registers
     asm volatile("" : "+v"(ln));
     // every load is done, the entry and the page too (named here, so that the
-    // compiler waits for them nowhere else)
-    asm volatile("s_waitcnt vmcnt(0)" : "+v"(entry), "+v"(page)::"memory");
-    __syncthreads();
+    // compiler waits for them nowhere else), and all waves are here.  Written out:
+    // the waves of a workgroup may come to it by two ways (RG = 8).
+    const auto meet = [&] {
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : "+v"(entry), "+v"(page)::"memory");
+    };
     const int next = slot + 1 == NS ? 0 : slot + 1, after_next = next + 1 == NS ? 0 : next + 1;  // of i + 1, i + 2
     const auto load = [&](auto p) { load_piece(ln, t0 + i + 2, after_next, p); };
     if constexpr (ONE) {
-      const auto weigh = [&](auto p) { weigh_piece(ln, (i + 1) & 1, p); };
-      const auto widen = [&](auto p) { widen_piece(ln, next, (i + 1) & 1, p); };
-      score(ln, next, [&] { unroll<LOADS>(load); });
-      finish_scores(ln, t0 + i + 1, next);
+      // waves 0 .. 3 meet the others before they score tile i + 1, waves 4 .. 7
+      // after they scored tile i
+      const bool early = w < 4;
+      const int st = early ? i + 1 : i, ss = early ? next : slot;
+      if (early) meet();
+      score(ln, ss, [](auto, auto) {});
+      finish_scores(ln, t0 + st, ss);
+      unroll<WEIGHS>([&](auto p) { weigh_piece(ln, st & 1, p); });
+      if (!early) meet();
       output(ln, i & 1, i & 1, [&](auto step, auto steps) {
-        pieces_after<steps, WEIGHS + WIDENS, step>([&](auto p) {
-          if constexpr (p < WEIGHS) weigh(p);
-          else widen(std::integral_constant<int, p - WEIGHS>{});
+        pieces_after<steps, LOADS + WIDENS, step>([&](auto p) {
+          if constexpr (p < LOADS) load(p);
+          else widen_piece(ln, next, (i + 1) & 1, std::integral_constant<int, p - LOADS>{});
         });
       });
     } else {
+      meet();
       unroll<LOADS>(load);
       unroll<WIDENS>([&](auto p) { widen_piece(ln, slot, 0, p); });
       if (scoring) {
-        score(ln, next, [] {});
+        score(ln, next, [](auto, auto) {});
         finish_scores(ln, t0 + i + 1, next);
       }
       __syncthreads();
