@@ -109,6 +109,25 @@ struct Work {
   float2* part_ml;  // reference, sum
 };
 
+// How the output lies in the waves' registers.  RG = 8: 64 rows x 128 values a
+// wave, else all rows x 64 values (tiles of values x rows: 32 x 32, for RG = 1
+// 16 x 16): of the shapes with as many registers the ones with the least reads of
+// weights and values.
+template <int RG>
+struct Output {
+  static constexpr int XT = RG == 8 || RG == 1 ? 4 : 2;  // tiles of values
+  static constexpr int YT = RG >= 4 ? 2 : 1;             // tiles of rows
+  static constexpr int QUADS = RG == 1 ? XT : 4 * XT * YT;  // registers / 4, (y XT + x) 4 + i
+  __device__ static __forceinline__ int row(int w, int lane, int y) {
+    return RG == 1 ? lane & 15 : (RG == 8 ? 64 * (w >> 2) : 0) + 32 * y + (lane & 31);
+  }
+  // the first of four values
+  __device__ static __forceinline__ int value(int w, int lane, int x, int i) {
+    return RG == 1 ? 64 * w + 16 * x + 4 * (lane >> 4)
+                   : (RG == 8 ? 128 * (w & 3) : 64 * w) + 32 * x + 8 * i + 4 * (lane >> 5);
+  }
+};
+
 // A workgroup of 8 waves attends 16 RG rows (heads of one query; in a prefix call
 // heads of consecutive queries of a sequence) to one split of their keys, 32 at
 // a time, in four stages:
@@ -122,8 +141,7 @@ struct Work {
 //           it: one bf16 would round it by up to 2^-8, as much as the output's own
 //           rounding, and fp16 would lose the small ones;
 //   widen   codes to bf16 in LDS, 4 keys a wave;
-//   output  transposed, values x rows: a wave has 64 of the 512 values for all
-//           rows, and the values are read transposed from LDS once per tile.
+//   output  transposed, values x rows, the values read transposed from LDS.
 // RG = 8: a wave scores its 16 rows against all 32 keys; the stages of an
 // iteration (output of tile i; score and widen of i + 1; load of i + 2) need
 // nothing of each other, so one barrier per tile is enough, and the two waves of
@@ -145,12 +163,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
   constexpr int NKT = ONE ? 2 : 1;             // key tiles of 16 per wave
   constexpr int KG = ONE ? 1 : 2;              // waves that share a row group's keys
   constexpr int SCORERS = RG * KG;             // waves that score
-  constexpr int CT = RG == 1 ? 1 : RG / 2;     // output column tiles (of 32 rows, or of 16)
-  constexpr int NQ = RG == 1 ? 4 : 8 * CT;     // output registers per lane / 4
+  using O = Output<RG>;
   constexpr int NS = ONE ? 2 : 3;              // tiles' codes held
   constexpr int NV = ONE ? 2 : 1;              // tiles' values held
   constexpr int WB = ROWS * kWeightStride;
-  __shared__ __attribute__((aligned(16))) uint8_t s_val[NV * kValueBytes + (NV == 1 ? 512 : 0)];
+  __shared__ __attribute__((aligned(16))) uint8_t s_val[NV * kValueBytes];
   __shared__ __attribute__((aligned(16))) uint8_t s_codes[NS * kCodesBytes];
   __shared__ __attribute__((aligned(16))) uint8_t s_rope[NS * kRopeBytes];
   __shared__ __attribute__((aligned(16))) uint8_t s_scale[NS * kScalesBytes];
@@ -287,12 +304,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
     }
   }
   float m = -INFINITY, l = 0.f;
-  v16f o[2][CT];
+  v16f o[O::XT][O::YT];
   v4f o1[4];
 #pragma unroll
-  for (int x = 0; x < 2; ++x)
+  for (int x = 0; x < O::XT; ++x)
 #pragma unroll
-    for (int y = 0; y < CT; ++y)
+    for (int y = 0; y < O::YT; ++y)
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[x][y][i] = 0.f;
 #pragma unroll
@@ -466,46 +483,48 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
         __builtin_amdgcn_sched_barrier(0);
       });
     } else {
-      // keys 16 k + 8 h + 4 r + quad, chunks 8 w + 4 x + 2 (g & 1) + (ln & 3) / 2
-      const uint8_t* base = s_val + vslot * kValueBytes + (8 * h + quad) * 2 * kLatent + 256 * (w >> 1) + 8 * (ln & 1);
-      const uint32_t at0 = (uint32_t)(((8 * (w & 1) + 2 * (g & 1) + ((ln & 3) >> 1)) ^ (4 * quad + 2 * h)) << 4);
-      constexpr int STEPS = 2 * CT;  // a step: 16 keys, 32 rows
-      v4s v0[2][2], v1[2][2];
-      auto read_value = [&](auto k, int x) {
-        const uint8_t* from = base + k * 16 * 2 * kLatent;
-        v0[k][x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, from + (at0 ^ (x << 6))));
-        v1[k][x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, from + (at0 ^ (x << 6) ^ 16) + 4 * 2 * kLatent));
+      // keys 16 k + 8 h + 4 r + quad, chunks c0 + 4 x + 2 (g & 1) + (ln & 3) / 2 with
+      // c0 = 16 (w & 3) (RG = 8) or 8 w
+      const uint8_t* base = s_val + vslot * kValueBytes + (8 * h + quad) * 2 * kLatent +
+                            256 * (RG == 8 ? w & 3 : w >> 1) + 8 * (ln & 1);
+      const uint32_t at0 =
+          (uint32_t)((((RG == 8 ? 0 : 8 * (w & 1)) + 2 * (g & 1) + ((ln & 3) >> 1)) ^ (4 * quad + 2 * h)) << 4);
+      constexpr int STEPS = 2 * O::XT, AHEAD = 1;  // a step: 16 keys, 32 values, all rows; values are read one ahead
+      v4s v0[STEPS], v1[STEPS];
+      auto read_value = [&](auto i) {
+        const uint8_t* from = base + i / O::XT * 16 * 2 * kLatent;
+        const uint32_t d = (uint32_t)(i % O::XT << 6);
+        v0[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, from + (at0 ^ d)));
+        v1[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, from + (at0 ^ d ^ 16) + 4 * 2 * kLatent));
       };
-      v8bf wt[STEPS][2];
-      auto read_weights = [&](auto i, int part) {
-        constexpr int k = i / CT, y = i % CT;
-        const uint8_t* wp = wgt + (32 * y + (ln & 31)) * kWeightStride + 32 * k + 16 * h;
-        wt[i][part] = __builtin_bit_cast(v8bf, *reinterpret_cast<const v4i*>(wp + part * 2 * KT));
+      v8bf wt[2][2][O::YT];  // [16 keys][high, low][32 rows]
+      auto read_weight = [&](int k, int part, int y) {
+        wt[k][part][y] = __builtin_bit_cast(
+            v8bf, *reinterpret_cast<const v4i*>(wgt + O::row(w, ln, y) * kWeightStride + 32 * k + 16 * h + part * 2 * KT));
       };
-      read_value(std::integral_constant<int, 0>{}, 0);
-      read_value(std::integral_constant<int, 0>{}, 1);
-      read_weights(std::integral_constant<int, 0>{}, 0);
-      read_weights(std::integral_constant<int, 0>{}, 1);
 #pragma unroll
-      for (int y = 0; y < CT; ++y) {
-        const float al = s_alpha[wslot][32 * y + (ln & 31)];
+      for (int y = 0; y < O::YT; ++y) read_weight(0, 0, y);
+      unroll<AHEAD>(read_value);
+#pragma unroll
+      for (int y = 0; y < O::YT; ++y) read_weight(0, 1, y);
+#pragma unroll
+      for (int y = 0; y < O::YT; ++y) {
+        const float al = s_alpha[wslot][O::row(w, ln, y)];
         if (__any(al != 1.f)) {
 #pragma unroll
-          for (int x = 0; x < 2; ++x) o[x][y] *= al;
+          for (int x = 0; x < O::XT; ++x) o[x][y] *= al;
         }
       }
       __builtin_amdgcn_sched_barrier(0);
       unroll<STEPS>([&](auto i) {
-        constexpr int k = i / CT, y = i % CT;
-        unroll<4>([&](auto u) {  // both value tiles with the high parts, then with the low ones
-          constexpr int x = u % 2;
-          const v8bf v = __builtin_bit_cast(v8bf, __builtin_shufflevector(v0[k][x], v1[k][x], 0, 1, 2, 3, 4, 5, 6, 7));
-          o[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, wt[i][u / 2], o[x][y], 0, 0, 0);
-          // the next step's operands as registers fall free
-          if constexpr (i + 1 < STEPS && u == 1) read_weights(std::integral_constant<int, i + 1>{}, 0);
-          if constexpr (i + 1 < STEPS && u == 2) read_weights(std::integral_constant<int, i + 1>{}, 1);
-          if constexpr (i + 1 == CT && u >= 2) read_value(std::integral_constant<int, 1>{}, u - 2);
-          after(std::integral_constant<int, 4 * i + u>{}, std::integral_constant<int, 4 * STEPS>{});
+        constexpr int k = i / O::XT, x = i % O::XT;
+        const v8bf v = __builtin_bit_cast(v8bf, __builtin_shufflevector(v0[i], v1[i], 0, 1, 2, 3, 4, 5, 6, 7));
+        unroll<2 * O::YT>([&](auto u) {  // all rows with the high parts, then with the low ones
+          constexpr int part = u / O::YT, y = u % O::YT;
+          o[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, wt[k][part][y], o[x][y], 0, 0, 0);
+          if constexpr (u == 0 && i + AHEAD < STEPS) read_value(std::integral_constant<int, i + AHEAD>{});
+          if constexpr (i + 1 == O::XT) read_weight(1, part, y);  // in place of the one that was used last here
+          after(std::integral_constant<int, 2 * O::YT * i + u>{}, std::integral_constant<int, 2 * O::YT * STEPS>{});
           __builtin_amdgcn_sched_barrier(0);
         });
       });
@@ -609,18 +628,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
   if (wk.splits > 1) {
     if (tid < ROWS) wk.part_ml[part * ROWS + tid] = {s_max[0][tid], total_of(tid)};
     // the registers as they lie: the joining kernel has the same lanes
-    float4* po = wk.part_o + part * NQ * (64 * kWaves) + tid;
+    float4* po = wk.part_o + part * O::QUADS * (64 * kWaves) + tid;
     if constexpr (RG == 1) {
 #pragma unroll
       for (int x = 0; x < 4; ++x) po[x * 64 * kWaves] = float4{o1[x][0], o1[x][1], o1[x][2], o1[x][3]};
     } else {
 #pragma unroll
-      for (int y = 0; y < CT; ++y)
+      for (int y = 0; y < O::YT; ++y)
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+        for (int x = 0; x < O::XT; ++x)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            po[((2 * y + x) * 4 + i) * 64 * kWaves] =
+            po[((O::XT * y + x) * 4 + i) * 64 * kWaves] =
                 float4{o[x][y][4 * i], o[x][y][4 * i + 1], o[x][y][4 * i + 2], o[x][y][4 * i + 3]};
     }
     return;
@@ -631,38 +650,36 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
     if (a.lse) a.lse[orow + tid] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
     if (sm.stat) sm.stat[orow + tid] = {top == -INFINITY ? 0.f : top, sum == 0.f ? 0.f : 1.f / sum};
   }
-  // 32 rows (16) at a time through LDS, so that whole rows are written
-  constexpr int OS = 2 * kLatent + 16, OR = RG == 1 ? 16 : 32;
-  static_assert(OR * OS <= sizeof(s_val), "the rows fit");
+  // A row tile of every wave at a time through LDS, so that whole rows are
+  // written; chunks of 8 values change places by the row against bank conflicts.
+  constexpr int OR = RG == 1 ? 16 : RG == 8 ? 64 : 32;  // rows at a time
+  static_assert(OR * 2 * kLatent <= sizeof(s_val), "the rows fit");
 #pragma unroll
-  for (int y = 0; y < CT; ++y) {
-    const int row = 32 * y + (RG == 1 ? lane & 15 : lane & 31);
+  for (int y = 0; y < O::YT; ++y) {
+    const int row = O::row(w, lane, y), at_row = RG == 8 ? (row & 31) + 32 * (w >> 2) : row - 32 * y;
     const float sum = total_of(row), inv = sum == 0.f ? 0.f : 1.f / sum;
-    uint8_t* to = s_val + (row - 32 * y) * OS;
+    auto put = [&](int value, float a0, float a1, float a2, float a3) {
+      const v4bf v = {(__bf16)(a0 * inv), (__bf16)(a1 * inv), (__bf16)(a2 * inv), (__bf16)(a3 * inv)};
+      *reinterpret_cast<v4bf*>(s_val + at_row * 2 * kLatent + (((value >> 3) ^ (at_row & 63)) << 4) + (value & 4) * 2) = v;
+    };
     if constexpr (RG == 1) {
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        v4bf v;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = (__bf16)(o1[x][i] * inv);
-        *reinterpret_cast<v4bf*>(to + 2 * (64 * w + 16 * x + 4 * g)) = v;
-      }
+      for (int x = 0; x < O::XT; ++x) put(O::value(w, lane, x, 0), o1[x][0], o1[x][1], o1[x][2], o1[x][3]);
     } else {
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
+      for (int x = 0; x < O::XT; ++x)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          v4bf v;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = (__bf16)(o[x][y][4 * j + i] * inv);
-          *reinterpret_cast<v4bf*>(to + 2 * (64 * w + 32 * x + 8 * j + 4 * (lane >> 5))) = v;
-        }
+        for (int i = 0; i < 4; ++i)
+          put(O::value(w, lane, x, i), o[x][y][4 * i], o[x][y][4 * i + 1], o[x][y][4 * i + 2], o[x][y][4 * i + 3]);
     }
     __syncthreads();
-    for (int r = w; r < OR && 32 * y + r < rows; r += kWaves)
-      *reinterpret_cast<uint4*>(a.out + (orow + 32 * y + r) * kLatent + 8 * lane) =
-          *reinterpret_cast<const uint4*>(s_val + r * OS + 16 * lane);
-    if (y + 1 < CT) __syncthreads();
+    for (int r = w; r < OR; r += kWaves) {
+      const int out = RG == 8 ? 64 * (r >> 5) + 32 * y + (r & 31) : 32 * y + r;
+      if (out < rows)
+        *reinterpret_cast<uint4*>(a.out + (orow + out) * kLatent + 8 * lane) =
+            *reinterpret_cast<const uint4*>(s_val + r * 2 * kLatent + ((lane ^ (r & 63)) << 4));
+    }
+    if (y + 1 < O::YT) __syncthreads();
   }
 }
 
@@ -672,9 +689,9 @@ template <int RG>
 constexpr int kJoinQuads = RG == 1 ? 2 : 4;
 template <int RG>
 __global__ __launch_bounds__(64 * kWaves) void join_kernel(AttendArgs a, RunTable t, ScoreMap sm, Work wk) {
+  using O = Output<RG>;
   constexpr int ROWS = 16 * RG;
-  constexpr int CT = RG == 1 ? 1 : RG / 2;
-  constexpr int NQ = RG == 1 ? 4 : 8 * CT;
+  constexpr int NQ = O::QUADS;
   constexpr int JQ = kJoinQuads<RG>;
   extern __shared__ float s_w[];  // [splits][ROWS]
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
@@ -710,9 +727,8 @@ __global__ __launch_bounds__(64 * kWaves) void join_kernel(AttendArgs a, RunTabl
 #pragma unroll
   for (int j = 0; j < JQ; ++j) {
     const int quad = blockIdx.x * JQ + j;
-    const int row = RG == 1 ? lane & 15 : 32 * (quad / 8) + (lane & 31);
-    const int dv = RG == 1 ? 64 * w + 16 * quad + 4 * (lane >> 4)
-                           : 64 * w + 32 * (quad / 4 % 2) + 8 * (quad % 4) + 4 * (lane >> 5);
+    const int x = RG == 1 ? quad : quad / 4 % O::XT;
+    const int row = O::row(w, lane, RG == 1 ? 0 : quad / 4 / O::XT), dv = O::value(w, lane, x, quad % 4);
     const float4* po = wk.part_o + (part * NQ + quad) * (64 * kWaves) + tid;
     float4 sum = {0.f, 0.f, 0.f, 0.f};
     for (int s = 0; s < wk.splits; ++s) {
@@ -870,8 +886,7 @@ hipError_t launch_rows(const AttendArgs& a, const RunTable& t, const ScoreMap& s
   hipLaunchKernelGGL(attend_kernel<RG>, dim3(grid), dim3(64 * kWaves), 0, stream, a, t, sm, wk);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || wk.splits == 1) return e;
-  constexpr int NQ = RG == 1 ? 4 : 4 * RG;
-  hipLaunchKernelGGL(join_kernel<RG>, dim3(NQ / kJoinQuads<RG>, (unsigned)(wk.units * wk.row_tiles)), dim3(64 * kWaves),
+  hipLaunchKernelGGL(join_kernel<RG>, dim3(Output<RG>::QUADS / kJoinQuads<RG>, (unsigned)(wk.units * wk.row_tiles)), dim3(64 * kWaves),
                      (size_t)wk.splits * 16 * RG * 4, stream, a, t, sm, wk);
   return hipGetLastError();
 }
