@@ -683,18 +683,33 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
   }
 }
 
-// Joins the splits of a row tile: blockIdx.x a chunk of the lanes' registers,
-// blockIdx.y the row tile.
+// Joins the splits of a row tile (blockIdx.y).  An item is four registers of one
+// wave of the attention kernel, 1 KB a split; the items of one group hold the same
+// rows and share the splits' weights.  Bound by the bytes of the splits' outputs.
 template <int RG>
-constexpr int kJoinQuads = RG == 1 ? 2 : 4;
+struct Join {
+  static constexpr int kRows = RG == 1 ? 16 : 32;
+  static constexpr int kGroups = 16 * RG / kRows;
+  static constexpr int kItems = kWaves * Output<RG>::QUADS / kGroups;
+  static constexpr int kSharing = RG == 8 ? 4 : kWaves;  // waves of the attention kernel with the same rows
+};
+// Waves that share an item, each with every so-many-th split, their sums added up
+// in LDS: many splits mean few row tiles, and one wave for 128 splits leaves the
+// chip empty (1 x 128 rows x 128 splits: 202 us, with 8 waves 16); with 8 splits of
+// 32 x 128 rows 8 waves of one split each take 50 us, one wave for all 17.
+__host__ __device__ inline int join_waves(int splits) { return splits > 32 ? 8 : splits > 16 ? 4 : splits > 8 ? 2 : 1; }
+
 template <int RG>
 __global__ __launch_bounds__(64 * kWaves) void join_kernel(AttendArgs a, RunTable t, ScoreMap sm, Work wk) {
   using O = Output<RG>;
+  using J = Join<RG>;
   constexpr int ROWS = 16 * RG;
-  constexpr int NQ = O::QUADS;
-  constexpr int JQ = kJoinQuads<RG>;
-  extern __shared__ float s_w[];  // [splits][ROWS]
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  constexpr int LR = J::kRows;
+  constexpr int SL = 64 * kWaves / LR;   // splits whose weights are made side by side
+  extern __shared__ float s_w[];         // [splits][LR] weights
+  __shared__ float s_red[SL][LR];
+  __shared__ float4 s_sum[kWaves][64];
+  const int tid = threadIdx.x, lane = tid & 63, part_wave = tid >> 6;
   const int unit = blockIdx.y / wk.row_tiles, rt = blockIdx.y % wk.row_tiles;
   const bool sets = a.idx != nullptr;
   const int b = sets ? run_of(t, unit) : unit;
@@ -704,45 +719,72 @@ __global__ __launch_bounds__(64 * kWaves) void join_kernel(AttendArgs a, RunTabl
   const int rows = min(ROWS, unit_rows - first);
   const int64_t orow = ((int64_t)t.row0[b] + (sets ? unit - t.row0[b] : 0)) * a.heads + first;
   const int64_t part = (int64_t)blockIdx.y * wk.splits;
-  const float2* ml = wk.part_ml + part * ROWS;
-  if (tid < ROWS) {
+  // a group of rows, and of its registers (item: wave of the attention kernel,
+  // then quad) the one that this wave joins with per - 1 others
+  const int per = join_waves(wk.splits), blocks = J::kItems * per / kWaves;
+  const int group = blockIdx.x / blocks, item = (blockIdx.x % blocks * kWaves + part_wave) / per;
+  const int y = group % O::YT, q = item / J::kSharing;
+  const int w = group / O::YT * J::kSharing + item % J::kSharing;
+  const int x = RG == 1 ? q : q / 4, quad = (RG == 1 ? 0 : 4 * O::XT * y) + q;
+  const int row0 = O::row(w, 0, y);  // the first of the group's rows
+  {
+    const int r = tid % LR, s0 = tid / LR;
+    const float2* ml = wk.part_ml + part * ROWS + row0 + r;
     float top = -INFINITY;
-    for (int s = 0; s < wk.splits; ++s) top = fmaxf(top, ml[s * ROWS + tid].x);
+    for (int s = s0; s < wk.splits; s += SL) top = fmaxf(top, ml[(int64_t)s * ROWS].x);
+    s_red[s0][r] = top;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < SL; ++k) top = fmaxf(top, s_red[k][r]);
+    __syncthreads();
     const float ref = top == -INFINITY ? 0.f : top;
     float sum = 0.f;
-    for (int s = 0; s < wk.splits; ++s) {
-      const float2 v = ml[s * ROWS + tid];
+    for (int s = s0; s < wk.splits; s += SL) {
+      const float2 v = ml[(int64_t)s * ROWS];
       const float e = __builtin_amdgcn_exp2f(v.x - ref);
-      s_w[s * ROWS + tid] = e;
+      s_w[s * LR + r] = e;
       sum = fmaf(e, v.y, sum);
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    for (int s = 0; s < wk.splits; ++s) s_w[s * ROWS + tid] *= inv;
-    if (blockIdx.x == 0 && tid < rows) {
-      if (a.lse) a.lse[orow + tid] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
-      if (sm.stat) sm.stat[orow + tid] = {ref, inv};
-    }
-  }
-  __syncthreads();
+    s_red[s0][r] = sum;
+    __syncthreads();
+    sum = 0.f;
 #pragma unroll
-  for (int j = 0; j < JQ; ++j) {
-    const int quad = blockIdx.x * JQ + j;
-    const int x = RG == 1 ? quad : quad / 4 % O::XT;
-    const int row = O::row(w, lane, RG == 1 ? 0 : quad / 4 / O::XT), dv = O::value(w, lane, x, quad % 4);
-    const float4* po = wk.part_o + (part * NQ + quad) * (64 * kWaves) + tid;
-    float4 sum = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < wk.splits; ++s) {
-      const float e = s_w[s * ROWS + row];
-      if (e == 0.f) continue;  // an empty split wrote no output
-      const float4 v = po[(int64_t)s * NQ * (64 * kWaves)];
-      sum.x = fmaf(e, v.x, sum.x);
-      sum.y = fmaf(e, v.y, sum.y);
-      sum.z = fmaf(e, v.z, sum.z);
-      sum.w = fmaf(e, v.w, sum.w);
+    for (int k = 0; k < SL; ++k) sum += s_red[k][r];
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    for (int s = s0; s < wk.splits; s += SL) s_w[s * LR + r] *= inv;
+    // a group's first block writes its rows' statistics
+    if (s0 == 0 && row0 + r < rows && blockIdx.x % blocks == 0) {
+      if (a.lse) a.lse[orow + row0 + r] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+      if (sm.stat) sm.stat[orow + row0 + r] = {ref, inv};
     }
+    __syncthreads();
+  }
+  const float4* po = wk.part_o + (part * O::QUADS + quad) * (64 * kWaves) + 64 * w + lane;
+  float4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int s = part_wave % per; s < wk.splits; s += per) {
+    const float e = s_w[s * LR + lane % LR];
+    float4 v = {0.f, 0.f, 0.f, 0.f};
+    if (e != 0.f) v = po[(int64_t)s * O::QUADS * (64 * kWaves)];  // an empty split wrote no output
+    sum.x = fmaf(e, v.x, sum.x);
+    sum.y = fmaf(e, v.y, sum.y);
+    sum.z = fmaf(e, v.z, sum.z);
+    sum.w = fmaf(e, v.w, sum.w);
+  }
+  s_sum[part_wave][lane] = sum;
+  __syncthreads();
+  if (part_wave % per == 0) {
+    for (int k = 1; k < per; ++k) {
+      const float4 v = s_sum[part_wave + k][lane];
+      sum.x += v.x;
+      sum.y += v.y;
+      sum.z += v.z;
+      sum.w += v.w;
+    }
+    const int row = O::row(w, lane, y);
     if (row < rows) {
       const v4bf v = {(__bf16)sum.x, (__bf16)sum.y, (__bf16)sum.z, (__bf16)sum.w};
-      *reinterpret_cast<v4bf*>(a.out + (orow + row) * kLatent + dv) = v;
+      *reinterpret_cast<v4bf*>(a.out + (orow + row) * kLatent + O::value(w, lane, x, quad % 4)) = v;
     }
   }
 }
@@ -886,8 +928,10 @@ hipError_t launch_rows(const AttendArgs& a, const RunTable& t, const ScoreMap& s
   hipLaunchKernelGGL(attend_kernel<RG>, dim3(grid), dim3(64 * kWaves), 0, stream, a, t, sm, wk);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || wk.splits == 1) return e;
-  hipLaunchKernelGGL(join_kernel<RG>, dim3(Output<RG>::QUADS / kJoinQuads<RG>, (unsigned)(wk.units * wk.row_tiles)), dim3(64 * kWaves),
-                     (size_t)wk.splits * 16 * RG * 4, stream, a, t, sm, wk);
+  using J = Join<RG>;
+  hipLaunchKernelGGL(join_kernel<RG>, dim3((unsigned)(J::kGroups * J::kItems * join_waves(wk.splits) / kWaves),
+                          (unsigned)(wk.units * wk.row_tiles)),
+                     dim3(64 * kWaves), (size_t)wk.splits * J::kRows * 4, stream, a, t, sm, wk);
   return hipGetLastError();
 }
 
