@@ -101,10 +101,14 @@ constexpr int kWeightStride = 4 * kTileKeys + 16;
 constexpr int kQueryStride = 2 * kRope + 64 + 16;
 constexpr int kWaves = 8;
 
-// What one launch's workgroups are: units (query rows of an index-set call,
-// else sequences) x splits of the unit's keys x tiles of 16 RG rows.
+// What one launch's workgroups are: for every unit (query row of an index-set call,
+// else sequence) tiles of 16 RG rows x splits of the unit's keys.  Units of an
+// index-set call are alike; a sequence has as many splits as its length asks for,
+// and its workgroups follow those of the sequence before it (first).
 struct Work {
-  int units, splits, tiles_per_split, row_tiles;
+  int units, tiles_per_split;
+  int row_tiles, splits;  // of a unit, for sequences the most
+  int32_t first[kMaxSeq + 1];
   float4* part_o;
   float2* part_ml;  // reference, sum
 };
@@ -154,6 +158,23 @@ struct Output {
 // stages is cut into pieces issued between the output's matrix products, which
 // run on their own once issued; scheduling barriers keep the two from being
 // sorted apart.
+// The sequence that workgroup i belongs to: the last one with first <= i (one
+// without workgroups shares its first with the next).
+__device__ __forceinline__ int owner_of(const int32_t* first, int n, int i) {
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (first[mid] <= i) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+// splits of a sequence's keys
+__host__ __device__ inline int splits_of(const RunTable& t, int b, int tiles_per_split) {
+  const int tiles = (t.pos0[b] + t.n_rows[b] + kTileKeys - 1) / kTileKeys;
+  return tiles > tiles_per_split ? (tiles + tiles_per_split - 1) / tiles_per_split : 1;
+}
+
 template <int RG>
 __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, RunTable t, ScoreMap sm,
                                                                               Work wk) {
@@ -180,16 +201,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // consecutive work items share an XCD (workgroups go to the 8 XCDs in turn)
-  const int total = wk.units * wk.splits * wk.row_tiles;
-  const int xcd = blockIdx.x & 7, per = total >> 3, rem = total & 7;
-  const int item = xcd * per + min(xcd, rem) + (int)(blockIdx.x >> 3);
-  const int rt = item % wk.row_tiles, split = item / wk.row_tiles % wk.splits, unit = item / wk.row_tiles / wk.splits;
   const bool sets = a.idx != nullptr;
+  const int part = blockIdx.x;
+  const int unit = sets ? part / (wk.row_tiles * wk.splits) : owner_of(wk.first, t.n, part);
   const int b = sets ? run_of(t, unit) : unit;
   const int unit_rows = sets ? a.heads : t.n_rows[b] * a.heads;
+  const int row_tiles = (unit_rows + ROWS - 1) / ROWS;
+  const int splits = sets ? wk.splits : splits_of(t, b, wk.tiles_per_split);
+  const int in_unit = part - (sets ? unit * row_tiles * splits : wk.first[b]);
+  const int split = in_unit % splits, rt = row_tiles - 1 - in_unit / splits;  // the rows with the most keys first
   const int first = rt * ROWS;
-  if (first >= unit_rows) return;
   const int rows = min(ROWS, unit_rows - first);
   const int i_first = sets ? unit - t.row0[b] : 0;                       // the unit's first query in its sequence
   const int pos_last = t.pos0[b] + (sets ? i_first : (first + rows - 1) / a.heads);
@@ -197,9 +218,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
   const int n = sets ? a.topk : sm.s2 ? t.pos0[b] + t.n_rows[b] : pos_last + 1;
   const int all_tiles = (n + KT - 1) / KT;
   const int t0 = split * wk.tiles_per_split, t1 = min(all_tiles, t0 + wk.tiles_per_split);
-  const int64_t part = ((int64_t)unit * wk.row_tiles + rt) * wk.splits + split;
-  if (t0 >= t1 && wk.splits > 1) {
-    if (tid < ROWS) wk.part_ml[part * ROWS + tid] = {-INFINITY, 0.f};
+  if (t0 >= t1 && splits > 1) {
+    if (tid < ROWS) wk.part_ml[(int64_t)part * ROWS + tid] = {-INFINITY, 0.f};
     return;
   }
 
@@ -625,10 +645,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
     if constexpr (KG > 1) sum += s_sum[1][row];
     return sum;
   };
-  if (wk.splits > 1) {
-    if (tid < ROWS) wk.part_ml[part * ROWS + tid] = {s_max[0][tid], total_of(tid)};
+  if (splits > 1) {
+    if (tid < ROWS) wk.part_ml[(int64_t)part * ROWS + tid] = {s_max[0][tid], total_of(tid)};
     // the registers as they lie: the joining kernel has the same lanes
-    float4* po = wk.part_o + part * O::QUADS * (64 * kWaves) + tid;
+    float4* po = wk.part_o + (int64_t)part * O::QUADS * (64 * kWaves) + tid;
     if constexpr (RG == 1) {
 #pragma unroll
       for (int x = 0; x < 4; ++x) po[x * 64 * kWaves] = float4{o1[x][0], o1[x][1], o1[x][2], o1[x][3]};
@@ -715,10 +735,12 @@ __global__ __launch_bounds__(64 * kWaves) void join_kernel(AttendArgs a, RunTabl
   const int b = sets ? run_of(t, unit) : unit;
   const int unit_rows = sets ? a.heads : t.n_rows[b] * a.heads;
   const int first = rt * ROWS;
-  if (first >= unit_rows) return;
+  const int splits = sets ? wk.splits : splits_of(t, b, wk.tiles_per_split);
+  if (first >= unit_rows || splits == 1) return;
   const int rows = min(ROWS, unit_rows - first);
   const int64_t orow = ((int64_t)t.row0[b] + (sets ? unit - t.row0[b] : 0)) * a.heads + first;
-  const int64_t part = (int64_t)blockIdx.y * wk.splits;
+  const int row_tiles = (unit_rows + ROWS - 1) / ROWS;
+  const int64_t part = (sets ? unit * row_tiles * splits : wk.first[b]) + (row_tiles - 1 - rt) * splits;
   // a group of rows, and of its registers (item: wave of the attention kernel,
   // then quad) the one that this wave joins with per - 1 others
   const int per = join_waves(wk.splits), blocks = J::kItems * per / kWaves;
@@ -731,7 +753,7 @@ __global__ __launch_bounds__(64 * kWaves) void join_kernel(AttendArgs a, RunTabl
     const int r = tid % LR, s0 = tid / LR;
     const float2* ml = wk.part_ml + part * ROWS + row0 + r;
     float top = -INFINITY;
-    for (int s = s0; s < wk.splits; s += SL) top = fmaxf(top, ml[(int64_t)s * ROWS].x);
+    for (int s = s0; s < splits; s += SL) top = fmaxf(top, ml[(int64_t)s * ROWS].x);
     s_red[s0][r] = top;
     __syncthreads();
 #pragma unroll
@@ -739,7 +761,7 @@ __global__ __launch_bounds__(64 * kWaves) void join_kernel(AttendArgs a, RunTabl
     __syncthreads();
     const float ref = top == -INFINITY ? 0.f : top;
     float sum = 0.f;
-    for (int s = s0; s < wk.splits; s += SL) {
+    for (int s = s0; s < splits; s += SL) {
       const float2 v = ml[(int64_t)s * ROWS];
       const float e = __builtin_amdgcn_exp2f(v.x - ref);
       s_w[s * LR + r] = e;
@@ -751,7 +773,7 @@ __global__ __launch_bounds__(64 * kWaves) void join_kernel(AttendArgs a, RunTabl
 #pragma unroll
     for (int k = 0; k < SL; ++k) sum += s_red[k][r];
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    for (int s = s0; s < wk.splits; s += SL) s_w[s * LR + r] *= inv;
+    for (int s = s0; s < splits; s += SL) s_w[s * LR + r] *= inv;
     // a group's first block writes its rows' statistics
     if (s0 == 0 && row0 + r < rows && blockIdx.x % blocks == 0) {
       if (a.lse) a.lse[orow + row0 + r] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
@@ -762,7 +784,7 @@ __global__ __launch_bounds__(64 * kWaves) void join_kernel(AttendArgs a, RunTabl
   const float4* po = wk.part_o + (part * O::QUADS + quad) * (64 * kWaves) + 64 * w + lane;
   float4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-  for (int s = part_wave % per; s < wk.splits; s += per) {
+  for (int s = part_wave % per; s < splits; s += per) {
     const float e = s_w[s * LR + lane % LR];
     float4 v = {0.f, 0.f, 0.f, 0.f};
     if (e != 0.f) v = po[(int64_t)s * O::QUADS * (64 * kWaves)];  // an empty split wrote no output
@@ -860,6 +882,7 @@ struct Plan {
   int padded;
   int64_t base[kMaxSeq];
   int rows, max_n;
+  int64_t workgroups;
   int rg;       // row groups of 16 per workgroup
   Work wk;
   size_t bytes() const {
@@ -867,12 +890,11 @@ struct Plan {
   }
 };
 
-constexpr int kTargetWgs = 256;  // one per CU
-constexpr int kMaxSplits = 128;
+constexpr int kCus = 256;
 
 Plan plan_of(const AttendArgs& a, const RunTable& t) {
   Plan p{};
-  int64_t words = 0, unit_tiles = 0;
+  int64_t words = 0;
   int max_rows = 0;
   p.padded = (a.topk + kTileKeys - 1) / kTileKeys * kTileKeys;
   for (int b = 0; b < t.n; ++b) {
@@ -898,34 +920,41 @@ Plan plan_of(const AttendArgs& a, const RunTable& t) {
   p.wk.units = a.idx ? p.rows : t.n;
   p.wk.row_tiles = (int)((unit_rows + R - 1) / R);
   const int max_tiles = a.idx ? p.padded / kTileKeys : (p.max_n + kTileKeys - 1) / kTileKeys;
-  // tiles of all row tiles: what the workgroups share out evenly
-  if (a.idx) {
-    unit_tiles = (int64_t)p.rows * p.wk.row_tiles * max_tiles;
-  } else {
-    for (int b = 0; b < t.n; ++b)
-      unit_tiles += ((int64_t)t.n_rows[b] * a.heads + R - 1) / R * ((t.pos0[b] + t.n_rows[b] + kTileKeys - 1) / kTileKeys);
-  }
-  const int64_t least = p.rg == 8 ? 8 : p.rg == 4 ? 6 : 4;
-  int64_t each = (unit_tiles + kTargetWgs - 1) / kTargetWgs;
-  if (each < least) each = least;
-  if ((max_tiles + each - 1) / each > kMaxSplits) each = (max_tiles + kMaxSplits - 1) / kMaxSplits;
-  p.wk.splits = (int)((max_tiles + each - 1) / each);
-  if (p.wk.splits < 1) p.wk.splits = 1;
+  const auto row_tiles_of = [&](int b) { return ((int64_t)t.n_rows[b] * a.heads + R - 1) / R; };
+  // Splits of as few tiles as give no more workgroups than run at once: one more
+  // would wait for another to end.
+  const int64_t target = kCus;
+  const auto workgroups = [&](int64_t each) {
+    if (a.idx) return (int64_t)p.rows * p.wk.row_tiles * (max_tiles > each ? (max_tiles + each - 1) / each : 1);
+    int64_t w = 0;
+    for (int b = 0; b < t.n; ++b) w += row_tiles_of(b) * splits_of(t, b, (int)each);
+    return w;
+  };
+  int64_t each = p.rg == 8 ? 8 : p.rg == 4 ? 6 : 4;
+  while (each < max_tiles && workgroups(each) > target) each += 1 + each / 32;
+  if (each >= max_tiles) each = max_tiles > 0 ? max_tiles : 1;
   p.wk.tiles_per_split = (int)each;
+  p.wk.splits = max_tiles > 0 ? (int)((max_tiles + each - 1) / each) : 1;
+  p.workgroups = workgroups(each);
+  if (!a.idx) {
+    int32_t w = 0;
+    for (int b = 0; b < t.n; ++b) {
+      p.wk.first[b] = w;
+      w += (int32_t)(row_tiles_of(b) * splits_of(t, b, (int)each));
+    }
+    p.wk.first[t.n] = w;
+  }
   if (p.wk.splits > 1) {
-    const int64_t parts = (int64_t)p.wk.units * p.wk.row_tiles * p.wk.splits;
-    p.part_o = (size_t)parts * R * kLatent * 4;
-    p.part_ml = (size_t)parts * R * sizeof(float2);
-  } else {
-    p.wk.tiles_per_split = max_tiles > 0 ? max_tiles : 1;
+    p.part_o = (size_t)p.workgroups * R * kLatent * 4;
+    p.part_ml = (size_t)p.workgroups * R * sizeof(float2);
   }
   return p;
 }
 
 template <int RG>
-hipError_t launch_rows(const AttendArgs& a, const RunTable& t, const ScoreMap& sm, const Work& wk, hipStream_t stream) {
-  const unsigned grid = (unsigned)(wk.units * wk.splits * wk.row_tiles);
-  hipLaunchKernelGGL(attend_kernel<RG>, dim3(grid), dim3(64 * kWaves), 0, stream, a, t, sm, wk);
+hipError_t launch_rows(const AttendArgs& a, const RunTable& t, const ScoreMap& sm, const Work& wk, unsigned workgroups,
+                       hipStream_t stream) {
+  hipLaunchKernelGGL(attend_kernel<RG>, dim3(workgroups), dim3(64 * kWaves), 0, stream, a, t, sm, wk);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || wk.splits == 1) return e;
   using J = Join<RG>;
@@ -953,10 +982,10 @@ hipError_t launch_attend(const AttendArgs& a, const RunTable& t, hipStream_t str
   uint8_t* parts = ws + round256(p.scores) + round256(p.stats) + round256(p.slots);
   p.wk.part_o = (float4*)parts;
   p.wk.part_ml = (float2*)(parts + round256(p.part_o));
-  hipError_t e = p.rg == 8   ? launch_rows<8>(a, t, sm, p.wk, stream)
-                 : p.rg == 4 ? launch_rows<4>(a, t, sm, p.wk, stream)
-                 : p.rg == 2 ? launch_rows<2>(a, t, sm, p.wk, stream)
-                             : launch_rows<1>(a, t, sm, p.wk, stream);
+  hipError_t e = p.rg == 8   ? launch_rows<8>(a, t, sm, p.wk, (unsigned)p.workgroups, stream)
+                 : p.rg == 4 ? launch_rows<4>(a, t, sm, p.wk, (unsigned)p.workgroups, stream)
+                 : p.rg == 2 ? launch_rows<2>(a, t, sm, p.wk, (unsigned)p.workgroups, stream)
+                             : launch_rows<1>(a, t, sm, p.wk, (unsigned)p.workgroups, stream);
   if (e != hipSuccess || !a.acc || (a.idx && a.topk == 0)) return e;
   if (!a.idx) {
     const unsigned tiles = (unsigned)((p.max_n + kTileKeys - 1) / kTileKeys);
