@@ -84,6 +84,20 @@ __device__ __forceinline__ float groups_sum(float x) {
   return __uint_as_float(e[0]) + __uint_as_float(e[1]);
 }
 
+// A reduction over groups of LANES consecutive lanes, the result in all of them.
+template <int LANES, class Op>
+__device__ __forceinline__ float row_reduce(float x, Op op) {
+  x = op(x, lane_xor1(x));
+  x = op(x, lane_xor2(x));
+  x = op(x, lane_xor4(x));
+  if constexpr (LANES >= 16) x = op(x, lane_xor8(x));
+  if constexpr (LANES == 32) {
+    const auto e = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = op(__uint_as_float(e[0]), __uint_as_float(e[1]));
+  }
+  return x;
+}
+
 // LDS.  As loaded, 1024 bytes of one wave's load (4 keys' codes, 8 keys' position
 // values) are a group, the groups 1088 bytes apart; the 16-byte chunks of a row
 // change places by two bits of the key.  Together the two put one chunk of 16
@@ -182,13 +196,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
   constexpr int ROWS = 16 * RG;
   constexpr int KT = kTileKeys;
   constexpr int NKT = ONE ? 2 : 1;             // key tiles of 16 per wave
-  constexpr int KG = ONE ? 1 : 2;              // waves that share a row group's keys
-  constexpr int SCORERS = RG * KG;             // waves that score
+  constexpr int DG = ONE ? 1 : 4 / RG;         // waves that share 16 rows' products with 16 keys
+  constexpr int TT = 4 / DG;                   // a wave's part of them: blocks of 128 latent values
+  constexpr int KPT = ONE ? 1 : RG, LPR = kTileKeys / KPT;  // a thread's scores of a tile, threads of a row
   using O = Output<RG>;
-  constexpr int NS = ONE ? 2 : 3;              // tiles' codes held
-  constexpr int NV = ONE ? 2 : 1;              // tiles' values held
+  constexpr int AHEAD = ONE ? 1 : RG == 1 ? 3 : 2;  // tiles in flight; RG <= 4: as many as LDS has room for
+  constexpr int NS = AHEAD + (ONE ? 1 : 2);    // tiles' codes held
   constexpr int WB = ROWS * kWeightStride;
-  __shared__ __attribute__((aligned(16))) uint8_t s_val[NV * kValueBytes];
+  __shared__ __attribute__((aligned(16))) uint8_t s_val[2 * kValueBytes];
   __shared__ __attribute__((aligned(16))) uint8_t s_codes[NS * kCodesBytes];
   __shared__ __attribute__((aligned(16))) uint8_t s_rope[NS * kRopeBytes];
   __shared__ __attribute__((aligned(16))) uint8_t s_scale[NS * kScalesBytes];
@@ -197,7 +212,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
   // the part of the queries that finds no register: the position values and the
   // last 32 latent ones
   __shared__ __attribute__((aligned(16))) uint8_t s_qr[ONE ? ROWS * kQueryStride : 16];
-  __shared__ float s_alpha[2][ROWS], s_max[KG][ROWS], s_sum[KG][ROWS];
+  // partial scores of two tiles
+  constexpr int PR = kTileKeys + 4;  // words from one row to the next
+  __shared__ __attribute__((aligned(16))) float s_part[ONE ? 4 : 2 * DG * ROWS * PR];
+  __shared__ int s_entry[ONE ? 1 : 4 * 64], s_page[ONE ? 1 : 4 * 64];  // of 8 tiles' keys, on their way
+  __shared__ float s_alpha[2][ROWS], s_max[ROWS], s_sum[ROWS];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -223,15 +242,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
     return;
   }
 
-  const int kt = ONE ? 0 : w / RG;             // the wave's (first) 16 keys of a tile,
-  const int row0 = ONE ? 16 * w : 16 * (w % RG);  // and its rows of scores
-  const bool scoring = SCORERS == kWaves || w < SCORERS;
+  const int kt = ONE ? 0 : w / RG & 1;         // the wave's (first) 16 keys of a tile,
+  const int row0 = ONE ? 16 * w : 16 * (w % RG);  // its rows of scores,
+  const int dg = ONE ? 0 : w / (2 * RG);       // and its part of the products
 
-  // Keys 8 (w mod 4) + (lane & 7) of a tile, found in three steps a tile apart,
-  // so that no step waits for its load: the set's entry; the page of its
-  // position; the cache row.  Waves 0 .. 3 load position values and scales of
-  // these keys, waves 4 .. 7 their codes.
-  // Both loads are made in every call (where there is no set or no page table, of
+  // Keys 8 (w mod 4) + (lane & 7) of a tile, found in three steps, so that no step
+  // waits for its load: the set's entry; the page of its position; the cache row.
+  // Waves 0 .. 3 load position values and scales of these keys, waves 4 .. 7 their
+  // codes.
+  // RG = 8: a step a tile.  Both loads are made in every call (where there is no set or no page table, of
   // any readable word): a choice between a load's result and another value would
   // be made, and waited for, where the load is.
   const bool paged = a.map.pages != nullptr;
@@ -294,33 +313,89 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
     }
   };
   constexpr int LOADS = 5;
+  // RG <= 4: a step for the keys of 8 tiles, one a lane; waves 0 .. 3 load entries
+  // and pages into LDS, so that the only loads in the loop are those that the
+  // counts in meet() know.
+  int row_of = 0, at_of = 0;  // of the 8 tiles that are loaded
+  auto fetch8 = [&](int tile) {  // where the lane's entry of the 8 tiles from this one is
+    const int k = min((tile + (lane >> 3)) * KT + 8 * w4 + (lane & 7), n - 1);
+    return idx + (sets ? k : 0);
+  };
+  auto place8 = [&](int tile, int e) {  // pos and at of the 8 tiles from this one
+    const int k = (tile + (lane >> 3)) * KT + 8 * w4 + (lane & 7);
+    e = sets ? e : k;
+    const bool ok = ((uint32_t)e <= (uint32_t)pos_last) & (tile + (lane >> 3) < t1) & (k < n);
+    pos = ok ? e : 0;
+    at = ok ? e : 0x7FFFFFFF;
+  };
+  auto page8 = [&] { return pages + (paged ? pos >> a.map.shift : 0); };
+  int key_row1 = 0, key_row2 = 0, key_pos = 0;  // the rows of the lane's two loads; the masking position
+  auto rows_of = [&](int ln, int i) {           // of tile t0 + i, one of the 8
+    key_row1 = __shfl(row_of, 8 * (i & 7) + (ln >> (code_wave ? 4 : 3)), 64);
+    key_row2 = __shfl(row_of, 8 * (i & 7) + (code_wave ? 4 + (ln >> 4) : ln >> 2 & 7), 64);
+    key_pos = __shfl(at_of, 8 * (i & 7) + (ln & 7), 64);
+  };
+  auto next_rows = [&](int ln, int i) {  // the same, after steps that are due
+    if ((i & 7) == 0) {
+      row_of = locate(pos, s_page[64 * w4 + ln]);
+      at_of = at;
+      place8(t0 + i + 8, s_entry[64 * w4 + ln]);
+    } else if ((i & 7) == 1 && !code_wave) {  // every wave has read the ones before
+      load_lds4(page8(), (uint32_t)(uintptr_t)LDS(int, s_page) + 256 * w4);
+      load_lds4(fetch8(t0 + i - 1 + 16), (uint32_t)(uintptr_t)LDS(int, s_entry) + 256 * w4);
+    }
+    rows_of(ln, i);
+  };
+  auto load_rows = [&](int ln, int slot) {
+    const int64_t r1 = key_row1, r2 = key_row2;
+    if (code_wave) {
+      const int key = ln >> 4, chunk = (ln & 15) ^ key;
+      load_lds16(a.cache.codes + r1 * kCodeBytes + (chunk << 4), codes0 + slot * kCodesBytes + 2 * w4 * kGroup);
+      load_lds16(a.cache.codes + r2 * kCodeBytes + (chunk << 4), codes0 + slot * kCodesBytes + (2 * w4 + 1) * kGroup);
+    } else {
+      const int key = ln >> 3, chunk = (ln & 7) ^ (key >> 1);
+      load_lds16(reinterpret_cast<const uint8_t*>(a.cache.rope) + r1 * 2 * kRope + (chunk << 4),
+                 rope0 + slot * kRopeBytes + w4 * kGroup);
+      load_lds4(a.cache.scales + r2 * kScaleBytes + 4 * (ln & 3), scale0 + slot * kScalesBytes + w4 * 256);
+      s_pos[slot * KT + 8 * w4 + (ln & 7)] = key_pos;
+    }
+  };
 
   const float c = a.scale * kLog2e;
   // The wave's query rows as the second operand of the score products: lane (row
   // r, group g) has values 8 u .. + 7 of block 4 g + t in product 4 t + u, then
   // 8 g .. + 7 of each 32 position values.
-  constexpr int QK = ONE ? kLatent / 32 - 1 : kAttnDim / 32;  // products whose query part stays in registers
-  v4i q[QK];
-  // the last position the lane's row attends to; rows past the last one take its query, masked
+  constexpr int QK = ONE ? kLatent / 32 - 1 : 4 * TT;  // latent products whose query part stays in registers
+  constexpr int QR = ONE ? 0 : DG == 1 ? 2 : 1;        // and those of position values
+  v4i q[QK + QR];
+  // the last position that a row of scores attends to (RG = 8: the lane's, else the
+  // thread's); rows past the last one take its query, masked
   int limit;
   {
     const int mine = row0 + (lane & 15), flat = first + min(mine, rows - 1), g = lane >> 4;
     const int i = sets ? 0 : flat / a.heads, head = flat - i * a.heads;
-    limit = mine < rows ? t.pos0[b] + i_first + i : -1;
+    if constexpr (ONE) {
+      limit = mine < rows ? t.pos0[b] + i_first + i : -1;
+    } else {
+      const int r = tid / LPR;
+      limit = r < rows ? t.pos0[b] + i_first + (sets ? 0 : (first + r) / a.heads) : -1;
+    }
     const uint16_t* from = a.q + ((int64_t)t.row0[b] + i_first + i) * a.q_row + (int64_t)head * a.q_head;
-    if (scoring) {
 #pragma unroll
-      for (int k = 0; k < kLatent / 32; ++k) {
-        const v4i v = *reinterpret_cast<const v4i*>(from + 32 * (4 * g + k / 4) + 8 * (k % 4));
-        if (k < QK) q[k] = v;
-        else *reinterpret_cast<v4i*>(s_qr + mine * kQueryStride + 2 * kRope + 16 * g) = v;  // its own wave's
-      }
+    for (int k = 0; k < 4 * TT; ++k) {
+      const v4i v = *reinterpret_cast<const v4i*>(from + 32 * (4 * g + TT * dg + k / 4) + 8 * (k % 4));
+      if (k < QK) q[k] = v;
+      else *reinterpret_cast<v4i*>(s_qr + mine * kQueryStride + 2 * kRope + 16 * g) = v;  // its own wave's
+    }
+    if constexpr (ONE) {
 #pragma unroll
-      for (int k = 0; k < kRope / 32; ++k) {
-        const v4i v = *reinterpret_cast<const v4i*>(from + kLatent + 32 * k + 8 * g);
-        if constexpr (ONE) *reinterpret_cast<v4i*>(s_qr + mine * kQueryStride + 64 * k + 16 * g) = v;
-        else q[kLatent / 32 + k] = v;
-      }
+      for (int k = 0; k < kRope / 32; ++k)
+        *reinterpret_cast<v4i*>(s_qr + mine * kQueryStride + 64 * k + 16 * g) =
+            *reinterpret_cast<const v4i*>(from + kLatent + 32 * k + 8 * g);
+    } else {
+#pragma unroll
+      for (int k = 0; k < QR; ++k)
+        q[QK + k] = DG == 4 && dg >= 2 ? v4i{0, 0, 0, 0} : *reinterpret_cast<const v4i*>(from + kLatent + 32 * (QR == 2 ? k : dg & 1) + 8 * g);
     }
   }
   float m = -INFINITY, l = 0.f;
@@ -341,7 +416,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
   }
 
   // ---- the other stages
-  // one of the wave's 4 keys, 8 values a lane: read, then widened
+  // 8 values a lane of the wave's j-th key, widened
+  auto put_values = [&](int ln, int j, int vslot, uint32_t word, int byte) {
+    // a NaN block makes the key's scores NaN; as a value it must not reach the
+    // rows that do not attend to the key (0 * NaN)
+    const int e = byte & ((byte - 255) >> 31);
+    *reinterpret_cast<uint4*>(s_val + vslot * kValueBytes + (4 * w + j) * 2 * kLatent +
+                              (16 * ln ^ (swizzle(4 * w + j) << 4))) = decode8(word, scale_operand(e));
+  };
+  // one of the wave's 4 keys: read, then widened
   uint32_t word[2];
   int byte[2];
   auto widen_piece = [&](int ln, int slot, int vslot, auto piece) {
@@ -351,25 +434,21 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
                                                        j * kCodeBytes);
       byte[j & 1] = s_scale[slot * kScalesBytes + (w >> 1) * 256 + (4 * (w & 1) + j) * kScaleBytes + (ln >> 2)];
     } else {
-      // a NaN block makes the key's scores NaN; as a value it must not reach the
-      // rows that do not attend to the key (0 * NaN)
-      const int e = byte[j & 1] & ((byte[j & 1] - 255) >> 31);
-      *reinterpret_cast<uint4*>(s_val + vslot * kValueBytes + (4 * w + j) * 2 * kLatent +
-                                (16 * ln ^ (swizzle(4 * w + j) << 4))) = decode8(word[j & 1], scale_operand(e));
+      put_values(ln, j, vslot, word[j & 1], byte[j & 1]);
     }
   };
   constexpr int WIDENS = 8;
 
   // scores of the wave's rows and keys, operands read ahead
   v4f s[NKT];
-  auto score = [&](int ln, int slot, auto after) {
+  auto score = [&](int ln, int slot) {
     constexpr int STEPS = 4 * 4 * NKT;  // products; those of the key tiles take turns, so that none waits for the one before
     const int key = ln & 15, g = ln >> 4;
-    const uint8_t* codes = s_codes + slot * kCodesBytes + 4 * kt * kGroup;
+    const uint8_t* codes = s_codes + slot * kCodesBytes;
     const uint32_t at0 = (uint32_t)((key >> 2) * kGroup + (key & 3) * kCodeBytes + 64 * g + ((key & 3) << 4));
     const uint8_t* rope = s_rope + slot * kRopeBytes + (key >> 3) * kGroup + (key & 7) * 2 * kRope +
-                          ((g ^ ((key >> 1) & 3)) << 4) + 2 * kt * kGroup;
-    const uint8_t* scale = s_scale + slot * kScalesBytes + (key >> 3) * 256 + (key & 7) * kScaleBytes + 4 * g + 2 * kt * 256;
+                          ((g ^ ((key >> 1) & 3)) << 4);
+    const uint8_t* scale = s_scale + slot * kScalesBytes + (key >> 3) * 256 + (key & 7) * kScaleBytes + 4 * g;
     v4i x[4][NKT];  // [128 values][key tile]
     uint32_t sk[NKT];
     auto read = [&](auto tt) {
@@ -386,8 +465,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
       for (int k = 0; k < 2; ++k) {
 #pragma unroll
         for (int j = 0; j < NKT; ++j) xr[j][k] = *reinterpret_cast<const v4i*>(rope + 2 * j * kGroup + 64 * k);
-        if constexpr (ONE) qr[k] = *reinterpret_cast<const v4i*>(s_qr + (row0 + key) * kQueryStride + 64 * k + 16 * g);
-        else qr[k] = q[kLatent / 32 + k];
+        qr[k] = *reinterpret_cast<const v4i*>(s_qr + (row0 + key) * kQueryStride + 64 * k + 16 * g);
       }
 #pragma unroll
       for (int j = 0; j < NKT; ++j) s[j] = v4f{0.f, 0.f, 0.f, 0.f};
@@ -409,12 +487,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
     unroll<STEPS>([&](auto v) {
       constexpr int tt = v / (4 * NKT), u = v / NKT % 4, j = v % NKT;
       if constexpr (v % (4 * NKT) == 0 && tt + 1 < 4) read(std::integral_constant<int, tt + 1>{});
-      if constexpr (ONE && v == 3 * 4 * NKT)
+      if constexpr (v == 3 * 4 * NKT)
         last = *reinterpret_cast<const v4i*>(s_qr + (row0 + key) * kQueryStride + 2 * kRope + 16 * g);
       if constexpr (v + 1 < STEPS) widen(std::integral_constant<int, v + 1>{});
       const v4i qu = 4 * tt + u < QK ? q[4 * tt + u < QK ? 4 * tt + u : 0] : last;
       s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide[v & 1], __builtin_bit_cast(v8bf, qu), s[j], 0, 0, 0);
-      after(v, std::integral_constant<int, STEPS>{});
       __builtin_amdgcn_sched_barrier(0);
     });
   };
@@ -426,7 +503,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
     top = -INFINITY;
 #pragma unroll
     for (int j = 0; j < NKT; ++j) {
-      const int k4 = 16 * (kt + j) + 4 * g;
+      const int k4 = 16 * j + 4 * g;
       const v4i key_at = *reinterpret_cast<const v4i*>(&s_pos[slot * KT + k4]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -437,7 +514,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
         *reinterpret_cast<v4f*>(s2 + (int64_t)tile * unit_rows * KT + ((row0 + key) * KT + k4)) = s[j];
     }
     top = groups_max(top);
-    if constexpr (!ONE) s_max[kt][row0 + key] = top;
   };
   // the scores' weights to s_w[wslot]
   float ref = 0.f, alpha = 1.f, e[NKT][4];
@@ -445,7 +521,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
   auto weigh_piece = [&](int ln, int wslot, auto piece) {
     const int key = ln & 15, g = ln >> 4, mine = row0 + key;
     if constexpr (piece == 0) {
-      if constexpr (!ONE) top = fmaxf(s_max[0][mine], s_max[1][mine]);
       const bool move = top > m + 32.f;
       const float next = move ? top : m;
       alpha = move ? __builtin_amdgcn_exp2f(m - next) : 1.f;
@@ -466,7 +541,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
         v4bf lo;
 #pragma unroll
         for (int i = 0; i < 4; ++i) lo[i] = (__bf16)(e[j][i] - (float)hi[j][i]);
-        uint8_t* to = s_w + wslot * WB + mine * kWeightStride + 32 * (kt + j) + 8 * g;
+        uint8_t* to = s_w + wslot * WB + mine * kWeightStride + 32 * j + 8 * g;
         *reinterpret_cast<v4bf*>(to) = hi[j];
         *reinterpret_cast<v4bf*>(to + 2 * KT) = lo;
       }
@@ -474,155 +549,323 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
   };
   constexpr int WEIGHS = 1 + 3 * NKT;
 
-  auto output = [&](int ln, int vslot, int wslot, auto after) {
+  // RG <= 4: what a wave reads from LDS for the stages of an iteration
+  v4i x[TT], xr[QR ? QR : 1];  // score: its keys' codes and position values
+  uint32_t sk = 0;             // and scales
+  float zp[KPT][DG];           // weigh: the scores' parts
+  int key_at[KPT];
+  uint32_t codes4[4];          // widen: its 4 keys
+  int scale4[4];
+  constexpr int OS = RG == 1 ? 4 : 2 * O::XT;  // output: steps of 16 (RG = 1: all 32) keys, 32 (16) values, all rows
+  v4s v0[OS], v1[OS];
+  v8bf wt[2][2][O::YT];  // [16 keys][high, low][32 rows]; RG = 1: [0][high, low][0]
+  float al[O::YT];
+  auto read_score = [&](int ln, int slot) {
+    const int key = ln & 15, g = ln >> 4;
+    const uint8_t* codes = s_codes + slot * kCodesBytes + 4 * kt * kGroup;
+    const uint32_t at0 = (uint32_t)((key >> 2) * kGroup + (key & 3) * kCodeBytes + 64 * g + ((key & 3) << 4));
+    const uint8_t* rope = s_rope + slot * kRopeBytes + (key >> 3) * kGroup + (key & 7) * 2 * kRope +
+                          ((g ^ ((key >> 1) & 3)) << 4) + 2 * kt * kGroup;
+    sk = *reinterpret_cast<const uint32_t*>(s_scale + slot * kScalesBytes + (key >> 3) * 256 + (key & 7) * kScaleBytes +
+                                            4 * g + 2 * kt * 256);
+#pragma unroll
+    for (int k = 0; k < QR; ++k) xr[k] = *reinterpret_cast<const v4i*>(rope + 64 * (QR == 2 ? k : dg & 1));
+#pragma unroll
+    for (int i = 0; i < TT; ++i) x[i] = *reinterpret_cast<const v4i*>(codes + (at0 ^ ((TT * dg + i) << 4)));
+  };
+  // the wave's part of the scores of its rows and keys, to s_part[buf]
+  auto score_part = [&](int ln, int buf) {
+    v4f sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < QR; ++k) {
+      if (DG == 4 && dg >= 2) xr[k] = v4i{0, 0, 0, 0};  // two of four waves have no position values left
+      sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, xr[k]), __builtin_bit_cast(v8bf, q[QK + k]),
+                                                    sum, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < TT; ++i) {
+      const float by = scale_operand(sk >> (8 * (TT * dg + i)) & 255u);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, decode8((uint32_t)x[i][u], by)),
+                                                      __builtin_bit_cast(v8bf, q[4 * i + u]), sum, 0, 0, 0);
+    }
+    *reinterpret_cast<v4f*>(&s_part[((buf * DG + dg) * ROWS + row0 + (ln & 15)) * PR + 16 * kt + 4 * (ln >> 4)]) = sum;
+  };
+  auto read_part = [&](int td, int slot, int buf) {
+    const int row = td / LPR, k0 = td % LPR * KPT;
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+      key_at[i] = s_pos[slot * KT + k0 + i];
+#pragma unroll
+      for (int d = 0; d < DG; ++d) zp[i][d] = s_part[((buf * DG + d) * ROWS + row) * PR + k0 + i];
+    }
+  };
+  // the weights of KPT scores of one row to s_w[wslot]
+  auto weigh_part = [&](int td, int tile, int wslot) {
+    const int row = td / LPR, k0 = td % LPR * KPT;
+    float z[KPT], e[KPT], top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+      z[i] = zp[i][0];
+#pragma unroll
+      for (int d = 1; d < DG; ++d) z[i] += zp[i][d];
+      z[i] = key_at[i] <= limit ? z[i] * c : -INFINITY;
+      top = fmaxf(top, z[i]);
+    }
+    top = row_reduce<LPR>(top, [](float x, float y) { return fmaxf(x, y); });
+    const bool move = top > m + 32.f;
+    const float next = move ? top : m;
+    const float alpha = move ? __builtin_amdgcn_exp2f(m - next) : 1.f;
+    const float ref = next == -INFINITY ? 0.f : next;
+    m = next;
+    l *= alpha;
+    if (k0 == 0) s_alpha[wslot][row] = alpha;
+    __bf16* to = reinterpret_cast<__bf16*>(s_w + wslot * WB + row * kWeightStride) + k0;
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+      e[i] = __builtin_amdgcn_exp2f(z[i] - ref);
+      l += e[i];
+      const __bf16 hi = (__bf16)e[i];
+      to[i] = hi;
+      to[KT + i] = (__bf16)(e[i] - (float)hi);
+      zp[i][0] = z[i];
+    }
+  };
+  auto keep_scores = [&](int td, int tile) {
+    const int row = td / LPR, k0 = td % LPR * KPT;
+    if (s2 && tile < t1 && row < rows) {
+#pragma unroll
+      for (int i = 0; i < KPT; ++i) s2[(int64_t)tile * unit_rows * KT + (row * KT + k0 + i)] = zp[i][0];
+    }
+  };
+  auto read_codes = [&](int ln, int slot) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      codes4[j] = *reinterpret_cast<const uint32_t*>(s_codes + slot * kCodesBytes + w * kGroup + ((4 * ln) ^ (j << 4)) +
+                                                     j * kCodeBytes);
+      scale4[j] = s_scale[slot * kScalesBytes + (w >> 1) * 256 + (4 * (w & 1) + j) * kScaleBytes + (ln >> 2)];
+    }
+  };
+  auto widen_codes = [&](int ln, int vslot) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      put_values(ln, j, vslot, codes4[j], scale4[j]);
+  };
+  auto read_output = [&](int ln, int vslot, int wslot) {
     const uint8_t* wgt = s_w + wslot * WB;
     const int g = ln >> 4, quad = (ln & 15) >> 2, h = ln >> 5;
     if constexpr (RG == 1) {
       // keys 8 g + 4 r + quad, chunks 8 w + 2 x + (ln & 3) / 2
       const uint8_t* base = s_val + vslot * kValueBytes + (8 * g + quad) * 2 * kLatent + 256 * (w >> 1) + 8 * (ln & 1);
       const uint32_t at0 = (uint32_t)(((8 * (w & 1) + ((ln & 3) >> 1)) ^ (4 * quad + (2 * g & 3))) << 4);
-      v4s v0[4], v1[4];
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        v0[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, base + (at0 ^ (x << 5))));
-        v1[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, base + (at0 ^ (x << 5) ^ 16) + 4 * 2 * kLatent));
+      for (int i = 0; i < OS; ++i) {
+        v0[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, base + (at0 ^ (i << 5))));
+        v1[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, base + (at0 ^ (i << 5) ^ 16) + 4 * 2 * kLatent));
       }
       const uint8_t* wp = wgt + (ln & 15) * kWeightStride + 16 * g;
-      const v8bf wt[2] = {__builtin_bit_cast(v8bf, *reinterpret_cast<const v4i*>(wp)),
-                          __builtin_bit_cast(v8bf, *reinterpret_cast<const v4i*>(wp + 2 * KT))};
-      const float al = s_alpha[wslot][ln & 15];
-      if (__any(al != 1.f)) {
 #pragma unroll
-        for (int x = 0; x < 4; ++x) o1[x] *= al;
-      }
-      unroll<8>([&](auto u) {
-        constexpr int x = u % 4;
-        const v8bf v = __builtin_bit_cast(v8bf, __builtin_shufflevector(v0[x], v1[x], 0, 1, 2, 3, 4, 5, 6, 7));
-        o1[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, wt[u / 4], o1[x], 0, 0, 0);
-        after(u, std::integral_constant<int, 8>{});
-        __builtin_amdgcn_sched_barrier(0);
-      });
-    } else {
-      // keys 16 k + 8 h + 4 r + quad, chunks c0 + 4 x + 2 (g & 1) + (ln & 3) / 2 with
-      // c0 = 16 (w & 3) (RG = 8) or 8 w
-      const uint8_t* base = s_val + vslot * kValueBytes + (8 * h + quad) * 2 * kLatent +
-                            256 * (RG == 8 ? w & 3 : w >> 1) + 8 * (ln & 1);
-      const uint32_t at0 =
-          (uint32_t)((((RG == 8 ? 0 : 8 * (w & 1)) + 2 * (g & 1) + ((ln & 3) >> 1)) ^ (4 * quad + 2 * h)) << 4);
-      constexpr int STEPS = 2 * O::XT, AHEAD = 1;  // a step: 16 keys, 32 values, all rows; values are read one ahead
-      v4s v0[STEPS], v1[STEPS];
-      auto read_value = [&](auto i) {
+      for (int part = 0; part < 2; ++part)
+        wt[0][part][0] = __builtin_bit_cast(v8bf, *reinterpret_cast<const v4i*>(wp + part * 2 * KT));
+      al[0] = s_alpha[wslot][ln & 15];
+    } else if constexpr (!ONE) {
+      // keys 16 k + 8 h + 4 r + quad, chunks 8 w + 4 x + 2 (g & 1) + (ln & 3) / 2
+      const uint8_t* base = s_val + vslot * kValueBytes + (8 * h + quad) * 2 * kLatent + 256 * (w >> 1) + 8 * (ln & 1);
+      const uint32_t at0 = (uint32_t)((((8 * (w & 1)) + 2 * (g & 1) + ((ln & 3) >> 1)) ^ (4 * quad + 2 * h)) << 4);
+#pragma unroll
+      for (int i = 0; i < OS; ++i) {
         const uint8_t* from = base + i / O::XT * 16 * 2 * kLatent;
         const uint32_t d = (uint32_t)(i % O::XT << 6);
         v0[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, from + (at0 ^ d)));
         v1[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, from + (at0 ^ d ^ 16) + 4 * 2 * kLatent));
-      };
-      v8bf wt[2][2][O::YT];  // [16 keys][high, low][32 rows]
-      auto read_weight = [&](int k, int part, int y) {
-        wt[k][part][y] = __builtin_bit_cast(
-            v8bf, *reinterpret_cast<const v4i*>(wgt + O::row(w, ln, y) * kWeightStride + 32 * k + 16 * h + part * 2 * KT));
-      };
-#pragma unroll
-      for (int y = 0; y < O::YT; ++y) read_weight(0, 0, y);
-      unroll<AHEAD>(read_value);
-#pragma unroll
-      for (int y = 0; y < O::YT; ++y) read_weight(0, 1, y);
+      }
 #pragma unroll
       for (int y = 0; y < O::YT; ++y) {
-        const float al = s_alpha[wslot][O::row(w, ln, y)];
-        if (__any(al != 1.f)) {
 #pragma unroll
-          for (int x = 0; x < O::XT; ++x) o[x][y] *= al;
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int part = 0; part < 2; ++part)
+            wt[k][part][y] = __builtin_bit_cast(
+                v8bf, *reinterpret_cast<const v4i*>(wgt + O::row(w, ln, y) * kWeightStride + 32 * k + 16 * h + part * 2 * KT));
+        al[y] = s_alpha[wslot][O::row(w, ln, y)];
+      }
+    }
+  };
+  auto add_output = [&] {
+#pragma unroll
+    for (int y = 0; y < O::YT; ++y)
+      if (RG < 4 || __any(al[y] != 1.f)) {
+#pragma unroll
+        for (int i = 0; i < O::XT; ++i) {
+          if constexpr (RG == 1) o1[i] *= al[y];
+          else o[i][y] *= al[y];
         }
       }
-      __builtin_amdgcn_sched_barrier(0);
-      unroll<STEPS>([&](auto i) {
-        constexpr int k = i / O::XT, x = i % O::XT;
+#pragma unroll
+    for (int part = 0; part < 2; ++part)  // all with the high parts, then with the low ones
+#pragma unroll
+      for (int i = 0; i < OS; ++i) {
         const v8bf v = __builtin_bit_cast(v8bf, __builtin_shufflevector(v0[i], v1[i], 0, 1, 2, 3, 4, 5, 6, 7));
-        unroll<2 * O::YT>([&](auto u) {  // all rows with the high parts, then with the low ones
-          constexpr int part = u / O::YT, y = u % O::YT;
-          o[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, wt[k][part][y], o[x][y], 0, 0, 0);
-          if constexpr (u == 0 && i + AHEAD < STEPS) read_value(std::integral_constant<int, i + AHEAD>{});
-          if constexpr (i + 1 == O::XT) read_weight(1, part, y);  // in place of the one that was used last here
-          after(std::integral_constant<int, 2 * O::YT * i + u>{}, std::integral_constant<int, 2 * O::YT * STEPS>{});
-          __builtin_amdgcn_sched_barrier(0);
-        });
-      });
+        if constexpr (RG == 1) {
+          o1[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, wt[0][part][0], o1[i], 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int y = 0; y < O::YT; ++y)
+            o[i % O::XT][y] =
+                __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, wt[i / O::XT][part][y], o[i % O::XT][y], 0, 0, 0);
+        }
+      }
+  };
+
+  // RG = 8: values are read one step ahead, other stages' pieces issued between the products
+  auto output = [&](int ln, int vslot, int wslot, auto after) {
+    const uint8_t* wgt = s_w + wslot * WB;
+    const int g = ln >> 4, quad = (ln & 15) >> 2, h = ln >> 5;
+    // keys 16 k + 8 h + 4 r + quad, chunks 16 (w & 3) + 4 x + 2 (g & 1) + (ln & 3) / 2
+    const uint8_t* base = s_val + vslot * kValueBytes + (8 * h + quad) * 2 * kLatent +
+                          256 * (w & 3) + 8 * (ln & 1);
+    const uint32_t at0 =
+        (uint32_t)(((2 * (g & 1) + ((ln & 3) >> 1)) ^ (4 * quad + 2 * h)) << 4);
+    constexpr int STEPS = 2 * O::XT;  // a step: 16 keys, 32 values, all rows; values are read one ahead
+    v4s v0[STEPS], v1[STEPS];
+    auto read_value = [&](auto i) {
+      const uint8_t* from = base + i / O::XT * 16 * 2 * kLatent;
+      const uint32_t d = (uint32_t)(i % O::XT << 6);
+      v0[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, from + (at0 ^ d)));
+      v1[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, from + (at0 ^ d ^ 16) + 4 * 2 * kLatent));
+    };
+    v8bf wt[2][2][O::YT];  // [16 keys][high, low][32 rows]
+    auto read_weight = [&](int k, int part, int y) {
+      wt[k][part][y] = __builtin_bit_cast(
+          v8bf, *reinterpret_cast<const v4i*>(wgt + O::row(w, ln, y) * kWeightStride + 32 * k + 16 * h + part * 2 * KT));
+    };
+#pragma unroll
+    for (int y = 0; y < O::YT; ++y) read_weight(0, 0, y);
+    read_value(std::integral_constant<int, 0>{});
+#pragma unroll
+    for (int y = 0; y < O::YT; ++y) read_weight(0, 1, y);
+#pragma unroll
+    for (int y = 0; y < O::YT; ++y) {
+      const float al = s_alpha[wslot][O::row(w, ln, y)];
+      if (__any(al != 1.f)) {
+#pragma unroll
+        for (int x = 0; x < O::XT; ++x) o[x][y] *= al;
+      }
     }
+    __builtin_amdgcn_sched_barrier(0);
+    unroll<STEPS>([&](auto i) {
+      constexpr int k = i / O::XT, x = i % O::XT;
+      const v8bf v = __builtin_bit_cast(v8bf, __builtin_shufflevector(v0[i], v1[i], 0, 1, 2, 3, 4, 5, 6, 7));
+      unroll<2 * O::YT>([&](auto u) {  // all rows with the high parts, then with the low ones
+        constexpr int part = u / O::YT, y = u % O::YT;
+        o[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, wt[k][part][y], o[x][y], 0, 0, 0);
+        if constexpr (u == 0 && i + 1 < STEPS) read_value(std::integral_constant<int, i + 1>{});
+        if constexpr (i + 1 == O::XT) read_weight(1, part, y);  // in place of the one that was used last here
+        after(std::integral_constant<int, 2 * O::YT * i + u>{}, std::integral_constant<int, 2 * O::YT * STEPS>{});
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    });
   };
 
   const int count = t1 - t0;
   if (count > 0) {
-    const int entry0 = fetch(lane, t0);
-    entry = fetch(lane, t0 + 1);
-    page = place(lane, t0, entry0, pos, at);
-    unroll<LOADS>([&](auto p) { load_piece(lane, t0, 0, p); });
-    if constexpr (!ONE) unroll<LOADS>([&](auto p) { load_piece(lane, t0 + 1, 1, p); });
+    if constexpr (ONE) {
+      const int entry0 = fetch(lane, t0);
+      entry = fetch(lane, t0 + 1);
+      page = place(lane, t0, entry0, pos, at);
+      unroll<LOADS>([&](auto p) { load_piece(lane, t0, 0, p); });
+    } else {
+      place8(t0, *fetch8(t0));
+      row_of = locate(pos, *page8());
+      at_of = at;
+      place8(t0 + 8, *fetch8(t0 + 8));
+      // as after a step of tile 0
+      if (!code_wave) load_lds4(fetch8(t0 + 16), (uint32_t)(uintptr_t)LDS(int, s_entry) + 256 * w4);
+      if (!code_wave) load_lds4(page8(), (uint32_t)(uintptr_t)LDS(int, s_page) + 256 * w4);
+      for (int i = 0; i < NS; ++i) {
+        rows_of(lane, i);
+        load_rows(lane, i);
+      }
+    }
   }
   // the query is in registers before the loop (its waits would fall inside it)
-  if (scoring) {
 #pragma unroll
-    for (int k = 0; k < QK; ++k) asm volatile("s_waitcnt vmcnt(0)" : "+v"(q[k]));
-  }
+  for (int k = 0; k < QK + QR; ++k) asm volatile("s_waitcnt vmcnt(0)" : "+v"(q[k]));
+  // RG = 8: every load is done, the entry and the page too (named here, so that the
+  // compiler waits for them nowhere else), and all waves are here.  Written out:
+  // the waves of a workgroup may come to it by two ways.
+  const auto meet = [&] {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : "+v"(entry), "+v"(page)::"memory");
+  };
+  // RG <= 4: of the loads those that were issued AHEAD or more iterations ago are
+  // done.  Each iteration since has issued at least 2 of them, and a store where
+  // the wave keeps scores.
+  const bool stores = s2 && w * (64 / LPR) < rows;
+  const auto meet_ahead = [&] {
+    if (stores) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * (AHEAD - 1)) : "memory");
+    else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * (AHEAD - 1)) : "memory");
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  };
   if (count > 0) {
-    asm volatile("s_waitcnt vmcnt(0)" : "+v"(entry), "+v"(page)::"memory");
-    __syncthreads();
-    if constexpr (ONE) unroll<LOADS>([&](auto p) { load_piece(lane, t0 + 1, 1, p); });
-    const bool now = ONE ? w < 4 : scoring;
-    if (now) {
-      score(lane, 0, [](auto, auto) {});
-      finish_scores(lane, t0, 0);
+    meet();
+    if constexpr (ONE) {
+      unroll<LOADS>([&](auto p) { load_piece(lane, t0 + 1, 1, p); });
+      if (w < 4) {
+        score(lane, 0);
+        finish_scores(lane, t0, 0);
+        unroll<WEIGHS>([&](auto p) { weigh_piece(lane, 0, p); });
+      }
+    } else {
+      read_score(lane, 0);
+      score_part(lane, 0);
+      meet();
+      read_score(lane, 1);
+      read_part(tid, 0, 0);
+      score_part(lane, 1);
+      weigh_part(tid, t0, 0);
+      keep_scores(tid, t0);
     }
-    if constexpr (!ONE) __syncthreads();
-    if (now) unroll<WEIGHS>([&](auto p) { weigh_piece(lane, 0, p); });
-    if constexpr (ONE) unroll<WIDENS>([&](auto p) { widen_piece(lane, 0, 0, p); });
+    unroll<WIDENS>([&](auto p) { widen_piece(lane, 0, 0, p); });
   }
-  // Iteration i: tile i + 2 is loaded, i + 1 scored, i put out (past the last
-  // tile masked ones, of row 0).
+  // Iteration i puts out tile i (past the last tile masked ones, of row 0).
   int slot = 0;  // of tile i's codes
   for (int i = 0; i < count; ++i) {
-    int ln = lane;  // addresses are made anew for every tile rather than kept in registers
-    asm volatile("" : "+v"(ln));
-    // every load is done, the entry and the page too (named here, so that the
-    // compiler waits for them nowhere else), and all waves are here.  Written out:
-    // the waves of a workgroup may come to it by two ways (RG = 8).
-    const auto meet = [&] {
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : "+v"(entry), "+v"(page)::"memory");
-    };
+    int ln = lane;
+    if constexpr (RG >= 4) asm volatile("" : "+v"(ln));  // no registers are left to keep addresses in: made anew for every tile
     const int next = slot + 1 == NS ? 0 : slot + 1, after_next = next + 1 == NS ? 0 : next + 1;  // of i + 1, i + 2
-    const auto load = [&](auto p) { load_piece(ln, t0 + i + 2, after_next, p); };
     if constexpr (ONE) {
-      // waves 0 .. 3 meet the others before they score tile i + 1, waves 4 .. 7
-      // after they scored tile i
+      // tile i + 2 is loaded, i + 1 scored; waves 0 .. 3 meet the others before they
+      // score tile i + 1, waves 4 .. 7 after they scored tile i
       const bool early = w < 4;
       const int st = early ? i + 1 : i, ss = early ? next : slot;
       if (early) meet();
-      score(ln, ss, [](auto, auto) {});
+      score(ln, ss);
       finish_scores(ln, t0 + st, ss);
       unroll<WEIGHS>([&](auto p) { weigh_piece(ln, st & 1, p); });
       if (!early) meet();
       output(ln, i & 1, i & 1, [&](auto step, auto steps) {
         pieces_after<steps, LOADS + WIDENS, step>([&](auto p) {
-          if constexpr (p < LOADS) load(p);
+          if constexpr (p < LOADS) load_piece(ln, t0 + i + 2, after_next, p);
           else widen_piece(ln, next, (i + 1) & 1, std::integral_constant<int, p - LOADS>{});
         });
       });
     } else {
-      meet();
-      unroll<LOADS>(load);
-      unroll<WIDENS>([&](auto p) { widen_piece(ln, slot, 0, p); });
-      if (scoring) {
-        score(ln, next, [](auto, auto) {});
-        finish_scores(ln, t0 + i + 1, next);
-      }
-      __syncthreads();
-      if (scoring) {
-        output(ln, 0, i & 1, [&](auto step, auto steps) {
-          pieces_after<steps, WEIGHS, step>([&](auto p) { weigh_piece(ln, (i + 1) & 1, p); });
-        });
-      } else {
-        output(ln, 0, i & 1, [](auto, auto) {});
-      }
+      // tile i + 2 + AHEAD is loaded, i + 2 multiplied, i + 1 weighed and widened
+      meet_ahead();
+      next_rows(ln, i + NS);
+      read_part(64 * w + ln, next, (i + 1) & 1);
+      read_score(ln, after_next);
+      read_codes(ln, next);
+      if constexpr (RG < 4) read_output(ln, i & 1, i & 1);
+      __builtin_amdgcn_sched_barrier(0);
+      weigh_part(64 * w + ln, t0 + i + 1, (i + 1) & 1);
+      score_part(ln, i & 1);
+      widen_codes(ln, (i + 1) & 1);
+      if constexpr (RG == 4) read_output(ln, i & 1, i & 1);  // no registers for it before
+      add_output();
+      keep_scores(64 * w + ln, t0 + i + 1);
+      load_rows(ln, slot);
     }
     slot = next;
   }
@@ -631,22 +874,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
 
   // the rows' statistics
   __syncthreads();
-  const int g = lane >> 4;
-  if (scoring) {
+  if constexpr (ONE) {
     l = groups_sum(l);
-    if (g == 0) {
-      s_sum[ONE ? 0 : kt][row0 + lane] = l;
-      s_max[0][row0 + lane] = m;  // the waves of the rows hold the same
+    if (lane < 16) {
+      s_sum[row0 + lane] = l;
+      s_max[row0 + lane] = m;
+    }
+  } else {
+    l = row_reduce<LPR>(l, [](float x, float y) { return x + y; });
+    if (tid % LPR == 0) {
+      s_sum[tid / LPR] = l;
+      s_max[tid / LPR] = m;
     }
   }
   __syncthreads();
-  auto total_of = [&](int row) {
-    float sum = s_sum[0][row];
-    if constexpr (KG > 1) sum += s_sum[1][row];
-    return sum;
-  };
   if (splits > 1) {
-    if (tid < ROWS) wk.part_ml[(int64_t)part * ROWS + tid] = {s_max[0][tid], total_of(tid)};
+    if (tid < ROWS) wk.part_ml[(int64_t)part * ROWS + tid] = {s_max[tid], s_sum[tid]};
     // the registers as they lie: the joining kernel has the same lanes
     float4* po = wk.part_o + (int64_t)part * O::QUADS * (64 * kWaves) + tid;
     if constexpr (RG == 1) {
@@ -666,7 +909,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
   }
   const int64_t orow = ((int64_t)t.row0[b] + i_first) * a.heads + first;
   if (tid < rows) {
-    const float sum = total_of(tid), top = s_max[0][tid];
+    const float sum = s_sum[tid], top = s_max[tid];
     if (a.lse) a.lse[orow + tid] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
     if (sm.stat) sm.stat[orow + tid] = {top == -INFINITY ? 0.f : top, sum == 0.f ? 0.f : 1.f / sum};
   }
@@ -677,7 +920,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
 #pragma unroll
   for (int y = 0; y < O::YT; ++y) {
     const int row = O::row(w, lane, y), at_row = RG == 8 ? (row & 31) + 32 * (w >> 2) : row - 32 * y;
-    const float sum = total_of(row), inv = sum == 0.f ? 0.f : 1.f / sum;
+    const float sum = s_sum[row], inv = sum == 0.f ? 0.f : 1.f / sum;
     auto put = [&](int value, float a0, float a1, float a2, float a3) {
       const v4bf v = {(__bf16)(a0 * inv), (__bf16)(a1 * inv), (__bf16)(a2 * inv), (__bf16)(a3 * inv)};
       *reinterpret_cast<v4bf*>(s_val + at_row * 2 * kLatent + (((value >> 3) ^ (at_row & 63)) << 4) + (value & 4) * 2) = v;
