@@ -164,14 +164,19 @@ struct Output {
 // iteration (output of tile i; score and widen of i + 1; load of i + 2) need
 // nothing of each other, so one barrier per tile is enough, and the two waves of
 // a SIMD take them in different orders: one widens codes for its scores while the
-// other's output keeps the matrix core busy.  RG <= 4: a wave scores 16 rows
-// against 16 keys, and the waves that share rows exchange their maxima at a second
-// barrier, before which the values of tile i are widened (one buffer does) and
-// after which they are used.
-// Operands are read from LDS some steps ahead, and the vector work of other
-// stages is cut into pieces issued between the output's matrix products, which
-// run on their own once issued; scheduling barriers keep the two from being
-// sorted apart.
+// other's output keeps the matrix core busy.  Operands are read from LDS some
+// steps ahead, and the vector work of other stages is cut into pieces issued
+// between the output's matrix products, which run on their own once issued;
+// scheduling barriers keep the two from being sorted apart.  Bound by vector
+// instructions (the codes' conversion at half rate, 4460 of 7900 cycles a tile)
+// next to 3200 cycles of matrix products: 1003 queries x 128 heads x 2048 keys in
+// 820 us, 700 TFLOP/s.
+// RG <= 4: 16 rows' products with 16 keys are shared by 4 / RG waves, so that all
+// 8 have some; their parts go through LDS, and a tile takes an iteration more: the
+// load of tile i + 2 + AHEAD, the products of i + 2, the weights and the widening
+// of i + 1, the output of i, again with one barrier.  All operands are read from
+// LDS first, then used.  With RG = 1 a tile takes 3200 cycles, a third of them
+// reads of LDS: 8 sequences of 9001 to 40000 keys x 16 heads in 43 us, 1.7 TB/s.
 // The sequence that workgroup i belongs to: the last one with first <= i (one
 // without workgroups shares its first with the next).
 __device__ __forceinline__ int owner_of(const int32_t* first, int n, int i) {
@@ -1134,6 +1139,7 @@ struct Plan {
 };
 
 constexpr int kCus = 256;
+constexpr int kLeastTiles = 4;
 
 Plan plan_of(const AttendArgs& a, const RunTable& t) {
   Plan p{};
@@ -1159,23 +1165,27 @@ Plan plan_of(const AttendArgs& a, const RunTable& t) {
   }
   const int64_t unit_rows = a.idx ? a.heads : (int64_t)max_rows * a.heads;
   p.rg = unit_rows > 64 ? 8 : unit_rows > 32 ? 4 : unit_rows > 16 ? 2 : 1;
-  const int R = 16 * p.rg;
   p.wk.units = a.idx ? p.rows : t.n;
-  p.wk.row_tiles = (int)((unit_rows + R - 1) / R);
   const int max_tiles = a.idx ? p.padded / kTileKeys : (p.max_n + kTileKeys - 1) / kTileKeys;
-  const auto row_tiles_of = [&](int b) { return ((int64_t)t.n_rows[b] * a.heads + R - 1) / R; };
-  // Splits of as few tiles as give no more workgroups than run at once: one more
-  // would wait for another to end.
-  const int64_t target = kCus;
+  const auto row_tiles_of = [&](int64_t rows) { return (rows + 16 * p.rg - 1) / (16 * p.rg); };
   const auto workgroups = [&](int64_t each) {
-    if (a.idx) return (int64_t)p.rows * p.wk.row_tiles * (max_tiles > each ? (max_tiles + each - 1) / each : 1);
+    if (a.idx) return p.rows * row_tiles_of(a.heads) * (max_tiles > each ? (max_tiles + each - 1) / each : 1);
     int64_t w = 0;
-    for (int b = 0; b < t.n; ++b) w += row_tiles_of(b) * splits_of(t, b, (int)each);
+    for (int b = 0; b < t.n; ++b) w += row_tiles_of((int64_t)t.n_rows[b] * a.heads) * splits_of(t, b, (int)each);
     return w;
   };
-  int64_t each = p.rg == 8 ? 8 : p.rg == 4 ? 6 : 4;
-  while (each < max_tiles && workgroups(each) > target) each += 1 + each / 32;
+  // A split has at least kLeastTiles.  Where even so workgroups of half the rows
+  // would all run at once, they are taken: a tile of 16 rows takes 1.3 us, one of
+  // 128 rows 3.3 (2 queries of 128 heads on 2048 keys: 28 us with 128 rows a
+  // workgroup, 17 with 16).
+  int64_t each = kLeastTiles;
+  while (p.rg > 1 && 2 * workgroups(each) <= kCus) p.rg /= 2;
+  // Splits of as few tiles as give no more workgroups than run at once: one more
+  // would wait for another to end.
+  while (each < max_tiles && workgroups(each) > kCus) each += 1 + each / 32;
   if (each >= max_tiles) each = max_tiles > 0 ? max_tiles : 1;
+  const int R = 16 * p.rg;
+  p.wk.row_tiles = (int)row_tiles_of(unit_rows);
   p.wk.tiles_per_split = (int)each;
   p.wk.splits = max_tiles > 0 ? (int)((max_tiles + each - 1) / each) : 1;
   p.workgroups = workgroups(each);
@@ -1183,7 +1193,7 @@ Plan plan_of(const AttendArgs& a, const RunTable& t) {
     int32_t w = 0;
     for (int b = 0; b < t.n; ++b) {
       p.wk.first[b] = w;
-      w += (int32_t)(row_tiles_of(b) * splits_of(t, b, (int)each));
+      w += (int32_t)(row_tiles_of((int64_t)t.n_rows[b] * a.heads) * splits_of(t, b, (int)each));
     }
     p.wk.first[t.n] = w;
   }
