@@ -248,9 +248,14 @@ def _ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
+def _current_stream(device=None) -> int:
+    """The current stream's handle, without a torch stream object (3 us a call)."""
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if device is None else device)
+
+
 def _stream(stream):
     if stream is None:
-        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        return ctypes.c_void_p(_current_stream())
     if isinstance(stream, torch.cuda.Stream):
         return ctypes.c_void_p(stream.cuda_stream)
     return ctypes.c_void_p(int(stream))
@@ -290,12 +295,12 @@ def workspace(nbytes: int, device, stream=None) -> torch.Tensor:
     is allocated with that stream current, so torch's caching allocator orders
     its reuse after the work already queued on the stream when it is replaced."""
     dev = torch.device(device)
-    s = _torch_stream(stream, dev)
-    key = (dev.type, dev.index, s.cuda_stream)
+    handle = _current_stream(dev.index) if stream is None else _stream(stream).value or 0
+    key = (dev.type, dev.index, handle)
     buf = _WS.get(key)
     if buf is None or buf.numel() < nbytes:
         _WS.pop(key, None)
-        with torch.cuda.stream(s):
+        with torch.cuda.stream(_torch_stream(stream, dev)):
             buf = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=dev)
         _WS[key] = buf
     return buf
@@ -760,12 +765,9 @@ def pivot_cache4_attend(q, cache, q_pos0, n_k, scale, idx=None, cu_q=None, acc=N
     _check_batch(cache._keep[3], batch)
     a = pivot_attend_args()
     a.heads, a.batch, a.n_q = heads, batch, 0 if cu_q is not None else q.shape[1]
-    keep = [_host_ints(q_pos0), _host_ints(n_k)]
-    PI = ctypes.POINTER(ctypes.c_int32)
-    a.q_pos0, a.n_k = ctypes.cast(keep[0], PI), ctypes.cast(keep[1], PI)
+    a.q_pos0, a.n_k = _host_ints(q_pos0), _host_ints(n_k)
     if cu_q is not None:
-        keep.append(_host_ints(cu_q))
-        a.cu_q = ctypes.cast(keep[2], PI)
+        a.cu_q = _host_ints(cu_q)
     a.q, a.q_row_stride, a.q_head_stride = q.data_ptr(), row_stride, head_stride
     a.cache = cache
     if idx is not None:
@@ -810,8 +812,7 @@ def pivot_evict(acc, n_k, keep, arrays, from_map, to_map, sink=0, recent=0, out_
     out_acc = (torch.empty((batch, keep), dtype=torch.float32, device=acc.device) if out_acc is None
                else _expect(out_acc, torch.float32, (batch, keep), "out_acc"))
     a = pivot_evict_args()
-    nk = _host_ints(n_k)
-    a.batch, a.n_k = batch, ctypes.cast(nk, ctypes.POINTER(ctypes.c_int32))
+    a.batch, a.n_k = batch, _host_ints(n_k)
     a.acc, a.acc_stride = acc.data_ptr(), acc.shape[1]
     a.keep, a.sink, a.recent = keep, sink, recent
     a.out_keep, a.out_acc = out_keep.data_ptr(), out_acc.data_ptr()
