@@ -543,3 +543,22 @@ def test_evict_without_arrays():
     a = acc.cpu().numpy()
     for b, n in enumerate((1000, 900)):
         assert host(kept)[b].tolist() == ref.evict(a[b], n, 100, 1, 1)
+
+
+@pytest.mark.parametrize("lens,keep,sink,recent", [
+    ([8193, 8192, 100], 500, 1, 1), ([12288, 12289], 9000, 5000, 4000), ([300000, 262145, 5], 4097, 4, 64),
+    ([40000], 30000, 9000, 12000), ([40000], 12345, 12000, 300), ([20000, 16385], 20000, 0, 0),
+])
+def test_evict_long_sequences(lens, keep, sink, recent):
+    rng = np.random.default_rng(keep)
+    acc = np.floor(4 * rng.standard_normal((len(lens), max(lens) + 3))).astype(np.float32)  # ties over the whole length
+    acc[:, rng.integers(0, max(lens), 50)] = np.nan
+    acc[:, rng.integers(0, max(lens), 50)] = np.inf
+    acc[0, : lens[0] // 3] = np.frombuffer(b"\xff" * 4, dtype=np.float32)[0]  # the lowest key there is
+    kept, out_acc = pv.pivot_evict(dev(acc), lens, keep, [], None, None, sink=sink, recent=recent)
+    kept, out_acc = host(kept), host(out_acc)
+    for b, n in enumerate(lens):
+        say("evict long", lens, keep, b)
+        want = ref.evict(acc[b], n, keep, sink, recent)
+        assert kept[b, : len(want)].tolist() == want and (kept[b, len(want):] == -1).all()
+        assert np.array_equal(out_acc[b, : len(want)].view(np.int32), acc[b, want].view(np.int32))
