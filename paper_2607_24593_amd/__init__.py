@@ -9,6 +9,7 @@ otherwise.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 
@@ -608,7 +609,7 @@ def _host_ints(v, batch=None):
     """A ctypes int32 array of host integers (one repeated for the batch, or a sequence)."""
     if isinstance(v, int):
         v = [v] * batch
-    return (ctypes.c_int32 * len(v))(*v)
+    return (ctypes.c_int32 * len(v)).from_buffer(array.array("i", v)) if len(v) else (ctypes.c_int32 * 0)()
 
 
 def _rows_of(t, width, what):
@@ -631,7 +632,7 @@ def _float_code(t) -> int:
 
 
 def _expect(t, dtype, shape, what):
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
     return t
 
@@ -650,14 +651,14 @@ def pivot_rmsnorm_fp8(x, weight, eps=1e-6, residual=None, group=0, residual_out=
         if residual.dtype != x.dtype or residual.shape != x.shape:
             raise ValueError("residual must have x's type and shape")
         ld_r = _rows_of(residual, dim, "residual")
-        residual_out = (torch.empty(x.shape, dtype=x.dtype, device=x.device) if residual_out is None
+        residual_out = (torch.empty_like(x, memory_format=torch.contiguous_format) if residual_out is None
                         else _expect(residual_out, x.dtype, x.shape, "residual_out"))
     elif residual_out is not None:
         raise ValueError("residual_out needs a residual")
     _expect(weight, x.dtype, (dim,), "weight")
-    rows = x.numel() // max(dim, 1)
+    rows = x.numel() // dim if dim else 0
     shape = tuple(x.shape[:-1]) + (-(-dim // group) if group else 1,)
-    codes = (torch.empty(x.shape, dtype=torch.uint8, device=x.device) if codes is None
+    codes = (torch.empty_like(x, dtype=torch.uint8, memory_format=torch.contiguous_format) if codes is None
              else _expect(codes, torch.uint8, x.shape, "codes"))
     scale = (torch.empty(shape, dtype=torch.float32, device=x.device) if scale is None
              else _expect(scale, torch.float32, shape, "scale"))
