@@ -481,10 +481,10 @@ pivot_status pivot_cache4_read(const pivot_cache4* c, int32_t batch, int32_t n, 
  * Row i of sequence b is at position q_pos0[b] + i; q_pos0[b] + n_q <= n_k[b].
  * A row with nothing to attend to, or only scores of -infinity, has out = 0 and
  * lse = -infinity and adds nothing.  A row that attends to a token with a NaN,
- * or whose query holds an infinity or a NaN, is NaN; tokens it does not attend
- * to never reach it.  Scores and sums are fp32 (the products are exact), the
- * weights are rounded to bf16 for the product with the values.  The same call
- * gives the same bits.
+ * or whose query holds one, is NaN; tokens it does not attend to never reach it.
+ * Scores and sums are fp32 (the products are exact), the weights are rounded to
+ * 16 bits (two bf16) for the product with the values.  The same call gives the
+ * same bits.
  * Workspace: pivot_cache4_attend_workspace_size(a) bytes (device, 256-byte
  * aligned; 0 for invalid shapes or none needed; reads the host arrays only).
  */
@@ -558,10 +558,10 @@ pivot_status pivot_evict(const pivot_evict_args* a);
 
 /*
  * Kernel timing.  Between pivot_profile_begin() and pivot_profile_end() every
- * kernel that the index calls and their stages launch is bracketed by two HIP events recorded on the
- * launch's stream.  pivot_profile_end() waits for those events and returns,
- * per kernel kind, the number of launches and the summed event-to-event time;
- * it then stops recording.  Event objects are host-side resources created on
+ * kernel that the index calls and their stages launch is bracketed by two HIP
+ * events recorded on the launch's stream.  pivot_profile_end() waits for those
+ * events and returns, per kernel kind, the number of launches and the summed
+ * event-to-event time; it then stops recording.  Event objects are host-side resources created on
  * first use; no device memory is allocated.  One profile at a time per process.
  * pivot_profile_begin_kinds(mask) brackets only the kinds whose bit
  * (1 << PIVOT_KERNEL_*) is set, so that the events of other kernels add no
