@@ -8,6 +8,7 @@
 // lse = -infinity and adds nothing to acc.
 //
 // Scores are kept in base 2 (z log2 e), statistics and sums in fp32.
+#include <algorithm>
 #include <utility>
 
 #include "cache4.h"
@@ -781,10 +782,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
       page = place(lane, t0, entry0, pos, at);
       unroll<LOADS>([&](auto p) { load_piece(lane, t0, 0, p); });
     } else {
-      place8(t0, *fetch8(t0));
+      const int entry0 = *fetch8(t0), entry8 = *fetch8(t0 + 8);
+      place8(t0, entry0);
       row_of = locate(pos, *page8());
       at_of = at;
-      place8(t0 + 8, *fetch8(t0 + 8));
+      place8(t0 + 8, entry8);
       // as after a step of tile 0
       if (!code_wave) load_lds4(fetch8(t0 + 16), (uint32_t)(uintptr_t)LDS(int, s_entry) + 256 * w4);
       if (!code_wave) load_lds4(page8(), (uint32_t)(uintptr_t)LDS(int, s_page) + 256 * w4);
@@ -1098,35 +1100,85 @@ __global__ __launch_bounds__(256) void slot_weights_kernel(AttendArgs a, ScoreMa
 }
 
 // acc += the slots' weights: a workgroup owns kRange positions of a sequence
-// and adds the sequence's rows one after the other (a position comes at most
-// once in a set, so every sum has one order).
-constexpr int kRange = 4096;
-__global__ __launch_bounds__(256) void slot_add_kernel(AttendArgs a, RunTable t, const float* __restrict__ slots,
-                                                       int padded) {
+// and adds rows one after the other (a position comes at most once in a set, so
+// every sum has one order).  A step is 2048 entries of a row, 2 a thread; the
+// entries of the next kAhead steps are loaded while these are added.  Many rows are
+// cut into `groups` whose sums are added up in order afterwards: one group of 1003
+// rows x 2048 takes 1160 us, 62 groups 46 with their addition.  32 sequences of 2 rows x 2048 take 14.
+constexpr int kRange = 8192;
+constexpr int kAddThreads = 1024;
+constexpr int kAhead = 4;
+__global__ __launch_bounds__(kAddThreads) void slot_add_kernel(AttendArgs a, RunTable t, const float* __restrict__ slots,
+                                                               int padded, int groups, float* parts) {
   __shared__ float sum[kRange];
-  const int b = blockIdx.y, tid = threadIdx.x;
-  const int lo = blockIdx.x * kRange, n = t.pos0[b] + t.n_rows[b];
+  const int b = blockIdx.y, tid = threadIdx.x, group = blockIdx.x % groups;
+  const int lo = blockIdx.x / groups * kRange, n = t.pos0[b] + t.n_rows[b];
   if (t.n_rows[b] == 0 || lo >= n) return;
-  for (int j = tid; j < kRange; j += 256) sum[j] = 0.f;
-  __syncthreads();
-  for (int i = 0; i < t.n_rows[b]; ++i) {
-    const int64_t r = t.row0[b] + i;
-    const int pos = t.pos0[b] + i;
-    for (int k = tid; k < a.topk; k += 256) {
-      const int key = a.idx[r * a.topk + k];
-      if (key <= pos && (uint32_t)(key - lo) < (uint32_t)kRange && key >= 0)
-        atomicAdd(&sum[key - lo], slots[r * padded + k]);
+  const int each = (t.n_rows[b] + groups - 1) / groups, row0 = group * each;
+  const int rows = max(0, min(each, t.n_rows[b] - row0));
+  const int passes = (a.topk + 2 * kAddThreads - 1) / (2 * kAddThreads), steps = rows * passes;
+  int key[2][kAhead][2];
+  float w[2][kAhead][2];
+  auto load = [&](int first, int (&keys)[kAhead][2], float (&ws)[kAhead][2]) {
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int i = (first + j) / passes, base = (first + j - i * passes) * 2 * kAddThreads;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int k = base + e * kAddThreads + tid;
+        const int64_t r = t.row0[b] + row0 + i;
+        const bool ok = first + j < steps && k < a.topk;
+        keys[j][e] = ok ? a.idx[r * a.topk + k] : -1;
+        ws[j][e] = ok ? slots[r * padded + k] : 0.f;
+      }
     }
-    __syncthreads();
+  };
+  auto add = [&](int first, const int (&keys)[kAhead][2], const float (&ws)[kAhead][2]) {
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (first + j >= steps) return;
+      const int i = (first + j) / passes, pos = t.pos0[b] + row0 + i;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int at = keys[j][e];
+        if (at >= 0 && at <= pos && (uint32_t)(at - lo) < (uint32_t)kRange) atomicAdd(&sum[at - lo], ws[j][e]);
+      }
+      __syncthreads();
+    }
+  };
+  load(0, key[0], w[0]);
+  for (int j = tid; j < kRange; j += kAddThreads) sum[j] = 0.f;
+  __syncthreads();
+  for (int first = 0; first < steps; first += 2 * kAhead) {
+    load(first + kAhead, key[1], w[1]);
+    add(first, key[0], w[0]);
+    load(first + 2 * kAhead, key[0], w[0]);
+    add(first + kAhead, key[1], w[1]);
   }
-  for (int j = tid; j < kRange && lo + j < n; j += 256)
+  if (groups > 1) {
+    float* part = parts + ((int64_t)b * groups + group) * (gridDim.x / groups * kRange) + lo;
+    for (int j = tid; j < kRange; j += kAddThreads) part[j] = sum[j];
+    return;
+  }
+  for (int j = tid; j < kRange && lo + j < n; j += kAddThreads)
     if (sum[j] != 0.f) a.acc[(int64_t)b * a.acc_stride + lo + j] += sum[j];
+}
+
+__global__ __launch_bounds__(256) void group_add_kernel(AttendArgs a, RunTable t, int groups, const float* parts,
+                                                        int64_t stride) {
+  const int b = blockIdx.y, at = blockIdx.x * 256 + threadIdx.x;
+  if (t.n_rows[b] == 0 || at >= t.pos0[b] + t.n_rows[b]) return;
+  float sum = 0.f;
+#pragma unroll 8
+  for (int g = 0; g < groups; ++g) sum += parts[((int64_t)b * groups + g) * stride + at];
+  if (sum != 0.f) a.acc[(int64_t)b * a.acc_stride + at] += sum;
 }
 
 size_t round256(size_t x) { return (x + 255) / 256 * 256; }
 
 struct Plan {
-  size_t scores, stats, slots, part_o, part_ml;
+  size_t scores, stats, slots, sums, part_o, part_ml;
+  int ranges, groups;  // of the slots' sums
   int padded;
   int64_t base[kMaxSeq];
   int rows, max_n;
@@ -1134,7 +1186,7 @@ struct Plan {
   int rg;       // row groups of 16 per workgroup
   Work wk;
   size_t bytes() const {
-    return round256(scores) + round256(stats) + round256(slots) + round256(part_o) + round256(part_ml);
+    return round256(scores) + round256(stats) + round256(slots) + round256(sums) + round256(part_o) + round256(part_ml);
   }
 };
 
@@ -1162,6 +1214,10 @@ Plan plan_of(const AttendArgs& a, const RunTable& t) {
     p.scores = (size_t)words * 4;
     p.stats = (size_t)p.rows * a.heads * sizeof(float2);
     p.slots = a.idx ? (size_t)p.rows * p.padded * 4 : 0;
+    // groups of 16 rows or more, as far as workgroups of two a CU are not many enough
+    p.ranges = (p.max_n + kRange - 1) / kRange;
+    p.groups = std::max(1, std::min(max_rows / 16, 2 * kCus / (t.n * p.ranges)));
+    p.sums = a.idx && p.groups > 1 ? (size_t)t.n * p.groups * p.ranges * kRange * 4 : 0;
   }
   const int64_t unit_rows = a.idx ? a.heads : (int64_t)max_rows * a.heads;
   p.rg = unit_rows > 64 ? 8 : unit_rows > 32 ? 4 : unit_rows > 16 ? 2 : 1;
@@ -1232,7 +1288,8 @@ hipError_t launch_attend(const AttendArgs& a, const RunTable& t, hipStream_t str
     for (int b = 0; b < t.n; ++b) sm.base[b] = p.base[b];
   }
   float* slots = (float*)(ws + round256(p.scores) + round256(p.stats));
-  uint8_t* parts = ws + round256(p.scores) + round256(p.stats) + round256(p.slots);
+  float* sums = (float*)((uint8_t*)slots + round256(p.slots));
+  uint8_t* parts = (uint8_t*)sums + round256(p.sums);
   p.wk.part_o = (float4*)parts;
   p.wk.part_ml = (float2*)(parts + round256(p.part_o));
   hipError_t e = p.rg == 8   ? launch_rows<8>(a, t, sm, p.wk, (unsigned)p.workgroups, stream)
@@ -1249,8 +1306,12 @@ hipError_t launch_attend(const AttendArgs& a, const RunTable& t, hipStream_t str
                      a, sm, slots, p.padded);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(slot_add_kernel, dim3((unsigned)((p.max_n + kRange - 1) / kRange), (unsigned)t.n), dim3(256), 0,
-                     stream, a, t, slots, p.padded);
+  hipLaunchKernelGGL(slot_add_kernel, dim3((unsigned)(p.ranges * p.groups), (unsigned)t.n), dim3(kAddThreads), 0, stream,
+                     a, t, slots, p.padded, p.groups, sums);
+  e = hipGetLastError();
+  if (e != hipSuccess || p.groups == 1) return e;
+  hipLaunchKernelGGL(group_add_kernel, dim3((unsigned)((p.max_n + 255) / 256), (unsigned)t.n), dim3(256), 0, stream, a, t,
+                     p.groups, sums, (int64_t)p.ranges * kRange);
   return hipGetLastError();
 }
 

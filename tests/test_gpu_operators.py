@@ -562,3 +562,42 @@ def test_evict_long_sequences(lens, keep, sink, recent):
         want = ref.evict(acc[b], n, keep, sink, recent)
         assert kept[b, : len(want)].tolist() == want and (kept[b, len(want):] == -1).all()
         assert np.array_equal(out_acc[b, : len(want)].view(np.int32), acc[b, want].view(np.int32))
+
+
+@pytest.mark.parametrize("topk", [130, 2100])
+def test_attend_weights_of_many_rows(topk):
+    """Weights of many rows on the same tokens, one long run beside a short one,
+    added in an order that does not change."""
+    rng = np.random.default_rng(topk)
+    lens, pos0, cu, heads = [9000, 40], [8880, 33], [0, 120, 127], 2
+    pool = Pool(lens, 0, rng)
+    n_rows = [120, 7]
+    q = _queries((127, heads), rng)
+    hot = rng.permutation(8880)[:topk + 20]
+    idx = _sets(rng, pos0, n_rows, topk, lambda r, pos: rng.permutation(hot if r < 120 else pos + 1)[:topk])
+    acc0 = rng.random((2, 9001)).astype(np.float32)
+    qd = torch.from_numpy(q).bfloat16().cuda().view(127, heads, 576)
+    got = []
+    for _ in range(2):
+        acc = dev(acc0)
+        say("attend weights of many rows", topk)
+        pv.pivot_cache4_attend(qd, pool.cache, pos0, lens, 0.04, cu_q=cu, idx=dev(idx), acc=acc)
+        got.append(host(acc))
+    assert np.array_equal(got[0], got[1])
+    r = 0
+    for b, n in enumerate(n_rows):
+        size = pos0[b] + n
+        latent, rope = pool.tokens(b, size)
+        total, slack = np.zeros(size), np.zeros(size)
+        for i in range(n):
+            allowed = np.zeros(size, dtype=bool)
+            s = idx[r]
+            allowed[s[(s >= 0) & (s <= pos0[b] + i)]] = True
+            _, _, w, bound, _ = ref.attend_rows(q[r], latent, rope, 0.04, allowed)
+            total += w
+            slack += (2.0 ** -17 * bound.max() + 2.0 ** -19) * w
+            r += 1
+        # at most rows + heads + 8 additions in fp32, each rounding once
+        tol = slack + (n + heads + 8) * 2.0 ** -24 * (total + acc0[b, :size]) + 1e-30
+        assert np.all(np.abs(got[0][b, :size].astype(np.float64) - total - acc0[b, :size]) <= tol)
+        assert np.array_equal(got[0][b, size:], acc0[b, size:])
