@@ -608,7 +608,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
     }
   };
   // the weights of KPT scores of one row to s_w[wslot]
-  auto weigh_part = [&](int td, int tile, int wslot) {
+  auto weigh_part = [&](int td, int wslot) {
     const int row = td / LPR, k0 = td % LPR * KPT;
     float z[KPT], e[KPT], top = -INFINITY;
 #pragma unroll
@@ -766,7 +766,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
       unroll<2 * O::YT>([&](auto u) {  // all rows with the high parts, then with the low ones
         constexpr int part = u / O::YT, y = u % O::YT;
         o[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, wt[k][part][y], o[x][y], 0, 0, 0);
-        if constexpr (u == 0 && i + 1 < STEPS) read_value(std::integral_constant<int, i + 1>{});
+        if constexpr (u == 0 && i + 1 < STEPS) read_value(std::integral_constant<int, (i + 1) % STEPS>{});
         if constexpr (i + 1 == O::XT) read_weight(1, part, y);  // in place of the one that was used last here
         after(std::integral_constant<int, 2 * O::YT * i + u>{}, std::integral_constant<int, 2 * O::YT * STEPS>{});
         __builtin_amdgcn_sched_barrier(0);
@@ -830,7 +830,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
       read_score(lane, 1);
       read_part(tid, 0, 0);
       score_part(lane, 1);
-      weigh_part(tid, t0, 0);
+      weigh_part(tid, 0);
       keep_scores(tid, t0);
     }
     unroll<WIDENS>([&](auto p) { widen_piece(lane, 0, 0, p); });
@@ -866,7 +866,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
       read_codes(ln, next);
       if constexpr (RG < 4) read_output(ln, i & 1, i & 1);
       __builtin_amdgcn_sched_barrier(0);
-      weigh_part(64 * w + ln, t0 + i + 1, (i + 1) & 1);
+      weigh_part(64 * w + ln, (i + 1) & 1);
       score_part(ln, i & 1);
       widen_codes(ln, (i + 1) & 1);
       if constexpr (RG == 4) read_output(ln, i & 1, i & 1);  // no registers for it before
