@@ -383,8 +383,8 @@ pivot_status pivot_encode_e4m3(const float* x, uint8_t* out, int64_t n, void* st
  * rows r < n_rows of `dim` values (1 .. 32768):
  *   h = x + residual                         (fp32; residual NULL: h = x)
  *   y = h * rsqrt(mean(h^2) + eps) * weight   (fp32, of the unrounded h)
- *   per group of the row: scale = max|y| / 448 (1 if that is 0),
- *                         codes = E4M3FN of y / scale, nearest even
+ *   per group of the row: scale = max|y| / 448, at least 2^-149 (1 if max|y| is 0),
+ *                         codes = E4M3FN of y / scale, nearest even, at most 448
  * dtype (x, residual, weight, residual_out): PIVOT_DT_BF16 or PIVOT_DT_FP32,
  * else PIVOT_ERR_UNSUPPORTED.
  *   x, residual   dev, rows ld_x / ld_residual values apart (>= dim)

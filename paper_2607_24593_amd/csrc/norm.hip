@@ -3,13 +3,15 @@
 //
 //   h = x + residual                        fp32 sum; stored rounded to x's type
 //   y = h * rsqrt(mean(h^2) + eps) * weight  fp32, of the unrounded h
-//   per group of the row: scale = max|y| / 448 (1 if that is 0), code = RNE(y / scale)
+//   per group of the row: scale = max|y| / 448 (1 if max|y| is 0, else at least 2^-149),
+//                         code = RNE(y / scale)
 //
 // One workgroup per row, the row held in registers: x, residual and weight are
 // read once and every output is written once, so the kernel is bound by bytes
 // (by latency for a few rows).  max|y| needs no second pass: with one scale
 // per row it is max|h w| times the rsqrt, reduced together with the sum of
-// squares; with a scale per 128 values, 16 neighbouring lanes hold a group.
+// squares (where max|h w| is no normal number the row's y are reduced instead);
+// with a scale per 128 values, 16 neighbouring lanes hold a group.
 // 8192 x 6144 fp32 values: 122 us, 5.4 TB/s, a copy's rate; 260 x 5003 bf16: 6.5;
 // one row of 4096: 2.7.
 #include "device_common.h"
@@ -83,11 +85,27 @@ __device__ __forceinline__ void store8(T* p, int e, int n, const float (&v)[kV])
   }
 }
 
-// y / s with r = 1 / s: one correction step, so the quotient is that of the
-// division up to its last bit's rounding.
-__device__ __forceinline__ float quotient(float y, float s, float r) {
-  const float q = y * r;
-  return fmaf(fmaf(-q, s, y), r, q);
+__device__ __forceinline__ float scale_of(float amax) { return amax > 0.f ? fmaxf(amax / 448.f, 0x1p-149f) : 1.f; }
+
+// y / s for y = h rstd w, with r = 1 / s: one correction step, so the quotient is
+// that of the division up to its last bit's rounding.  Below 2^-126 the reciprocal
+// may be infinite, so there the division itself is taken; such a scale is rounded
+// to few bits, and the quotient may pass 448 by half of them.
+__device__ __forceinline__ void quotients(float (&y)[kV], float s) {
+  if (s >= 0x1p-126f) {
+    const float r = 1.f / s;
+#pragma unroll
+    for (int i = 0; i < kV; ++i) {
+      const float q = y[i] * r;
+      y[i] = fmaf(fmaf(-q, s, y[i]), r, q);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kV; ++i) {
+      const float q = y[i] / s;
+      y[i] = q > 448.f ? 448.f : q < -448.f ? -448.f : q;
+    }
+  }
 }
 
 template <class T, int NT, int IT, bool GROUPS>
@@ -121,8 +139,7 @@ __global__ __launch_bounds__(NT) void norm_kernel(const T* x, int64_t ld_x, cons
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
       sq = fmaf(h[it][i], h[it][i], sq);
-      h[it][i] *= w[it][i];
-      top = fmaxf(top, fabsf(h[it][i]));
+      if constexpr (!GROUPS) top = fmaxf(top, fabsf(h[it][i] * w[it][i]));
     }
   }
   sq = wave_reduce(sq, [](float a, float b) { return a + b; });
@@ -137,11 +154,29 @@ __global__ __launch_bounds__(NT) void norm_kernel(const T* x, int64_t ld_x, cons
   const float rstd = 1.0f / sqrtf(sq / (float)dim + eps);
   uint8_t* out = codes + row * (int64_t)dim;
   const int groups = GROUPS ? (dim + kNormGroup - 1) / kNormGroup : 1;
-  float s = 1.f, r = 1.f;
+#pragma unroll
+  for (int it = 0; it < IT; ++it)
+#pragma unroll
+    for (int i = 0; i < kV; ++i) h[it][i] = h[it][i] * rstd * w[it][i];  // y
+  float s = 1.f;
   if constexpr (!GROUPS) {
-    const float amax = top * rstd;
-    s = amax > 0.f ? amax / 448.f : 1.f;
-    r = 1.f / s;
+    float amax = top * rstd;
+    if (!(top >= 0x1p-126f && top < INFINITY)) {  // the same in all threads: h w left fp32's range, y need not have
+      amax = 0.f;
+#pragma unroll
+      for (int it = 0; it < IT; ++it)
+#pragma unroll
+        for (int i = 0; i < kV; ++i) amax = fmaxf(amax, fabsf(h[it][i]));
+      amax = wave_reduce(amax, [](float a, float b) { return fmaxf(a, b); });
+      if constexpr (NW > 1) {
+        __syncthreads();
+        if ((tid & 63) == 0) part[0][tid >> 6] = amax;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < NW; ++i) amax = fmaxf(amax, part[0][i]);
+      }
+    }
+    s = scale_of(amax);
     if (tid == 0) scale[row] = s;
   }
 #pragma unroll
@@ -155,15 +190,12 @@ __global__ __launch_bounds__(NT) void norm_kernel(const T* x, int64_t ld_x, cons
       a = fmaxf(a, lane_xor2(a));
       a = fmaxf(a, lane_xor4(a));
       a = fmaxf(a, lane_xor8(a));
-      a *= rstd;
-      s = a > 0.f ? a / 448.f : 1.f;
-      r = 1.f / s;
+      s = scale_of(a);
       if (e < dim && (tid & 15) == 0) scale[row * groups + e / kNormGroup] = s;
     }
     if (e >= dim) continue;
-    float y[kV];
-#pragma unroll
-    for (int i = 0; i < kV; ++i) y[i] = quotient(h[it][i] * rstd, s, r);
+    float (&y)[kV] = h[it];
+    quotients(y, s);
     C8 c;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
