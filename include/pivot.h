@@ -473,8 +473,8 @@ pivot_status pivot_cache4_read(const pivot_cache4* c, int32_t batch, int32_t n, 
  *         aligned
  *   idx   dev int32 [rows, topk] as the index calls write it: a row attends to
  *         its entries in [0, its position] (others, the -1 padding among them,
- *         are skipped; entries of one row are distinct).  NULL: to every
- *         position up to its own
+ *         are skipped; entries of one row are distinct; topk may be 0).  NULL:
+ *         to every position up to its own
  *   out   dev bf16 [rows, heads, 512], 16-byte aligned
  *   lse   dev fp32 [rows, heads], or NULL
  *   acc   dev fp32 [B, acc_stride], or NULL; acc_stride >= every n_k[b]

@@ -740,8 +740,8 @@ def pivot_cache4_attend(q, cache, q_pos0, n_k, scale, idx=None, cu_q=None, acc=N
                         stream=None):
     """Attention of q (bf16 [B, n_q, heads, 576], or [rows, heads, 576] with the
     runs cu_q) over the 4-bit cache: (out bf16 [..., heads, 512], lse fp32
-    [..., heads]).  idx: int32 [..., topk] index sets, or None for every position
-    up to the query's own; acc: fp32 [B, >= max n_k], each token's softmax weight
+    [..., heads]).  idx: int32 [..., topk] index sets (topk 0: nothing to attend
+    to), or None for every position up to the query's own; acc: fp32 [B, >= max n_k], each token's softmax weight
     is added to it.  Rows and heads of q may be strided."""
     lead = q.shape[:-2]
     heads, dim = q.shape[-2:]
@@ -774,7 +774,8 @@ def pivot_cache4_attend(q, cache, q_pos0, n_k, scale, idx=None, cu_q=None, acc=N
     if idx is not None:
         if idx.dtype != torch.int32 or idx.shape[:-1] != lead or not idx.is_contiguous():
             raise ValueError("idx must be a contiguous int32 tensor with one row of entries per query")
-        a.idx, a.topk = idx.data_ptr(), idx.shape[-1]
+        # sets without entries have no address, and NULL means the prefix
+        a.idx, a.topk = idx.data_ptr() or q.data_ptr(), idx.shape[-1]
     a.scale = scale
     shape = tuple(lead) + (heads,)
     out = (torch.empty(shape + (PIVOT_CACHE4_LATENT,), dtype=torch.bfloat16, device=q.device) if out is None
