@@ -1061,12 +1061,15 @@ __global__ __launch_bounds__(64 * kWaves) void join_kernel(AttendArgs a, RunTabl
   }
 }
 
-// Sum over a tile's rows of the softmax weights of its 32 keys: 8 rows at a
-// time, each thread one key, the rows of a thread in ascending order.
-__device__ __forceinline__ float tile_weight(const float* tile, const float2* stat, int rows, float* red, int tid) {
+// Sum over a tile's rows from `least` on, those that attend to the thread's key,
+// of the softmax weights of its 32 keys: 8 rows at a time, each thread one key,
+// the rows of a thread in ascending order.  The rows before are left out, not
+// added as zeros: the masked scores of a NaN row give NaN.
+__device__ __forceinline__ float tile_weight(const float* tile, const float2* stat, int least, int rows, float* red,
+                                             int tid) {
   const int k = tid & 31, first = tid >> 5;
   float w = 0.f;
-  for (int r = first; r < rows; r += 8) {
+  for (int r = first + (max(least - first, 0) + 7) / 8 * 8; r < rows; r += 8) {
     const float2 st = stat[r];
     w = fmaf(exp2f(tile[r * kTileKeys + k] - st.x), st.y, w);
   }
@@ -1084,8 +1087,9 @@ __global__ __launch_bounds__(256) void dense_weights_kernel(AttendArgs a, RunTab
   const int b = blockIdx.y, tile = blockIdx.x, tid = threadIdx.x;
   const int n = t.pos0[b] + t.n_rows[b], rows = t.n_rows[b] * a.heads;
   if (rows == 0 || tile * kTileKeys >= n) return;
+  const int least = max(tile * kTileKeys + (tid & 31) - t.pos0[b], 0) * a.heads;
   const float w = tile_weight(sm.s2 + sm.base[b] + (int64_t)tile * rows * kTileKeys,
-                              sm.stat + (int64_t)t.row0[b] * a.heads, rows, red, tid);
+                              sm.stat + (int64_t)t.row0[b] * a.heads, least, rows, red, tid);
   const int s = tile * kTileKeys + tid;
   if (tid < kTileKeys && s < n) a.acc[(int64_t)b * a.acc_stride + s] += w;
 }
@@ -1095,7 +1099,7 @@ __global__ __launch_bounds__(256) void slot_weights_kernel(AttendArgs a, ScoreMa
   __shared__ float red[256];
   const int r = blockIdx.y, tile = blockIdx.x, tid = threadIdx.x;
   const float w = tile_weight(sm.s2 + ((int64_t)r * padded + tile * kTileKeys) * a.heads,
-                              sm.stat + (int64_t)r * a.heads, a.heads, red, tid);
+                              sm.stat + (int64_t)r * a.heads, 0, a.heads, red, tid);
   if (tid < kTileKeys) slots[(int64_t)r * padded + tile * kTileKeys + tid] = w;
 }
 
