@@ -427,6 +427,8 @@ typedef struct {
  *                            byte in its low half
  *   scales  dev [rows, 16]   E8M0: 2^(byte - 127) of each 32 values, 255 = NaN
  *   rope    dev [rows, 64]   bf16
+ * A value is exact in bf16, but for those of 2^128 and more (codes 4 and 6 times
+ * 2^126, 2 to 6 times 2^127), which are infinite.
  * All three 16-byte aligned.  One row serves all heads: keys are the whole row,
  * values its latent part.
  */
@@ -455,7 +457,7 @@ pivot_status pivot_cache4_write(const pivot_cache4* c, int32_t batch, int32_t n_
 
 /*
  * Read rows back: out (dev bf16 [B, n, 576], 16-byte aligned) receives the
- * values (exact in bf16) of positions idx (dev int32 [B, n]); a negative
+ * values of positions idx (dev int32 [B, n]); a negative
  * position, or one past what the map can hold, gives a row of zeros.
  */
 pivot_status pivot_cache4_read(const pivot_cache4* c, int32_t batch, int32_t n, const int32_t* idx, void* out,
@@ -481,7 +483,9 @@ pivot_status pivot_cache4_read(const pivot_cache4* c, int32_t batch, int32_t n, 
  * Row i of sequence b is at position q_pos0[b] + i; q_pos0[b] + n_q <= n_k[b].
  * A row with nothing to attend to, or only scores of -infinity, has out = 0 and
  * lse = -infinity and adds nothing.  A row that attends to a token with a NaN,
- * or whose query holds one, is NaN; tokens it does not attend to never reach it.
+ * or whose query holds one, is NaN, and so is one that attends to an infinite
+ * value, unless its score is -infinity; tokens it does not attend to never reach
+ * it.
  * Scores and sums are fp32 (the products are exact), the weights are rounded to
  * 16 bits (two bf16) for the product with the values.  The same call gives the
  * same bits.

@@ -99,6 +99,13 @@ __device__ __forceinline__ float row_reduce(float x, Op op) {
   return x;
 }
 
+// Two bf16 values, 0 for those that are infinite or NaN.
+__device__ __forceinline__ uint32_t finite(uint32_t v) {
+  if ((v & 0x7F80u) == 0x7F80u) v &= 0xFFFF0000u;
+  if ((v & 0x7F800000u) == 0x7F800000u) v &= 0xFFFFu;
+  return v;
+}
+
 // LDS.  As loaded, 1024 bytes of one wave's load (4 keys' codes, 8 keys' position
 // values) are a group, the groups 1088 bytes apart; the 16-byte chunks of a row
 // change places by two bits of the key.  Together the two put one chunk of 16
@@ -424,11 +431,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
   // ---- the other stages
   // 8 values a lane of the wave's j-th key, widened
   auto put_values = [&](int ln, int j, int vslot, uint32_t word, int byte) {
-    // a NaN block makes the key's scores NaN; as a value it must not reach the
-    // rows that do not attend to the key (0 * NaN)
-    const int e = byte & ((byte - 255) >> 31);
     *reinterpret_cast<uint4*>(s_val + vslot * kValueBytes + (4 * w + j) * 2 * kLatent +
-                              (16 * ln ^ (swizzle(4 * w + j) << 4))) = decode8(word, scale_operand(e));
+                              (16 * ln ^ (swizzle(4 * w + j) << 4))) = decode8(word, scale_operand(byte));
   };
   // one of the wave's 4 keys: read, then widened
   uint32_t word[2];
@@ -444,6 +448,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
     }
   };
   constexpr int WIDENS = 8;
+  // The wave's 4 keys once widened: a NaN or an infinity (byte 255; 2^128 and more,
+  // which bytes from 253 on can give) makes the key's scores NaN or infinite, its
+  // weight NaN or 0; as a value it must not reach the rows that do not attend to
+  // the key (0 * NaN), so 0 stands for it.
+  auto drop_infinite = [&](int ln, int slot, int vslot) {
+    if (!__any(s_scale[slot * kScalesBytes + (w >> 1) * 256 + (w & 1) * 64 + ln] >= 253)) return;
+#pragma unroll 1
+    for (int j = 0; j < 16; ++j) {
+      uint32_t& v = *reinterpret_cast<uint32_t*>(s_val + vslot * kValueBytes + 4 * w * 2 * kLatent + 256 * j + 4 * ln);
+      v = finite(v);
+    }
+  };
 
   // scores of the wave's rows and keys, operands read ahead
   v4f s[NKT];
@@ -840,6 +856,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
   for (int i = 0; i < count; ++i) {
     int ln = lane;
     if constexpr (RG >= 4) asm volatile("" : "+v"(ln));  // no registers are left to keep addresses in: made anew for every tile
+    drop_infinite(ln, slot, i & 1);
     const int next = slot + 1 == NS ? 0 : slot + 1, after_next = next + 1 == NS ? 0 : next + 1;  // of i + 1, i + 2
     if constexpr (ONE) {
       // tile i + 2 is loaded, i + 1 scored; waves 0 .. 3 meet the others before they

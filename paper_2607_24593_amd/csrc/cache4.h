@@ -54,7 +54,7 @@ typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ float scale_operand(uint32_t byte) { return __uint_as_float(byte << 23); }
 
 // Eight codes (one word) times a scale, as bf16: exact, since a code has two
-// significant bits.
+// significant bits, or infinite from 2^128 on.
 __device__ __forceinline__ uint4 decode8(uint32_t w, float scale) {
   uint4 o;
   o.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));

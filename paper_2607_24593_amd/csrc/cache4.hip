@@ -4,7 +4,8 @@
 // two with max|x| / 2^e <= 6 (6 is the largest E2M1 value, so nothing
 // saturates); its codes are the E2M1 values nearest to x / 2^e, ties to even.
 // Dividing by a power of two is exact, so is the product on reading: a value
-// read back is the code's value times 2^e in bf16.  A block of zeros has the
+// read back is the code's value times 2^e in bf16 (infinite where 3.5 * 2^126 and
+// more was rounded up to 4 * 2^126).  A block of zeros has the
 // scale byte 0, a block that holds an infinity or a NaN the byte 255 (all of
 // it reads as NaN).
 //
