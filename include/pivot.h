@@ -471,8 +471,8 @@ pivot_status pivot_cache4_read(const pivot_cache4* c, int32_t batch, int32_t n, 
  *   out[r,h] = sum_s softmax(z[r,h])[s] c_s     lse[r,h] = log sum_s exp(z[r,h,s])
  *   acc[b,s] += sum over the sequence's rows r and heads h of softmax(z[r,h])[s]
  *   q     dev bf16, row r head h at r * q_row_stride + h * q_head_stride, 576
- *         values (latent part first); strides are multiples of 8, q is 16-byte
- *         aligned
+ *         values (latent part first); strides are multiples of 8, a row's
+ *         heads come before the next row's, q is 16-byte aligned
  *   idx   dev int32 [rows, topk] as the index calls write it: a row attends to
  *         its entries in [0, its position] (others, the -1 padding among them,
  *         are skipped; entries of one row are distinct; topk may be 0).  NULL:

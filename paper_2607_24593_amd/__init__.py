@@ -742,7 +742,8 @@ def pivot_cache4_attend(q, cache, q_pos0, n_k, scale, idx=None, cu_q=None, acc=N
     runs cu_q) over the 4-bit cache: (out bf16 [..., heads, 512], lse fp32
     [..., heads]).  idx: int32 [..., topk] index sets (topk 0: nothing to attend
     to), or None for every position up to the query's own; acc: fp32 [B, >= max n_k], each token's softmax weight
-    is added to it.  Rows and heads of q may be strided."""
+    is added to it.  Rows and heads of q may be strided, a row's heads before the
+    next row's."""
     lead = q.shape[:-2]
     heads, dim = q.shape[-2:]
     if q.dtype != torch.bfloat16 or dim != PIVOT_CACHE4_LATENT + PIVOT_CACHE4_ROPE or q.stride(-1) != 1:
@@ -753,7 +754,7 @@ def pivot_cache4_attend(q, cache, q_pos0, n_k, scale, idx=None, cu_q=None, acc=N
     if cu_q is None:
         if q.dim() != 4 or q.shape[0] != batch:
             raise ValueError("q must be [B, n_q, heads, 576]")
-        if batch > 1 and q.shape[1] > 0 and q.stride(0) != q.shape[1] * q.stride(1):
+        if batch > 1 and q.shape[1] > 1 and q.stride(0) != q.shape[1] * q.stride(1):
             raise ValueError("the sequences of q must follow each other at its row stride")
         row_stride, n_rows = (q.stride(1) if q.shape[1] > 1 else q.stride(0)), batch * q.shape[1]
     else:
@@ -761,8 +762,8 @@ def pivot_cache4_attend(q, cache, q_pos0, n_k, scale, idx=None, cu_q=None, acc=N
             raise ValueError("q must be [rows, heads, 576] with rows = cu_q[-1] and len(cu_q) = B + 1")
         row_stride, n_rows = q.stride(0), q.shape[0]
     head_stride = q.stride(-2) if heads > 1 else dim
-    if n_rows <= 1:
-        row_stride = max(row_stride, (heads - 1) * head_stride + dim)
+    if n_rows <= 1:  # no next row
+        row_stride = (heads - 1) * head_stride + dim
     _check_batch(cache._keep[3], batch)
     a = pivot_attend_args()
     a.heads, a.batch, a.n_q = heads, batch, 0 if cu_q is not None else q.shape[1]

@@ -1,6 +1,7 @@
 """GPU tests of the attention over the 4-bit cache (and of the cache) at the edges
 of their inputs, against plain definitions in 64 bits (ops_ref): empty index
-sets, rows of NaN, infinities in masked places, the ends of bf16."""
+sets, rows of NaN, infinities in masked places, the ends of bf16, strides of
+single queries."""
 import numpy as np
 import pytest
 import torch
@@ -148,3 +149,23 @@ def test_cache_values_at_the_ends_of_bf16():
     back = pv.pivot_cache4_read(c, torch.arange(40, dtype=torch.int32, device="cuda")[None]).double().cpu().numpy()[0, :, :512]
     want[39, 2:4] = [np.inf, -np.inf]  # 4 * 2^126
     assert want[39, 0] == 3 * 2.0 ** 126 and np.array_equal(back, want)
+
+
+@pytest.mark.parametrize("layout", ["slice", "heads first"])
+def test_attend_single_queries_of_a_wider_tensor(layout):
+    """One query a sequence: its dimension's stride has no meaning."""
+    rng = np.random.default_rng(91)
+    lens, heads = [70, 33, 50, 64], 16
+    pool = Pool(lens, 16, rng)
+    if layout == "slice":
+        wide = torch.from_numpy(_queries((4, 3, heads), rng)).bfloat16().cuda()
+        q = wide[:, 1:2]
+    else:
+        wide = torch.from_numpy(_queries((4, heads, 1), rng)).bfloat16().cuda()
+        q = wide.transpose(1, 2)
+    say("attend single queries", layout, tuple(q.stride()))
+    want = pv.pivot_cache4_attend(q.contiguous(), pool.cache, [n - 1 for n in lens], lens, 0.04)
+    got = pv.pivot_cache4_attend(q, pool.cache, [n - 1 for n in lens], lens, 0.04)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    got = pv.pivot_cache4_attend(q[1:2], Pool([33], 0, rng).cache, [32], [33], 0.04)  # any row stride, one row
+    assert torch.isfinite(got[1]).all()
