@@ -612,6 +612,17 @@ def _host_ints(v, batch=None):
     return (ctypes.c_int32 * len(v)).from_buffer(array.array("i", v)) if len(v) else (ctypes.c_int32 * 0)()
 
 
+def _on_gpu(device, *tensors):
+    """Every tensor (or None) has to be on the GPU `device` (an index, negative for
+    the host): the library takes addresses as they are."""
+    same = device >= 0
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            same = False
+    if not same:
+        raise ValueError("the call's tensors must all be on one GPU")
+
+
 def _rows_of(t, width, what):
     """The row stride of a 2-D (or contiguous deeper) tensor of `width` values a row."""
     if t.shape[-1] != width or t.stride(-1) != 1:
@@ -656,6 +667,7 @@ def pivot_rmsnorm_fp8(x, weight, eps=1e-6, residual=None, group=0, residual_out=
     elif residual_out is not None:
         raise ValueError("residual_out needs a residual")
     _expect(weight, x.dtype, (dim,), "weight")
+    _on_gpu(x.get_device(), residual, residual_out, weight, codes, scale)
     rows = x.numel() // dim if dim else 0
     shape = tuple(x.shape[:-1]) + (-(-dim // group) if group else 1,)
     codes = (torch.empty_like(x, dtype=torch.uint8, memory_format=torch.contiguous_format) if codes is None
@@ -690,7 +702,11 @@ def make_cache4(codes, scales, rope, row_map) -> pivot_cache4:
     _expect(rope, torch.bfloat16, (n, PIVOT_CACHE4_ROPE), "rope")
     if row_map.rows > n:
         raise ValueError(f"the row map names {row_map.rows} rows, the cache holds {n}")
+    device, bt = codes.get_device(), getattr(row_map, "_bt", None)
+    if any(t is not None and t.get_device() != device for t in (scales, rope, bt)):
+        raise ValueError("the cache's tensors and its block table must be on one device")
     c = pivot_cache4()
+    c._device = device
     c.codes, c.scales, c.rope = codes.data_ptr(), scales.data_ptr(), rope.data_ptr()
     c.map = row_map
     c._keep = (codes, scales, rope, row_map)
@@ -716,6 +732,7 @@ def pivot_cache4_write(latent, rope, cache, pos0, n_new=None, cu=None, stream=No
         raise ValueError(f"latent and rope must hold {rows} rows")
     if cu is not None and len(cu) != batch + 1:
         raise ValueError("cu needs len(pos0) + 1 entries")
+    _on_gpu(cache._device, latent, rope)
     _check(lib().pivot_cache4_write(ctypes.byref(cache), batch, 0 if cu is not None else int(n_new),
                                     None if cu is None else _host_ints(cu), _host_ints(pos0), _ptr(latent),
                                     _rows_of(latent, PIVOT_CACHE4_LATENT, "latent"), _ptr(rope),
@@ -728,6 +745,7 @@ def pivot_cache4_read(cache, idx, out=None, stream=None):
     if idx.dtype != torch.int32 or idx.dim() != 2 or not idx.is_contiguous():
         raise ValueError("idx must be a contiguous int32 [B, n] tensor")
     _check_batch(cache._keep[3], idx.shape[0])
+    _on_gpu(cache._device, idx, out)
     shape = tuple(idx.shape) + (PIVOT_CACHE4_LATENT + PIVOT_CACHE4_ROPE,)
     out = (torch.empty(shape, dtype=torch.bfloat16, device=idx.device) if out is None
            else _expect(out, torch.bfloat16, shape, "out"))
@@ -765,6 +783,7 @@ def pivot_cache4_attend(q, cache, q_pos0, n_k, scale, idx=None, cu_q=None, acc=N
     if n_rows <= 1:  # no next row
         row_stride = (heads - 1) * head_stride + dim
     _check_batch(cache._keep[3], batch)
+    _on_gpu(cache._device, q, idx, acc, out, lse, ws)
     a = pivot_attend_args()
     a.heads, a.batch, a.n_q = heads, batch, 0 if cu_q is not None else q.shape[1]
     a.q_pos0, a.n_k = _host_ints(q_pos0), _host_ints(n_k)
@@ -820,15 +839,19 @@ def pivot_evict(acc, n_k, keep, arrays, from_map, to_map, sink=0, recent=0, out_
     a.keep, a.sink, a.recent = keep, sink, recent
     a.out_keep, a.out_acc = out_keep.data_ptr(), out_acc.data_ptr()
     a.n_arrays = len(arrays)
+    device = acc.get_device()
+    _on_gpu(device, out_keep, out_acc, ws)
     if arrays:
         a.from_, a.to = from_map, to_map
         _check_batch(from_map, batch, "from_map's block_table")
         _check_batch(to_map, batch, "to_map's block_table")
+        _on_gpu(device, getattr(from_map, "_bt", None), getattr(to_map, "_bt", None))
     for i, (src, dst) in enumerate(arrays):
         if not src.is_contiguous() or not dst.is_contiguous() or src.dtype != dst.dtype or src.shape[1:] != dst.shape[1:]:
             raise ValueError(f"array {i}: src and dst must be contiguous, of one type and row shape")
         if from_map.rows > src.shape[0] or to_map.rows > dst.shape[0]:
             raise ValueError(f"array {i} has fewer rows than its row map")
+        _on_gpu(device, src, dst)
         m = a.arrays[i]
         m.src, m.dst = src.data_ptr(), dst.data_ptr()
         m.row_bytes = src.element_size() * (src.numel() // max(src.shape[0], 1))
