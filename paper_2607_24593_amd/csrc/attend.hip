@@ -48,10 +48,10 @@ typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
 // tell apart from their target; the tile loop waits for them itself, before the
 // barrier that hands the tile over.
 __device__ __forceinline__ void load_lds16(const void* src, uint32_t dst) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(src) : "memory", "m0");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(dst), "v"(src) : "memory");
 }
 __device__ __forceinline__ void load_lds4(const void* src, uint32_t dst) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(dst), "v"(src) : "memory", "m0");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %1, off" ::"{m0}"(dst), "v"(src) : "memory");
 }
 
 // f(0), f(1), ..., f(N - 1) with the index a constant
