@@ -14,6 +14,8 @@
 // with a scale per 128 values, 16 neighbouring lanes hold a group.
 // 8192 x 6144 fp32 values: 122 us, 5.4 TB/s, a copy's rate; 260 x 5003 bf16: 6.5;
 // one row of 4096: 2.7.
+#include <algorithm>
+
 #include "device_common.h"
 #include "dpp.h"
 #include "ops.h"
@@ -214,18 +216,25 @@ __global__ __launch_bounds__(NT) void norm_kernel(const T* x, int64_t ld_x, cons
 
 template <class T, bool GROUPS>
 hipError_t launch(const NormArgs& a, hipStream_t stream) {
-  const T* x = (const T*)a.x;
-  const T* res = (const T*)a.residual;
-  const T* w = (const T*)a.weight;
-  const dim3 grid((unsigned)a.rows);
-#define PIVOT_NORM(NT, IT)                                                                                         \
-  hipLaunchKernelGGL((norm_kernel<T, NT, IT, GROUPS>), grid, dim3(NT), 0, stream, x, a.ld_x, res, a.ld_residual, w, \
-                     a.eps, a.dim, (T*)a.residual_out, a.codes, a.scale)
-  if (a.dim <= 2048) PIVOT_NORM(256, 1);
-  else if (a.dim <= 8192) PIVOT_NORM(1024, 1);
-  else PIVOT_NORM(1024, 4);
+  const int groups = GROUPS ? (a.dim + kNormGroup - 1) / kNormGroup : 1;
+  // a launch counts its threads in 32 bits, and drops what is above without an error
+  constexpr int64_t kMost = 1 << 21;
+  for (int64_t row = 0; row < a.rows; row += kMost) {
+    const T* x = (const T*)a.x + row * a.ld_x;
+    const T* res = a.residual ? (const T*)a.residual + row * a.ld_residual : nullptr;
+    T* res_out = a.residual_out ? (T*)a.residual_out + row * a.dim : nullptr;
+    const dim3 grid((unsigned)std::min<int64_t>(a.rows - row, kMost));
+#define PIVOT_NORM(NT, IT)                                                                                      \
+  hipLaunchKernelGGL((norm_kernel<T, NT, IT, GROUPS>), grid, dim3(NT), 0, stream, x, a.ld_x, res, a.ld_residual, \
+                     (const T*)a.weight, a.eps, a.dim, res_out, a.codes + row * a.dim, a.scale + row * groups)
+    if (a.dim <= 2048) PIVOT_NORM(256, 1);
+    else if (a.dim <= 8192) PIVOT_NORM(1024, 1);
+    else PIVOT_NORM(1024, 4);
 #undef PIVOT_NORM
-  return hipGetLastError();
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace

@@ -57,3 +57,22 @@ def test_norm_of_tiny_and_huge_outputs(dim, group, dtype):
     for std, size in ((1e12, 1e30), (1e-10, 1e-30)):
         _norm_edges((x.float() * std).to(dt), ((1 + 0.3 * torch.rand(dim, generator=g)) * size).to(dt), 0.0, group,
                     f"rows {std} weights {size}")
+
+
+def test_norm_of_more_rows_than_one_launch_holds():
+    """2^24 rows and some: 2^32 threads are more than a launch takes."""
+    rows, dim = (1 << 24) + 5, 8
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn((rows, dim), generator=g, device="cuda").bfloat16()
+    w = torch.ones(dim, dtype=torch.bfloat16, device="cuda")
+    say("norm of many rows")
+    codes, scale, h = pv.pivot_rmsnorm_fp8(x, w, 1e-6, residual=x)
+    assert torch.equal(h, x + x)  # twice a bf16 value is one
+    some = torch.cat([torch.arange(i, min(i + 64, rows), device="cuda")
+                      for i in (0, (1 << 21) - 32, (1 << 22) - 32, (1 << 23) + 1, rows - 64)])
+    for got, want in zip((codes, scale), pv.pivot_rmsnorm_fp8(x[some], w, 1e-6, residual=x[some])):
+        assert torch.equal(got[some], want)
+    y = 2 * x.float()
+    y = y * torch.rsqrt(y.square().mean(-1, keepdim=True) + 1e-6)
+    want = y.abs().amax(-1, keepdim=True) / 448
+    assert bool(((scale - want).abs() <= 4e-6 * want).all())
