@@ -258,7 +258,7 @@ pivot_status pivot_cache4_write(const pivot_cache4* c, int32_t batch, int32_t n_
   if (ld_latent < kLatent || ld_rope < kRope)
     return fail(PIVOT_ERR_INVALID_ARG, "rows overlap (ld_latent=%lld, ld_rope=%lld)", (long long)ld_latent,
                 (long long)ld_rope);
-  return for_pieces(batch, n_new, cu, pos0, nullptr, 0x7FFFFFFF, 0, [](int) -> int64_t { return 0; },
+  return for_pieces(batch, n_new, cu, pos0, nullptr, kMaxCacheRows, 0, [](int) -> int64_t { return 0; },
                     [&](const RunTable& t, int b0, int64_t row0, int n) -> pivot_status {
                       if (n == 0) return PIVOT_OK;
                       int64_t first;
@@ -281,7 +281,7 @@ pivot_status pivot_cache4_read(const pivot_cache4* c, int32_t batch, int32_t n, 
   if (!aligned(out, 16)) return fail(PIVOT_ERR_INVALID_ARG, "out must be 16-byte aligned");
   int64_t first;
   const KeyMap map = key_map(c->map, 0, &first);
-  const Cache4Read r{cache_at(*c, first), map, capacity(c->map), idx, batch, n, (uint16_t*)out};
+  const Cache4Read r{cache_at(*c, first), map, capacity(c->map), 0, idx, batch, n, (uint16_t*)out};
   return hip_check(launch_cache4_read(r, (hipStream_t)stream), "cache read kernel");
 }
 

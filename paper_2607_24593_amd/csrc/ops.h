@@ -23,8 +23,10 @@ struct NormArgs {
 };
 hipError_t launch_norm(int dtype, const NormArgs& a, hipStream_t stream);
 
-// Quantise `rows` packed tokens into the cache rows of their positions
-// (RunTable), and read rows back as bf16.
+// Quantise `rows` <= kMaxCacheRows packed tokens into the cache rows of their
+// positions (RunTable), and read rows back as bf16, a wave a row.  A launch counts
+// its threads in 32 bits, and drops what is above without an error.
+constexpr int kMaxCacheRows = 1 << 25;
 struct Cache4Write {
   const uint16_t* latent;
   int64_t ld_latent;
@@ -40,6 +42,7 @@ struct Cache4Read {
   Cache4 cache;
   KeyMap map;
   int64_t capacity;      // positions past it read as zeros, as negative ones do
+  int64_t first;         // of the launch's rows
   const int32_t* idx;    // [batch, n]
   int32_t batch, n;
   uint16_t* out;         // [batch, n, 576]

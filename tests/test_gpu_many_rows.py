@@ -1,0 +1,63 @@
+"""GPU tests of calls whose rows need more than the 2^32 threads that one launch
+counts: the 4-bit cache's write and read."""
+import numpy as np
+import pytest
+import torch
+
+import ops_ref as ref
+import paper_2607_24593_amd as pv
+from gpu_util import host, say
+
+pytestmark = pytest.mark.gpu
+
+ROWS = (1 << 26) + 3  # a wave a row
+
+
+@pytest.fixture
+def room():
+    """At least 140 GB of free device memory, given back afterwards."""
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 140 << 30:
+        pytest.skip("needs 140 GB of device memory")
+    yield
+    torch.cuda.empty_cache()
+
+
+def _cache(rows):
+    parts = (torch.zeros((rows, 256), dtype=torch.uint8, device="cuda"),
+             torch.zeros((rows, 16), dtype=torch.uint8, device="cuda"),
+             torch.zeros((rows, 64), dtype=torch.bfloat16, device="cuda"))
+    return parts, pv.make_cache4(*parts, pv.make_row_map(seq_stride=rows, rows=rows))
+
+
+def test_cache_write_of_many_rows(room):
+    parts, cache = _cache(ROWS)
+    latent = torch.zeros((ROWS, 512), dtype=torch.bfloat16, device="cuda")
+    rope = torch.zeros((ROWS, 64), dtype=torch.bfloat16, device="cuda")
+    some = torch.tensor([0, 7, 255, 1 << 24, (1 << 25) - 1, 1 << 25, (1 << 26) - 1, 1 << 26, ROWS - 1], device="cuda")
+    rng = np.random.default_rng(1)
+    x, r = ref.bf16(rng.standard_normal((len(some), 512))), ref.bf16(rng.standard_normal((len(some), 64)))
+    latent[some], rope[some] = torch.from_numpy(x).bfloat16().cuda(), torch.from_numpy(r).bfloat16().cuda()
+    say("cache write of many rows")
+    pv.pivot_cache4_write(latent, rope, cache, [0], ROWS)
+    codes, scales = ref.quantise(x)
+    got = [host(t[some]) for t in parts[:2]]
+    assert np.array_equal(got[1], scales)
+    assert np.array_equal(ref.values(got[0], got[1]), ref.values(codes, scales))
+    assert np.array_equal(parts[2][some].double().cpu().numpy(), r)
+
+
+def test_cache_read_of_many_rows(room):
+    parts, cache = _cache(16)
+    rng = np.random.default_rng(2)
+    x, r = ref.bf16(rng.standard_normal((16, 512))), ref.bf16(rng.standard_normal((16, 64)))
+    pv.pivot_cache4_write(torch.from_numpy(x).bfloat16().cuda(), torch.from_numpy(r).bfloat16().cuda(), cache, [0], 16)
+    idx = torch.full((1, ROWS), 3, dtype=torch.int32, device="cuda")
+    some = torch.tensor([0, 1 << 25, (1 << 26) - 1, 1 << 26, ROWS - 1], device="cuda")
+    idx[0, some] = torch.arange(5, dtype=torch.int32, device="cuda") + 8
+    say("cache read of many rows")
+    out = pv.pivot_cache4_read(cache, idx)[0]
+    want = pv.pivot_cache4_read(cache, torch.arange(16, dtype=torch.int32, device="cuda")[None])[0]
+    assert torch.equal(out[some], want[8:13])
+    near = torch.tensor([5, (1 << 25) + 1, (1 << 26) + 1], device="cuda")
+    assert torch.equal(out[near], want[3].expand(3, -1))
