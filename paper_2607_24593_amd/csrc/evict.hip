@@ -347,9 +347,9 @@ __device__ __forceinline__ void move_rows(const uint8_t* src, uint8_t* dst, int 
 }
 
 __global__ __launch_bounds__(256) void move_kernel(MoveArrays m, KeyMap from, KeyMap to, const int32_t* __restrict__ kept,
-                                                   int keep, unsigned groups) {
+                                                   int b0, int keep, unsigned groups) {
   __shared__ int64_t s_from[kMoveRows], s_to[kMoveRows];
-  const int b = (int)(blockIdx.x / groups), j = (int)(blockIdx.x % groups) * kMoveRows + threadIdx.x;
+  const int b = b0 + (int)(blockIdx.x / groups), j = (int)(blockIdx.x % groups) * kMoveRows + threadIdx.x;
   if (threadIdx.x < kMoveRows) {
     const int32_t pos = j < keep ? kept[(int64_t)b * keep + j] : -1;
     s_from[threadIdx.x] = pos < 0 ? -1 : from.row(b, pos);
@@ -403,8 +403,15 @@ hipError_t launch_evict(const EvictArgs& a, const RunTable& t, void* workspace, 
 hipError_t launch_move(const MoveArrays& m, const KeyMap& from, const KeyMap& to, const int32_t* kept, int batch,
                        int keep, hipStream_t stream) {
   const unsigned groups = (unsigned)((keep + kMoveRows - 1) / kMoveRows);  // of a sequence
-  hipLaunchKernelGGL(move_kernel, dim3(groups * (unsigned)batch), dim3(256), 0, stream, m, from, to, kept, keep, groups);
-  return hipGetLastError();
+  // a launch counts its threads in 32 bits, and drops what is above without an error
+  const int most = (int)(((1u << 24) - 1) / groups);  // sequences
+  for (int b = 0; b < batch; b += most) {
+    hipLaunchKernelGGL(move_kernel, dim3(groups * (unsigned)std::min(batch - b, most)), dim3(256), 0, stream, m, from, to,
+                       kept, b, keep, groups);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace pivot

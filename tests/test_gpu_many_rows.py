@@ -1,5 +1,5 @@
 """GPU tests of calls whose rows need more than the 2^32 threads that one launch
-counts: the 4-bit cache's write and read."""
+counts: the 4-bit cache's write and read, and the eviction's moves."""
 import numpy as np
 import pytest
 import torch
@@ -61,3 +61,16 @@ def test_cache_read_of_many_rows(room):
     assert torch.equal(out[some], want[8:13])
     near = torch.tensor([5, (1 << 25) + 1, (1 << 26) + 1], device="cuda")
     assert torch.equal(out[near], want[3].expand(3, -1))
+
+
+def test_evict_moves_of_many_sequences():
+    batch = (1 << 24) + 3
+    acc = torch.rand((batch, 2), device="cuda")
+    src = torch.arange(2 * batch, dtype=torch.int32, device="cuda")
+    dst = torch.zeros(batch, dtype=torch.int32, device="cuda")
+    say("evict moves of many sequences")
+    kept, out_acc = pv.pivot_evict(acc, [2] * batch, 1, [(src, dst)], pv.make_row_map(seq_stride=2, rows=2 * batch),
+                                   pv.make_row_map(seq_stride=1, rows=batch))
+    want = (acc[:, 1] > acc[:, 0]).int()
+    assert torch.equal(kept[:, 0], want) and torch.equal(out_acc[:, 0], acc.amax(1))
+    assert torch.equal(dst, 2 * torch.arange(batch, dtype=torch.int32, device="cuda") + want)
