@@ -1630,7 +1630,22 @@ static hipError_t topk_launch(const E* scores, int64_t ld, const SeqTable& st, c
   const int nrows = rs.i1 - rs.i0;
   if (nrows <= 0 || st.n <= 0) return hipSuccess;
   const int64_t blocks = (int64_t)st.n * nrows;
-  if (blocks > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
+  // A launch counts its threads in 32 bits, and drops what is above without an
+  // error: 2^22 rows of up to 1024 threads.  Rows of one sequence (the public
+  // select's; a call's score tiles hold far fewer) are cut into several launches.
+  constexpr int kMostRows = 1 << 21;
+  if (blocks > 2 * kMostRows) {
+    if (st.n > 1) return hipErrorInvalidConfiguration;
+    for (int64_t i = rs.i0; i < rs.i1; i += kMostRows) {
+      RowSpace part = rs;
+      part.i0 = (int32_t)i;
+      part.i1 = (int32_t)std::min<int64_t>(i + kMostRows, rs.i1);
+      const int64_t lim = std::min<int64_t>(lim_max, (int64_t)st.q_pos0[0] - rs.shift + (part.i1 - 1) * (int64_t)rs.step);
+      const hipError_t e = topk_launch(scores + (i - rs.i0) * ld, ld, st, part, od, lim, scratch, scratch_bytes, stream);
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+  }
   constexpr int N = ScoreVec<E>::N;
   // fp32 rows of which half and more are wanted: their candidates leave two
   // resident workgroups to a CU, and the two-pass select, which keeps only the

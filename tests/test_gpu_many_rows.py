@@ -1,5 +1,5 @@
 """GPU tests of calls whose rows need more than the 2^32 threads that one launch
-counts: the 4-bit cache's write and read, and the eviction's moves."""
+counts: the 4-bit cache's write and read, the eviction's moves, and the select."""
 import numpy as np
 import pytest
 import torch
@@ -74,3 +74,17 @@ def test_evict_moves_of_many_sequences():
     want = (acc[:, 1] > acc[:, 0]).int()
     assert torch.equal(kept[:, 0], want) and torch.equal(out_acc[:, 0], acc.amax(1))
     assert torch.equal(dst, 2 * torch.arange(batch, dtype=torch.int32, device="cuda") + want)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_select_of_many_rows(dtype):
+    """2^23 rows and some, 512 threads each."""
+    rows, ld, m = (1 << 23) + 9, 24, 3
+    g = torch.Generator(device="cuda").manual_seed(4)
+    perm = torch.randperm(ld, generator=g, device="cuda")
+    scores = (torch.arange(rows, device="cuda")[:, None] * 5 + perm) % ld  # a different order in every row
+    select = pv.pivot_topk_rows if dtype == torch.float32 else pv.pivot_topk_rows_bf16
+    say("select of many rows", dtype)
+    out = select(scores.to(dtype), ld, 0, m)
+    want = scores.topk(m, dim=1).indices.int()
+    assert torch.equal(out.sort(1).values, want.sort(1).values)
