@@ -376,9 +376,15 @@ __global__ __launch_bounds__(256) void encode_e4m3_kernel(const float* __restric
 
 hipError_t launch_encode_e4m3(const float* x, uint8_t* out, int64_t n, hipStream_t stream) {
   if (n <= 0) return hipSuccess;
-  int64_t blocks = (n + 1023) / 1024;
-  hipLaunchKernelGGL(encode_e4m3_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, x, out, n);
-  return hipGetLastError();
+  // a launch counts its threads in 32 bits, and drops what is above without an error
+  constexpr int64_t kMost = int64_t(1) << 33;
+  for (int64_t i = 0; i < n; i += kMost) {
+    const int64_t part = n - i < kMost ? n - i : kMost, blocks = (part + 1023) / 1024;
+    hipLaunchKernelGGL(encode_e4m3_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, x + i, out + i, part);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace pivot

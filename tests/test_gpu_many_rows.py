@@ -1,5 +1,6 @@
 """GPU tests of calls whose rows need more than the 2^32 threads that one launch
-counts: the 4-bit cache's write and read, the eviction's moves, and the select."""
+counts: the 4-bit cache's write and read, the eviction's moves, the
+select, and the encoder."""
 import numpy as np
 import pytest
 import torch
@@ -88,3 +89,12 @@ def test_select_of_many_rows(dtype):
     out = select(scores.to(dtype), ld, 0, m)
     want = scores.topk(m, dim=1).indices.int()
     assert torch.equal(out.sort(1).values, want.sort(1).values)
+
+
+def test_encode_of_many_values(room):
+    n = (1 << 34) + 5  # 4 a thread
+    x = torch.ones(n, device="cuda")
+    say("encode of many values")
+    out = pv.pivot_encode_e4m3(x)
+    del x
+    assert all(bool((out[i:i + (1 << 31)] == 0x38).all()) for i in range(0, n, 1 << 31))  # 1.0
