@@ -487,10 +487,15 @@ pivot_status pivot_cache4_read(const pivot_cache4* c, int32_t batch, int32_t n, 
  * value, unless its score is -infinity; tokens it does not attend to never reach
  * it.
  * Scores and sums are fp32 (the products are exact), the weights are rounded to
- * 16 bits (two bf16) for the product with the values.  The same call gives the
- * same bits.
+ * 16 bits (two bf16) for the product with the values.  The weights that are
+ * summed are relative to a score up to 32 octaves below the row's largest, so
+ * values of 2^80 and more may overflow the sums.  The same call gives the same
+ * bits.
  * Workspace: pivot_cache4_attend_workspace_size(a) bytes (device, 256-byte
  * aligned; 0 for invalid shapes or none needed; reads the host arrays only).
+ * With acc the scores of as many rows as fit 1 GiB (at least one row) are kept at
+ * once, beside partial outputs: a long or wide call asks for a little more than
+ * 1 GiB.
  */
 #define PIVOT_ATTEND_MAX_HEADS 128
 typedef struct {

@@ -605,10 +605,8 @@ def pivot_encode_e4m3(x, out=None, stream=None):
 
 # ---- operators around the index calls ----
 
-def _host_ints(v, batch=None):
-    """A ctypes int32 array of host integers (one repeated for the batch, or a sequence)."""
-    if isinstance(v, int):
-        v = [v] * batch
+def _host_ints(v):
+    """A ctypes int32 array of a sequence of host integers."""
     return (ctypes.c_int32 * len(v)).from_buffer(array.array("i", v)) if len(v) else (ctypes.c_int32 * 0)()
 
 

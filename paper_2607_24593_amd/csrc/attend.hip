@@ -176,15 +176,16 @@ struct Output {
 // steps ahead, and the vector work of other stages is cut into pieces issued
 // between the output's matrix products, which run on their own once issued;
 // scheduling barriers keep the two from being sorted apart.  Bound by vector
-// instructions (the codes' conversion at half rate, 4460 of 7900 cycles a tile)
-// next to 3200 cycles of matrix products: 1003 queries x 128 heads x 2048 keys in
-// 820 us, 700 TFLOP/s.
+// instructions (the codes' conversion at half rate, 4460 of 7900 cycles a tile:
+// every wave converts all 32 keys for its own rows, and the tile is widened once
+// more into LDS) next to 3200 cycles of matrix products: 1003 queries x 128 heads x
+// 2048 keys in 814 us, 703 TFLOP/s.
 // RG <= 4: 16 rows' products with 16 keys are shared by 4 / RG waves, so that all
 // 8 have some; their parts go through LDS, and a tile takes an iteration more: the
 // load of tile i + 2 + AHEAD, the products of i + 2, the weights and the widening
 // of i + 1, the output of i, again with one barrier.  All operands are read from
 // LDS first, then used.  With RG = 1 a tile takes 3200 cycles, a third of them
-// reads of LDS: 8 sequences of 9001 to 40000 keys x 16 heads in 43 us, 1.7 TB/s.
+// reads of LDS: 8 sequences of 9001 to 40000 keys x 16 heads in 43 us, 1.8 TB/s.
 // The sequence that workgroup i belongs to: the last one with first <= i (one
 // without workgroups shares its first with the next).
 __device__ __forceinline__ int owner_of(const int32_t* first, int n, int i) {

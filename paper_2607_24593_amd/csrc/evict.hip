@@ -11,10 +11,12 @@
 //
 // Up to kWhole = 32768 tokens one workgroup keeps a sequence's keys in registers
 // and does it all: 8192 tokens in 9.6 us, 20000 in 20, 32 sequences of 3000 to
-// 32768 side by side in 22.  Bound by one CU's vector instructions, nine a key
-// and pass.  A longer sequence is cut into chunks, a workgroup each, with a launch
+// 32768 side by side in 22.  There are instances of 8192 and of 32768 places, and
+// a sequence pays for all of its instance's: 8193 tokens take 17.4 us.  With 20000
+// one CU's vector instructions take 26200 of 47800 cycles on every SIMD; the rest
+// are waits for barriers, LDS and the first loads.  A longer sequence is cut into chunks, a workgroup each, with a launch
 // per pass and one that emits; every workgroup adds up the chunks' counts of the
-// pass before by itself.  That is five launches, 26 us at 32769 tokens and 31 at
+// pass before by itself.  That is five launches, 25 us at 32769 tokens and 33 at
 // 131072, where one workgroup takes 200; at 20000 it is 25.
 // The rows then move at a copy's rate: 131072 rows of 532 bytes in 30 us, 4.7 TB/s.
 #include <algorithm>
