@@ -234,6 +234,9 @@ pivot_status pivot_rmsnorm_fp8(int32_t dtype, int32_t n_rows, int32_t dim, const
   const uintptr_t e = dtype == PIVOT_DT_BF16 ? 2 : 4;
   if (!aligned(x, e) || !aligned(residual, e) || !aligned(weight, e) || !aligned(residual_out, e) || !aligned(scale, 4))
     return fail(PIVOT_ERR_INVALID_ARG, "a pointer is not aligned to its elements");
+  // a padded row's sums would land on other rows that are still to be read
+  if (residual_out && n_rows > 1 && ((residual_out == x && ld_x != dim) || (residual_out == residual && ld_residual != dim)))
+    return fail(PIVOT_ERR_INVALID_ARG, "residual_out may only be an input whose rows are not padded");
   const NormArgs a{x, ld_x, residual, ld_residual, weight, eps, n_rows, dim, group, residual_out, codes, scale};
   return hip_check(launch_norm(dtype, a, (hipStream_t)stream), "norm kernel");
 }

@@ -76,3 +76,18 @@ def test_norm_of_more_rows_than_one_launch_holds():
     y = y * torch.rsqrt(y.square().mean(-1, keepdim=True) + 1e-6)
     want = y.abs().amax(-1, keepdim=True) / 448
     assert bool(((scale - want).abs() <= 4e-6 * want).all())
+
+
+@pytest.mark.parametrize("rows", [1, 5])
+def test_norm_in_place(rows):
+    """The sums in place of x or of the residual, of rows that are not padded (or of one row)."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    wide = torch.randn((rows, 700), generator=g, device="cuda").bfloat16()
+    w = torch.ones(300, dtype=torch.bfloat16, device="cuda")
+    x, r = (torch.randn((rows, 300), generator=g, device="cuda").bfloat16() for _ in range(2))
+    for a, b, first in ((x, r, True), (x, r, False), (x, wide[:, :300], True), (wide[:, 9:309], r, False)):
+        want = pv.pivot_rmsnorm_fp8(a, w, 1e-6, residual=b)
+        a, b = (a.clone(), b) if first else (a, b.clone())
+        say("norm in place", rows)
+        got = pv.pivot_rmsnorm_fp8(a, w, 1e-6, residual=b, residual_out=a if first else b)
+        assert got[2] is (a if first else b) and all(torch.equal(s, t) for s, t in zip(got, want))
