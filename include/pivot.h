@@ -566,6 +566,174 @@ size_t pivot_evict_workspace_size(const pivot_evict_args* a);
 pivot_status pivot_evict(const pivot_evict_args* a);
 
 /*
+ * ---- A decode step with drafted tokens ----
+ *
+ * Products of few rows with weights in 4 bits, attention for trees of drafted
+ * tokens, and pages of a cache that sequences share.  The conventions above hold.
+ */
+
+/*
+ * y = x w^T for n_rows rows of x [n_rows, k] and weights w [n, k] in OCP MXFP4:
+ *   codes   dev [n, k / 2]   E2M1, the even value of a byte in its low half; 16-byte
+ *                            aligned
+ *   scales  dev [n, k / 32]  E8M0: 2^(byte - 127) of each 32 values, 255 = NaN
+ * as in the 4-bit cache (weights of 2^128 and more are infinite).  k is a multiple
+ * of 32 (else PIVOT_ERR_UNSUPPORTED), at most PIVOT_LINEAR4_MAX_K; n is any.
+ *   x       dev, rows ld_x >= k values apart: PIVOT_DT_BF16, or PIVOT_DT_FP8_E4M3
+ *           with x_scale dev fp32 [n_rows, group ? ceil(k / 128) : 1], group 0 (one
+ *           scale a row) or 128, as pivot_rmsnorm_fp8 writes them.  Pointers need
+ *           only their elements' alignment.
+ *   out     dev, rows ld_out >= n values apart: out_dtype PIVOT_DT_BF16 or
+ *           PIVOT_DT_FP32; must not overlap the inputs
+ * Products are exact and added in fp32; a row's scale multiplies its sum, a group's
+ * the sum of its 128 products; the result is rounded once.  The same call gives the
+ * same bits.  Meant for the few rows of a decode step (up to 64 read the weights
+ * once, more read them again for each 64).
+ * Workspace: pivot_linear4_workspace_size(a) bytes (device, 256-byte aligned; 0 for
+ * invalid shapes or none needed).
+ */
+#define PIVOT_LINEAR4_MAX_K (1 << 20)
+typedef struct {
+  int32_t x_dtype, out_dtype;
+  int32_t n_rows, n, k;
+  int32_t group;
+  const void* x;
+  int64_t ld_x;
+  const float* x_scale;
+  const void* codes;
+  const void* scales;
+  void* out;
+  int64_t ld_out;
+  void* workspace;
+  size_t workspace_bytes;
+  void* stream;
+} pivot_linear4_args;
+size_t pivot_linear4_workspace_size(const pivot_linear4_args* a);
+pivot_status pivot_linear4(const pivot_linear4_args* a);
+
+/*
+ * Weights w [n, k] (dev, PIVOT_DT_BF16 or PIVOT_DT_FP32, rows ld_w >= k values
+ * apart) to codes and scales of pivot_linear4, by pivot_cache4_write's rule: the
+ * smallest power of two 2^e (e >= -127) with max|w| / 2^e <= 6 over 32 values,
+ * codes nearest to w / 2^e, ties to even; 32 zeros have scale byte 0, an infinity
+ * or a NaN among them byte 255 and codes 0.  codes are 4-byte aligned.
+ */
+pivot_status pivot_linear4_pack(int32_t dtype, int32_t n, int32_t k, const void* w, int64_t ld_w, void* codes,
+                                void* scales, void* stream);
+
+/*
+ * pivot_cache4_attend for rows that are trees of drafted tokens.  The rows of
+ * sequence b are the nodes of its tree, node i in the cache at position q_pos0[b] +
+ * i.  A row attends to every position below q_pos0[b], and to node j where bit j
+ * mod 32 of word j / 32 of its mask is set: a node's own bit and its ancestors',
+ * but any bits are taken (a row whose mask is 0 sees the prefix alone).  With idx, to
+ * those of its entries.  Bits behind the sequence's last node are not read as
+ * nodes.
+ *   mask   dev uint32 [rows, words], rows as in q; 32 * words >= every sequence's
+ *          rows; words in [1, PIVOT_TREE_MAX_NODES / 32] (else UNSUPPORTED)
+ * Everything else as in pivot_cache4_attend, the workspace included.
+ */
+#define PIVOT_TREE_MAX_NODES 1024
+typedef struct {
+  const uint32_t* mask;
+  int32_t words;
+} pivot_tree;
+size_t pivot_cache4_attend_tree_workspace_size(const pivot_attend_args* a, const pivot_tree* t);
+pivot_status pivot_cache4_attend_tree(const pivot_attend_args* a, const pivot_tree* t);
+
+/*
+ * The accepted path of every sequence's tree, moved to where the next step expects
+ * it: row pos0[b] + path[b][j] of every array under `map` becomes row pos0[b] + j,
+ * in place.
+ *   path    dev int32 [batch, n]: the accepted nodes in ascending order, then -1.
+ *           An entry that is not above the one before it, or past what the map can
+ *           hold, ends the path as -1 does.
+ *   pos0    host [batch]: the tree's first position
+ *   arrays  n_arrays (1 .. PIVOT_EVICT_MAX_ARRAYS) row arrays, rows of a multiple of
+ *           4 bytes, 4-byte aligned
+ * The rows from pos0[b] to its last node must not be shared with another sequence.
+ */
+typedef struct {
+  void* rows;
+  int32_t row_bytes;
+} pivot_rows;
+pivot_status pivot_tree_accept(int32_t batch, int32_t n, const int32_t* path, const int32_t* pos0, int32_t n_arrays,
+                               const pivot_rows* arrays, const pivot_row_map* map, void* stream);
+
+/*
+ * Pages that sequences share.
+ *   table   dev int32 [slots, max_pages]: entry i of a slot is the page of its
+ *           positions i * page_size ..., -1 where there is none.  Its first rows are
+ *           a row map's block_table.
+ *   refs    dev int32 [n_pages]: how many slots hold a page; 0 for free pages
+ * page_size is a power of two in [16, 65536], n_pages * page_size and slots *
+ * max_pages at most 2^31 - 1.  A pool starts with every entry -1 and every count 0.
+ * Lists are host arrays of at most PIVOT_PAGES_MAX_LIST entries (else
+ * UNSUPPORTED), slots in [0, slots), tokens in [0, max_pages * page_size].  Table
+ * entries that name no page of the pool are left alone.
+ * Calls that change one pool run in the order of one stream.
+ */
+#define PIVOT_PAGES_MAX_LIST 256
+typedef struct {
+  int32_t* table;
+  int32_t slots, max_pages, page_size;
+  int32_t* refs;
+  int32_t n_pages;
+} pivot_pages;
+
+/* Slot dst[i], without pages until now, gets the pages of slot src[i]'s first
+ * tokens[i] tokens, counted once more.  No dst may come twice or be a src. */
+pivot_status pivot_pages_fork(const pivot_pages* p, int32_t n, const int32_t* src, const int32_t* dst,
+                              const int32_t* tokens, void* stream);
+
+/* Slot slot[i] goes back from tokens[i] tokens to keep[i] <= tokens[i]: pages that
+ * hold none of those are counted once less, their entries become -1.  Slots are
+ * distinct. */
+pivot_status pivot_pages_free(const pivot_pages* p, int32_t n, const int32_t* slot, const int32_t* tokens,
+                              const int32_t* keep, void* stream);
+
+/*
+ * Slots (distinct) grow from tokens[i] to new_tokens[i] >= tokens[i] tokens.  In the
+ * order of the list a slot that grows takes
+ *   - a page for its partly filled last one, if other slots hold that too: the new
+ *     one takes its entry, the old one is counted once less.  Of slots in the list
+ *     that share a page the last keeps it, if no others hold it;
+ *   - pages for its new tokens, from ceil(tokens / page_size) on;
+ * each time the lowest free page.
+ *   copies  dev int32 [n, 2]: (old page, new page) of the first kind, else (-1, -1):
+ *           their contents are to be copied (pivot_pages_copy) before they are used
+ *   state   dev int32 [2]: pages that were missing, pages that are free afterwards.
+ *           If any is missing nothing is changed, and copies are all -1.
+ * Workspace: pivot_pages_grow_workspace_size bytes (device, 256-byte aligned; 0 for
+ * invalid arguments).
+ */
+size_t pivot_pages_grow_workspace_size(const pivot_pages* p, int32_t n, const int32_t* tokens, const int32_t* new_tokens);
+pivot_status pivot_pages_grow(const pivot_pages* p, int32_t n, const int32_t* slot, const int32_t* tokens,
+                              const int32_t* new_tokens, int32_t* copies, int32_t* state, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/*
+ * The pages in use move to the pool's lowest: the highest page in use to the lowest
+ * free one, the next highest to the next, and so on while that is lower and for at
+ * most max_moves >= 0 pages.  Counts and the entries of all slots follow.
+ *   moves   dev int32 [max_moves, 2]: (old page, new page), then (-1, -1); contents
+ *           are to be copied (pivot_pages_copy) before anything is written
+ *   state   dev int32 [2]: moves, pages in use
+ */
+size_t pivot_pages_compact_workspace_size(const pivot_pages* p);
+pivot_status pivot_pages_compact(const pivot_pages* p, int32_t max_moves, int32_t* moves, int32_t* state, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/*
+ * Page pairs[i][0] of every array (n_pages * page_size rows, n_arrays in 1 ..
+ * PIVOT_EVICT_MAX_ARRAYS) copied to page pairs[i][1]; pairs (dev int32 [n, 2]) that
+ * name no pages of the pool are left out.  No page may be written by one pair and
+ * be part of another.
+ */
+pivot_status pivot_pages_copy(const pivot_pages* p, int32_t n, const int32_t* pairs, int32_t n_arrays,
+                              const pivot_rows* arrays, void* stream);
+
+/*
  * Kernel timing.  Between pivot_profile_begin() and pivot_profile_end() every
  * kernel that the index calls and their stages launch is bracketed by two HIP
  * events recorded on the launch's stream.  pivot_profile_end() waits for those

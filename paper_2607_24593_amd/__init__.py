@@ -30,6 +30,7 @@ PIVOT_REFINE_AUTO, PIVOT_REFINE_FUSED, PIVOT_REFINE_SPLIT = 0, 1, 2
 H, D = 64, 128
 PIVOT_CACHE4_LATENT, PIVOT_CACHE4_ROPE = 512, 64
 PIVOT_ATTEND_MAX_HEADS, PIVOT_EVICT_MAX_ARRAYS = 128, 8
+PIVOT_LINEAR4_MAX_K, PIVOT_TREE_MAX_NODES, PIVOT_PAGES_MAX_LIST = 1 << 20, 1024, 256
 
 EXPORTED = ["pivot_workspace_size", "pivot_dense_index", "pivot_group_index", "pivot_cand_width",
             "pivot_group_workspace_size", "pivot_group_index_opts", "pivot_dense_index_layout",
@@ -40,6 +41,10 @@ EXPORTED = ["pivot_workspace_size", "pivot_dense_index", "pivot_group_index", "p
             "pivot_group_index_noalloc",
             "pivot_rmsnorm_fp8", "pivot_cache4_write", "pivot_cache4_read", "pivot_cache4_attend",
             "pivot_cache4_attend_workspace_size", "pivot_evict", "pivot_evict_workspace_size",
+            "pivot_linear4", "pivot_linear4_workspace_size", "pivot_linear4_pack",
+            "pivot_cache4_attend_tree", "pivot_cache4_attend_tree_workspace_size", "pivot_tree_accept",
+            "pivot_pages_fork", "pivot_pages_free", "pivot_pages_grow", "pivot_pages_grow_workspace_size",
+            "pivot_pages_compact", "pivot_pages_compact_workspace_size", "pivot_pages_copy",
             "pivot_profile_end", "pivot_status_string", "pivot_last_error", "pivot_version"]
 KERNELS = ["proxy", "score", "select", "refine", "fill", "lin", "copy"]
 
@@ -119,6 +124,29 @@ class pivot_evict_args(ctypes.Structure):
         ("from_", pivot_row_map), ("to", pivot_row_map),
         ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t), ("stream", ctypes.c_void_p),
     ]
+
+
+class pivot_linear4_args(ctypes.Structure):
+    _fields_ = [
+        ("x_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("n", ctypes.c_int32),
+        ("k", ctypes.c_int32), ("group", ctypes.c_int32), ("x", ctypes.c_void_p), ("ld_x", ctypes.c_int64),
+        ("x_scale", ctypes.c_void_p), ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("out", ctypes.c_void_p),
+        ("ld_out", ctypes.c_int64), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+        ("stream", ctypes.c_void_p),
+    ]
+
+
+class pivot_tree(ctypes.Structure):
+    _fields_ = [("mask", ctypes.c_void_p), ("words", ctypes.c_int32)]
+
+
+class pivot_rows(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_void_p), ("row_bytes", ctypes.c_int32)]
+
+
+class pivot_pages(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("slots", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("refs", ctypes.c_void_p), ("n_pages", ctypes.c_int32)]
 
 
 def make_layout(cu_q=None, block_table=None, page_size=0, pool_keys=0) -> pivot_layout:
@@ -217,6 +245,36 @@ def lib():
         L.pivot_evict_workspace_size.argtypes = [ctypes.POINTER(pivot_evict_args)]
         L.pivot_evict.restype = I32
         L.pivot_evict.argtypes = [ctypes.POINTER(pivot_evict_args)]
+        SZ = ctypes.c_size_t
+        L.pivot_linear4_workspace_size.restype = SZ
+        L.pivot_linear4_workspace_size.argtypes = [ctypes.POINTER(pivot_linear4_args)]
+        L.pivot_linear4.restype = I32
+        L.pivot_linear4.argtypes = [ctypes.POINTER(pivot_linear4_args)]
+        L.pivot_linear4_pack.restype = I32
+        L.pivot_linear4_pack.argtypes = [I32, I32, I32, P, I64, P, P, P]
+        T = ctypes.POINTER(pivot_tree)
+        L.pivot_cache4_attend_tree_workspace_size.restype = SZ
+        L.pivot_cache4_attend_tree_workspace_size.argtypes = [ctypes.POINTER(pivot_attend_args), T]
+        L.pivot_cache4_attend_tree.restype = I32
+        L.pivot_cache4_attend_tree.argtypes = [ctypes.POINTER(pivot_attend_args), T]
+        R = ctypes.POINTER(pivot_rows)
+        L.pivot_tree_accept.restype = I32
+        L.pivot_tree_accept.argtypes = [I32, I32, P, PI, I32, R, ctypes.POINTER(pivot_row_map), P]
+        PG = ctypes.POINTER(pivot_pages)
+        L.pivot_pages_fork.restype = I32
+        L.pivot_pages_fork.argtypes = [PG, I32, PI, PI, PI, P]
+        L.pivot_pages_free.restype = I32
+        L.pivot_pages_free.argtypes = [PG, I32, PI, PI, PI, P]
+        L.pivot_pages_grow_workspace_size.restype = SZ
+        L.pivot_pages_grow_workspace_size.argtypes = [PG, I32, PI, PI]
+        L.pivot_pages_grow.restype = I32
+        L.pivot_pages_grow.argtypes = [PG, I32, PI, PI, PI, P, P, P, SZ, P]
+        L.pivot_pages_compact_workspace_size.restype = SZ
+        L.pivot_pages_compact_workspace_size.argtypes = [PG]
+        L.pivot_pages_compact.restype = I32
+        L.pivot_pages_compact.argtypes = [PG, I32, P, P, P, SZ, P]
+        L.pivot_pages_copy.restype = I32
+        L.pivot_pages_copy.argtypes = [PG, I32, P, I32, R, P]
         L.pivot_profile_begin.restype = I32
         L.pivot_profile_begin.argtypes = []
         L.pivot_profile_begin_kinds.restype = I32
@@ -753,13 +811,16 @@ def pivot_cache4_read(cache, idx, out=None, stream=None):
 
 
 def pivot_cache4_attend(q, cache, q_pos0, n_k, scale, idx=None, cu_q=None, acc=None, out=None, lse=None, ws=None,
-                        stream=None):
+                        stream=None, tree=None):
     """Attention of q (bf16 [B, n_q, heads, 576], or [rows, heads, 576] with the
     runs cu_q) over the 4-bit cache: (out bf16 [..., heads, 512], lse fp32
     [..., heads]).  idx: int32 [..., topk] index sets (topk 0: nothing to attend
     to), or None for every position up to the query's own; acc: fp32 [B, >= max n_k], each token's softmax weight
     is added to it.  Rows and heads of q may be strided, a row's heads before the
-    next row's."""
+    next row's.  tree: int32 [..., words], the masks of rows that are trees of drafted
+    tokens: bit j mod 32 of word j // 32 is set where the row attends to the j-th
+    row of its sequence (itself and its ancestors); all attend to the positions
+    before the first."""
     lead = q.shape[:-2]
     heads, dim = q.shape[-2:]
     if q.dtype != torch.bfloat16 or dim != PIVOT_CACHE4_LATENT + PIVOT_CACHE4_ROPE or q.stride(-1) != 1:
@@ -781,7 +842,7 @@ def pivot_cache4_attend(q, cache, q_pos0, n_k, scale, idx=None, cu_q=None, acc=N
     if n_rows <= 1:  # no next row
         row_stride = (heads - 1) * head_stride + dim
     _check_batch(cache._keep[3], batch)
-    _on_gpu(cache._device, q, idx, acc, out, lse, ws)
+    _on_gpu(cache._device, q, idx, acc, out, lse, ws, tree)
     a = pivot_attend_args()
     a.heads, a.batch, a.n_q = heads, batch, 0 if cu_q is not None else q.shape[1]
     a.q_pos0, a.n_k = _host_ints(q_pos0), _host_ints(n_k)
@@ -807,11 +868,21 @@ def pivot_cache4_attend(q, cache, q_pos0, n_k, scale, idx=None, cu_q=None, acc=N
         a.acc, a.acc_stride = acc.data_ptr(), acc.shape[1]
     a.stream = _stream(stream)
     L = lib()
-    need = L.pivot_cache4_attend_workspace_size(ctypes.byref(a))
+    if tree is not None:
+        if tree.dtype != torch.int32 or tree.shape[:-1] != lead or not tree.is_contiguous():
+            raise ValueError("tree must be a contiguous int32 tensor with one mask per query")
+        t = pivot_tree()
+        t.mask, t.words = tree.data_ptr(), tree.shape[-1]
+        need = L.pivot_cache4_attend_tree_workspace_size(ctypes.byref(a), ctypes.byref(t))
+    else:
+        need = L.pivot_cache4_attend_workspace_size(ctypes.byref(a))
     if need:
         buf = ws if ws is not None else workspace(need, q.device, stream)
         a.workspace, a.workspace_bytes = buf.data_ptr(), buf.numel() * buf.element_size()
-    _check(L.pivot_cache4_attend(ctypes.byref(a)), "pivot_cache4_attend")
+    if tree is not None:
+        _check(L.pivot_cache4_attend_tree(ctypes.byref(a), ctypes.byref(t)), "pivot_cache4_attend_tree")
+    else:
+        _check(L.pivot_cache4_attend(ctypes.byref(a)), "pivot_cache4_attend")
     return out, lse
 
 
@@ -861,3 +932,190 @@ def pivot_evict(acc, n_k, keep, arrays, from_map, to_map, sink=0, recent=0, out_
         a.workspace, a.workspace_bytes = buf.data_ptr(), buf.numel() * buf.element_size()
     _check(L.pivot_evict(ctypes.byref(a)), "pivot_evict")
     return out_keep, out_acc
+
+
+# ---- a decode step with drafted tokens ----
+
+def pivot_linear4_pack(w, codes=None, scales=None, stream=None):
+    """Weights [n, k] (bf16 or fp32, rows may be strided, k a multiple of 32) as the
+    4-bit operand of pivot_linear4: (codes uint8 [n, k / 2], scales uint8 [n, k / 32])."""
+    if w.dim() != 2:
+        raise ValueError("w must be [n, k]")
+    n, k = w.shape
+    code = _float_code(w)
+    if k % 32:
+        raise ValueError("k must be a multiple of 32")
+    ld = _rows_of(w, k, "w")
+    _on_gpu(w.get_device(), codes, scales)
+    codes = (torch.empty((n, k // 2), dtype=torch.uint8, device=w.device) if codes is None
+             else _expect(codes, torch.uint8, (n, k // 2), "codes"))
+    scales = (torch.empty((n, k // 32), dtype=torch.uint8, device=w.device) if scales is None
+              else _expect(scales, torch.uint8, (n, k // 32), "scales"))
+    _check(lib().pivot_linear4_pack(code, n, k, _ptr(w), ld, _ptr(codes), _ptr(scales), _stream(stream)),
+           "pivot_linear4_pack")
+    return codes, scales
+
+
+def pivot_linear4(x, codes, scales, x_scale=None, group=0, dtype=torch.bfloat16, out=None, ws=None, stream=None):
+    """x [..., k] times weights in 4 bits (pivot_linear4_pack): [..., n] in dtype
+    (bfloat16 or float32).  x is bf16, or fp8 codes (float8_e4m3fn or uint8) with
+    x_scale as pivot_rmsnorm_fp8 gives them: fp32 [..., 1] with group 0, [...,
+    ceil(k / 128)] with group 128.  Rows of a 2-D x and out may be strided."""
+    k = x.shape[-1]
+    n = codes.shape[0]
+    ld_x = _rows_of(x, k, "x")
+    _expect(codes, torch.uint8, (n, k // 2), "codes")
+    _expect(scales, torch.uint8, (n, k // 32), "scales")
+    a = pivot_linear4_args()
+    if x.dtype == torch.bfloat16:
+        if x_scale is not None or group:
+            raise ValueError("bf16 rows have no scales")
+    elif x.dtype in (torch.float8_e4m3fn, torch.uint8):
+        if x_scale is None:
+            raise ValueError("fp8 rows need x_scale")
+        _expect(x_scale, torch.float32, x.shape[:-1] + (-(-k // group) if group else 1,), "x_scale")
+        a.x_dtype, a.x_scale = PIVOT_DT_FP8_E4M3, x_scale.data_ptr()
+    else:
+        raise ValueError("x must be bfloat16 or fp8 codes")
+    if dtype == torch.float32:
+        a.out_dtype = PIVOT_DT_FP32
+    elif dtype != torch.bfloat16:
+        raise ValueError("dtype must be bfloat16 or float32")
+    _on_gpu(x.get_device(), codes, scales, x_scale, out, ws)
+    shape = x.shape[:-1] + (n,)
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=x.device)
+    elif out.dtype != dtype or out.shape != shape:
+        raise ValueError(f"out must be a {dtype} tensor of shape {tuple(shape)}")
+    a.n_rows, a.n, a.k, a.group = x.numel() // k if k else 0, n, k, group
+    a.x, a.ld_x, a.codes, a.scales = x.data_ptr(), ld_x, codes.data_ptr(), scales.data_ptr()
+    a.out, a.ld_out = out.data_ptr(), _rows_of(out, n, "out")
+    a.stream = _stream(stream)
+    L = lib()
+    need = L.pivot_linear4_workspace_size(ctypes.byref(a))
+    if need:
+        buf = ws if ws is not None else workspace(need, x.device, stream)
+        a.workspace, a.workspace_bytes = buf.data_ptr(), buf.numel() * buf.element_size()
+    _check(L.pivot_linear4(ctypes.byref(a)), "pivot_linear4")
+    return out
+
+
+def _row_arrays(arrays, rows, device):
+    """The C array of row arrays, one row a token along the first dimension."""
+    if not 1 <= len(arrays) <= PIVOT_EVICT_MAX_ARRAYS:
+        raise ValueError(f"a call takes 1 to {PIVOT_EVICT_MAX_ARRAYS} arrays")
+    c = (pivot_rows * len(arrays))()
+    for i, x in enumerate(arrays):
+        if x.get_device() != device:
+            raise ValueError("the call's tensors must all be on one GPU")
+        if not x.is_contiguous() or x.shape[0] < rows:
+            raise ValueError(f"array {i} must be contiguous, with {rows} rows")
+        c[i].rows, c[i].row_bytes = x.data_ptr(), x.element_size() * (x.numel() // max(x.shape[0], 1))
+    return c
+
+
+def pivot_tree_accept(path, pos0, arrays, row_map, stream=None):
+    """Move the accepted nodes of each sequence's tree to the positions that follow
+    its prefix, in place in every row array: row pos0[b] + path[b, j] becomes row
+    pos0[b] + j.  path: int32 [B, n], ascending, -1 behind the last accepted node."""
+    if path.dtype != torch.int32 or path.dim() != 2 or not path.is_contiguous() or path.shape[0] != len(pos0):
+        raise ValueError("path must be a contiguous int32 [len(pos0), n] tensor")
+    device = path.get_device()
+    _check_batch(row_map, len(pos0))
+    _on_gpu(device, getattr(row_map, "_bt", None))
+    c = _row_arrays(arrays, row_map.rows, device)
+    _check(lib().pivot_tree_accept(len(pos0), path.shape[1], _ptr(path), _host_ints(pos0), len(arrays), c,
+                                   ctypes.byref(row_map), _stream(stream)), "pivot_tree_accept")
+
+
+def make_pages(table, refs, page_size) -> pivot_pages:
+    """Pages that sequences share: table int32 [slots, max_pages] (-1: no page) and
+    refs int32 [n_pages], the slots that hold a page.  A pool starts with -1 and 0.
+    The tensors have to outlive the struct's use."""
+    if table.dtype != torch.int32 or table.dim() != 2 or not table.is_contiguous():
+        raise ValueError("table must be a contiguous int32 [slots, max_pages] tensor")
+    if refs.dtype != torch.int32 or refs.dim() != 1 or not refs.is_contiguous():
+        raise ValueError("refs must be a contiguous int32 [n_pages] tensor")
+    if table.get_device() != refs.get_device():
+        raise ValueError("table and refs must be on one device")
+    p = pivot_pages()
+    p.table, p.slots, p.max_pages, p.page_size = table.data_ptr(), table.shape[0], table.shape[1], int(page_size)
+    p.refs, p.n_pages = refs.data_ptr(), refs.shape[0]
+    p._keep = (table, refs)
+    p._device = table.get_device()
+    return p
+
+
+def _same_length(*lists):
+    if len({len(v) for v in lists}) != 1:
+        raise ValueError("the lists must have one entry per sequence")
+    return len(lists[0])
+
+
+def pivot_pages_fork(pages, src, dst, tokens, stream=None):
+    """Slots dst[i], without pages until now, share the pages of the first tokens[i]
+    tokens of slots src[i]."""
+    n = _same_length(src, dst, tokens)
+    _on_gpu(pages._device)
+    _check(lib().pivot_pages_fork(ctypes.byref(pages), n, _host_ints(src), _host_ints(dst), _host_ints(tokens),
+                                  _stream(stream)), "pivot_pages_fork")
+
+
+def pivot_pages_free(pages, slots, tokens, keep, stream=None):
+    """Slots go back from tokens[i] to keep[i] tokens; pages that no slot holds any
+    more are free."""
+    n = _same_length(slots, tokens, keep)
+    _on_gpu(pages._device)
+    _check(lib().pivot_pages_free(ctypes.byref(pages), n, _host_ints(slots), _host_ints(tokens), _host_ints(keep),
+                                  _stream(stream)), "pivot_pages_free")
+
+
+def pivot_pages_grow(pages, slots, tokens, new_tokens, copies=None, state=None, ws=None, stream=None):
+    """Slots grow from tokens[i] to new_tokens[i] tokens, from the lowest free pages
+    up; a partly filled last page that other slots hold too is replaced.  Returns
+    (copies int32 [n, 2], the (old, new) pages that pivot_pages_copy has to copy, -1
+    where none; state int32 [2]: pages missing, pages free afterwards).  If pages are
+    missing nothing has changed."""
+    n = _same_length(slots, tokens, new_tokens)
+    device = pages._keep[0].device
+    _on_gpu(pages._device, copies, state, ws)
+    copies = (torch.empty((n, 2), dtype=torch.int32, device=device) if copies is None
+              else _expect(copies, torch.int32, (n, 2), "copies"))
+    state = (torch.empty((2,), dtype=torch.int32, device=device) if state is None
+             else _expect(state, torch.int32, (2,), "state"))
+    L, now, then = lib(), _host_ints(tokens), _host_ints(new_tokens)
+    need = L.pivot_pages_grow_workspace_size(ctypes.byref(pages), n, now, then)
+    buf = ws if ws is not None else workspace(need, device, stream)
+    _check(L.pivot_pages_grow(ctypes.byref(pages), n, _host_ints(slots), now, then, _ptr(copies), _ptr(state), _ptr(buf),
+                              buf.numel() * buf.element_size(), _stream(stream)), "pivot_pages_grow")
+    return copies, state
+
+
+def pivot_pages_compact(pages, max_moves, moves=None, state=None, ws=None, stream=None):
+    """The highest pages in use move to the lowest free ones, at most max_moves of
+    them; counts and table follow.  Returns (moves int32 [max_moves, 2], the (old,
+    new) pages that pivot_pages_copy has to copy, -1 behind them; state int32 [2]:
+    moves, pages in use)."""
+    device = pages._keep[0].device
+    _on_gpu(pages._device, moves, state, ws)
+    moves = (torch.empty((max_moves, 2), dtype=torch.int32, device=device) if moves is None
+             else _expect(moves, torch.int32, (max_moves, 2), "moves"))
+    state = (torch.empty((2,), dtype=torch.int32, device=device) if state is None
+             else _expect(state, torch.int32, (2,), "state"))
+    L = lib()
+    need = L.pivot_pages_compact_workspace_size(ctypes.byref(pages))
+    buf = ws if ws is not None else workspace(need, device, stream)
+    _check(L.pivot_pages_compact(ctypes.byref(pages), max_moves, _ptr(moves), _ptr(state), _ptr(buf),
+                                 buf.numel() * buf.element_size(), _stream(stream)), "pivot_pages_compact")
+    return moves, state
+
+
+def pivot_pages_copy(pages, pairs, arrays, stream=None):
+    """Copy whole pages, pairs (old, new) int32 [n, 2], in every row array; pairs of
+    -1 are left out."""
+    if pairs.dtype != torch.int32 or pairs.dim() != 2 or pairs.shape[1] != 2 or not pairs.is_contiguous():
+        raise ValueError("pairs must be a contiguous int32 [n, 2] tensor")
+    _on_gpu(pages._device, pairs)
+    c = _row_arrays(arrays, pages.n_pages * pages.page_size, pages._device)
+    _check(lib().pivot_pages_copy(ctypes.byref(pages), pairs.shape[0], _ptr(pairs), len(arrays), c, _stream(stream)),
+           "pivot_pages_copy")

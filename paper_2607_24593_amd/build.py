@@ -14,7 +14,8 @@ LIB = os.path.join(HERE, "libpivot.so")
 BUILD_DIR = os.path.join(HERE, "_build")
 
 SOURCES = ["api.hip", "proxy.hip", "score.hip", "select.hip", "refine.hip",
-           "api_ops.hip", "norm.hip", "cache4.hip", "attend.hip", "evict.hip"]
+           "api_ops.hip", "norm.hip", "cache4.hip", "attend.hip", "evict.hip",
+           "linear4.hip", "accept.hip", "pages.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

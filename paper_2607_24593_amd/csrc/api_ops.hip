@@ -165,19 +165,95 @@ AttendArgs attend_shape(const pivot_attend_args* a) {
   return k;
 }
 
-// Launches of an attention call; f(launch arguments, table, b0, row0).
+// Launches of an attention call; f(launch arguments, table, b0, row0).  The table's
+// n_k are the positions that its rows may attend to: up to the last one's own, in a
+// tree up to the sequence's last node.
 template <class F>
-pivot_status attend_pieces(const pivot_attend_args* a, F f) {
+pivot_status attend_pieces(const pivot_attend_args* a, bool tree, F f) {
   const auto cost = [&](int b) -> int64_t {  // bytes of kept scores per query row
     if (!a->acc) return 0;
     const int64_t keys = a->idx ? a->topk : a->n_k[b];
     return (keys + 31) / 32 * 32 * 4 * a->heads;
   };
   return for_pieces(a->batch, a->n_q, a->cu_q, a->q_pos0, a->n_k, kMaxLaunchRows, kScoreBudget, cost,
-                    [&](const RunTable& t, int b0, int64_t row0, int rows) -> pivot_status {
+                    [&](const RunTable& piece, int b0, int64_t row0, int rows) -> pivot_status {
                       if (rows == 0) return PIVOT_OK;
+                      RunTable t = piece;
+                      for (int u = 0; u < t.n; ++u)
+                        t.n_k[u] = tree ? a->q_pos0[b0 + u] + run_rows(a->cu_q, a->n_q, b0 + u) : t.pos0[u] + t.n_rows[u];
                       return f(t, b0, row0);
                     });
+}
+
+pivot_status check_tree(const pivot_attend_args* a, const pivot_tree* tree) {
+  if (!tree) return fail(PIVOT_ERR_INVALID_ARG, "tree is NULL");
+  if (tree->words < 1 || tree->words > kTreeWords)
+    return fail(PIVOT_ERR_UNSUPPORTED, "words=%d must be in [1, %d]", tree->words, kTreeWords);
+  for (int b = 0; b < a->batch; ++b)
+    if (run_rows(a->cu_q, a->n_q, b) > 32 * tree->words)
+      return fail(PIVOT_ERR_INVALID_ARG, "sequence %d has %d nodes, a mask %d bits", b, run_rows(a->cu_q, a->n_q, b),
+                  32 * tree->words);
+  return PIVOT_OK;
+}
+
+size_t attend_need(const pivot_attend_args* a, bool tree) {
+  size_t need = 0;
+  const AttendArgs k = attend_shape(a);
+  attend_pieces(a, tree, [&](const RunTable& t, int, int64_t) -> pivot_status {
+    need = std::max(need, attend_workspace(k, t));
+    return PIVOT_OK;
+  });
+  return need;
+}
+
+// The call with its shapes (and the tree's) checked.
+pivot_status attend(const pivot_attend_args* a, const pivot_tree* tree) {
+  int64_t rows = 0, longest = 0;
+  for (int b = 0; b < a->batch; ++b) {
+    rows += run_rows(a->cu_q, a->n_q, b);
+    longest = std::max<int64_t>(longest, a->n_k[b]);
+  }
+  if (rows == 0) return PIVOT_OK;
+  const pivot_status s = check_cache(a->cache, a->batch, longest);
+  if (s != PIVOT_OK) return s;
+  if (!a->q || !a->out) return fail(PIVOT_ERR_INVALID_ARG, "q and out are required");
+  if (!aligned(a->q, 16) || !aligned(a->out, 16)) return fail(PIVOT_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
+  if (a->q_head_stride < kAttnDim || a->q_head_stride % 8 || a->q_row_stride % 8 ||
+      a->q_row_stride < (int64_t)(a->heads - 1) * a->q_head_stride + kAttnDim)
+    return fail(PIVOT_ERR_INVALID_ARG, "q strides (%lld, %lld): multiples of 8 values that keep rows apart",
+                (long long)a->q_row_stride, (long long)a->q_head_stride);
+  if (a->acc && a->acc_stride < longest)
+    return fail(PIVOT_ERR_INVALID_ARG, "acc_stride=%lld < %lld tokens", (long long)a->acc_stride, (long long)longest);
+  if (tree && (!tree->mask || !aligned(tree->mask, 4)))
+    return fail(PIVOT_ERR_INVALID_ARG, "the tree's mask is required, 4-byte aligned");
+  const size_t need = attend_need(a, tree != nullptr);
+  if (need > 0) {
+    if (!a->workspace || a->workspace_bytes < need)
+      return fail(PIVOT_ERR_WORKSPACE, "the call needs %zu workspace bytes", need);
+    if (!aligned(a->workspace, kAlign)) return fail(PIVOT_ERR_INVALID_ARG, "workspace must be %zu-byte aligned", kAlign);
+  }
+  return attend_pieces(a, tree != nullptr, [&](const RunTable& t, int b0, int64_t row0) -> pivot_status {
+    AttendArgs k = attend_shape(a);
+    int64_t first;
+    k.map = key_map(a->cache.map, b0, &first);
+    k.cache = cache_at(a->cache, first);
+    k.q = (const uint16_t*)a->q + row0 * a->q_row_stride;
+    k.q_row = a->q_row_stride;
+    k.q_head = a->q_head_stride;
+    if (a->idx) k.idx = a->idx + row0 * a->topk;
+    k.out = (uint16_t*)a->out + row0 * a->heads * kLatent;
+    k.lse = a->lse ? a->lse + row0 * a->heads : nullptr;
+    k.acc = a->acc ? a->acc + (int64_t)b0 * a->acc_stride : nullptr;
+    k.acc_stride = a->acc_stride;
+    k.workspace = a->workspace;
+    TreeMask m{};
+    if (tree) {
+      m.bits = tree->mask + row0 * tree->words;
+      m.words = tree->words;
+      for (int u = 0; u < t.n; ++u) m.base[u] = a->q_pos0[b0 + u];
+    }
+    return hip_check(launch_attend(k, t, tree ? &m : nullptr, (hipStream_t)a->stream), "attention kernels");
+  });
 }
 
 pivot_status check_evict_shape(const pivot_evict_args* a) {
@@ -210,6 +286,125 @@ RunTable evict_table(const pivot_evict_args* a, int b0) {
   t.n = std::min(kMaxSeq, a->batch - b0);
   for (int u = 0; u < t.n; ++u) t.n_k[u] = a->n_k[b0 + u];
   return t;
+}
+
+pivot_status check_rows(int n_arrays, const pivot_rows* arrays) {
+  if (n_arrays < 1 || n_arrays > PIVOT_EVICT_MAX_ARRAYS || !arrays)
+    return fail(PIVOT_ERR_INVALID_ARG, "n_arrays=%d must be in [1, %d]", n_arrays, PIVOT_EVICT_MAX_ARRAYS);
+  for (int i = 0; i < n_arrays; ++i) {
+    const pivot_rows& r = arrays[i];
+    if (!r.rows) return fail(PIVOT_ERR_INVALID_ARG, "array %d: null pointer", i);
+    if (r.row_bytes < 4 || r.row_bytes % 4 || !aligned(r.rows, 4))
+      return fail(PIVOT_ERR_INVALID_ARG, "array %d: rows of %d bytes (a multiple of 4, 4-byte aligned)", i, r.row_bytes);
+  }
+  return PIVOT_OK;
+}
+
+pivot_status check_pages(const pivot_pages* p) {
+  if (!p) return fail(PIVOT_ERR_INVALID_ARG, "pages is NULL");
+  const int P = p->page_size;
+  if (P < 16 || P > 65536 || (P & (P - 1)))
+    return fail(PIVOT_ERR_INVALID_ARG, "page_size=%d must be a power of two in [16, 65536]", P);
+  if (p->slots < 1 || p->max_pages < 1 || (int64_t)p->slots * p->max_pages > 0x7FFFFFFF)
+    return fail(PIVOT_ERR_INVALID_ARG, "a table of %d slots x %d pages", p->slots, p->max_pages);
+  if (p->n_pages < 1 || (int64_t)p->n_pages * P > 0x7FFFFFFF)
+    return fail(PIVOT_ERR_INVALID_ARG, "a pool of %d pages", p->n_pages);
+  return PIVOT_OK;
+}
+pivot_status check_pool(const pivot_pages* p) {
+  if (!p->table || !p->refs || !aligned(p->table, 4) || !aligned(p->refs, 4))
+    return fail(PIVOT_ERR_INVALID_ARG, "table and refs are required, 4-byte aligned");
+  return PIVOT_OK;
+}
+
+pivot_status check_list(const pivot_pages* p, int n) {
+  const pivot_status s = check_pages(p);
+  if (s != PIVOT_OK) return s;
+  if (n < 0) return fail(PIVOT_ERR_INVALID_ARG, "n must be >= 0");
+  if (n > PIVOT_PAGES_MAX_LIST) return fail(PIVOT_ERR_UNSUPPORTED, "n=%d exceeds %d", n, PIVOT_PAGES_MAX_LIST);
+  return PIVOT_OK;
+}
+// Slots of a list, distinct where they have to be (sorted: room for n values).
+pivot_status check_slots(const pivot_pages* p, int n, const int32_t* slot, int32_t* sorted, const char* what) {
+  if (!slot) return fail(PIVOT_ERR_INVALID_ARG, "%s (host array) is required", what);
+  for (int i = 0; i < n; ++i)
+    if (slot[i] < 0 || slot[i] >= p->slots) return fail(PIVOT_ERR_INVALID_ARG, "%s[%d]=%d of %d", what, i, slot[i], p->slots);
+  if (!sorted) return PIVOT_OK;
+  std::copy(slot, slot + n, sorted);
+  std::sort(sorted, sorted + n);
+  for (int i = 1; i < n; ++i)
+    if (sorted[i] == sorted[i - 1]) return fail(PIVOT_ERR_INVALID_ARG, "%s holds slot %d twice", what, sorted[i]);
+  return PIVOT_OK;
+}
+// 0 <= low[i] <= high[i] <= what a slot can hold (low NULL: 0).
+pivot_status check_tokens(const pivot_pages* p, int n, const int32_t* low, const int32_t* high) {
+  if (!high) return fail(PIVOT_ERR_INVALID_ARG, "the numbers of tokens (host arrays) are required");
+  for (int i = 0; i < n; ++i) {
+    if ((low && low[i] < 0) || high[i] < (low ? low[i] : 0))
+      return fail(PIVOT_ERR_INVALID_ARG, "entry %d: %d and %d tokens", i, low ? low[i] : 0, high[i]);
+    if (high[i] > (int64_t)p->max_pages * p->page_size)
+      return fail(PIVOT_ERR_INVALID_ARG, "entry %d: %d tokens exceed max_pages*page_size", i, high[i]);
+  }
+  return PIVOT_OK;
+}
+
+Pages pages_at(const pivot_pages* p) {
+  return Pages{p->table, p->refs, p->max_pages, p->n_pages, __builtin_ctz((unsigned)p->page_size)};
+}
+PageList page_list(int n, const int32_t* slot, const int32_t* a, const int32_t* b) {
+  PageList l{};
+  l.n = n;
+  std::copy(slot, slot + n, l.slot);
+  std::copy(a, a + n, l.a);
+  std::copy(b, b + n, l.b);
+  return l;
+}
+// Pages that a growth takes at most.
+int64_t pages_wanted(const pivot_pages* p, int n, const int32_t* tokens, const int32_t* new_tokens) {
+  const int64_t P = p->page_size;
+  int64_t want = 0;
+  for (int i = 0; i < n; ++i)
+    want += (new_tokens[i] + P - 1) / P - (tokens[i] + P - 1) / P + (new_tokens[i] > tokens[i] && tokens[i] % P != 0);
+  return std::min<int64_t>(want, p->n_pages);
+}
+
+// The checks of a product that concern shapes, not pointers.
+pivot_status check_linear4(const pivot_linear4_args* a) {
+  if (!a) return fail(PIVOT_ERR_INVALID_ARG, "args is NULL");
+  if (a->x_dtype != PIVOT_DT_BF16 && a->x_dtype != PIVOT_DT_FP8_E4M3)
+    return fail(PIVOT_ERR_UNSUPPORTED, "x_dtype %d: bf16 or fp8", a->x_dtype);
+  if (a->out_dtype != PIVOT_DT_BF16 && a->out_dtype != PIVOT_DT_FP32)
+    return fail(PIVOT_ERR_UNSUPPORTED, "out_dtype %d: bf16 or fp32", a->out_dtype);
+  if (a->n_rows < 0 || a->n < 0) return fail(PIVOT_ERR_INVALID_ARG, "n_rows and n must be >= 0");
+  if (a->k < 1) return fail(PIVOT_ERR_INVALID_ARG, "k must be >= 1");
+  if (a->k % kBlk || a->k > PIVOT_LINEAR4_MAX_K)
+    return fail(PIVOT_ERR_UNSUPPORTED, "k=%d must be a multiple of %d up to %d", a->k, kBlk, PIVOT_LINEAR4_MAX_K);
+  if (a->group != 0 && (a->group != 128 || a->x_dtype != PIVOT_DT_FP8_E4M3))
+    return fail(PIVOT_ERR_UNSUPPORTED, "group=%d: 0 (the row), or 128 with fp8", a->group);
+  if (a->ld_x < a->k || a->ld_out < a->n)
+    return fail(PIVOT_ERR_INVALID_ARG, "rows overlap (ld_x=%lld, ld_out=%lld)", (long long)a->ld_x, (long long)a->ld_out);
+  return PIVOT_OK;
+}
+
+// Launches of a product: f(arguments of at most kLinearRows rows, its first row).
+template <class F>
+pivot_status linear4_pieces(const pivot_linear4_args* a, F f) {
+  Linear4Args k{};
+  k.ld_x = a->ld_x;
+  k.x_fp8 = a->x_dtype == PIVOT_DT_FP8_E4M3;
+  k.group = a->group;
+  k.n = a->n;
+  k.k = a->k;
+  k.codes = (const uint8_t*)a->codes;
+  k.scales = (const uint8_t*)a->scales;
+  k.ld_out = a->ld_out;
+  k.out_fp32 = a->out_dtype == PIVOT_DT_FP32;
+  for (int64_t r = 0; r < a->n_rows && a->n > 0; r += kLinearRows) {
+    k.rows = (int32_t)std::min<int64_t>(kLinearRows, a->n_rows - r);
+    const pivot_status s = f(k, r);
+    if (s != PIVOT_OK) return s;
+  }
+  return PIVOT_OK;
 }
 
 }  // namespace
@@ -289,57 +484,59 @@ pivot_status pivot_cache4_read(const pivot_cache4* c, int32_t batch, int32_t n, 
 }
 
 size_t pivot_cache4_attend_workspace_size(const pivot_attend_args* a) {
-  if (check_attend_shape(a) != PIVOT_OK) return 0;
-  size_t need = 0;
-  AttendArgs k = attend_shape(a);
-  attend_pieces(a, [&](const RunTable& t, int, int64_t) -> pivot_status {
-    need = std::max(need, attend_workspace(k, t));
-    return PIVOT_OK;
-  });
-  return need;
+  return check_attend_shape(a) == PIVOT_OK ? attend_need(a, false) : 0;
 }
 
 pivot_status pivot_cache4_attend(const pivot_attend_args* a) {
+  const pivot_status s = check_attend_shape(a);
+  return s == PIVOT_OK ? attend(a, nullptr) : s;
+}
+
+size_t pivot_cache4_attend_tree_workspace_size(const pivot_attend_args* a, const pivot_tree* t) {
+  return check_attend_shape(a) == PIVOT_OK && check_tree(a, t) == PIVOT_OK ? attend_need(a, true) : 0;
+}
+
+pivot_status pivot_cache4_attend_tree(const pivot_attend_args* a, const pivot_tree* t) {
   pivot_status s = check_attend_shape(a);
-  if (s != PIVOT_OK) return s;
-  int64_t rows = 0, longest = 0;
-  for (int b = 0; b < a->batch; ++b) {
-    rows += run_rows(a->cu_q, a->n_q, b);
-    longest = std::max<int64_t>(longest, a->n_k[b]);
+  if (s == PIVOT_OK) s = check_tree(a, t);
+  return s == PIVOT_OK ? attend(a, t) : s;
+}
+
+pivot_status pivot_tree_accept(int32_t batch, int32_t n, const int32_t* path, const int32_t* pos0, int32_t n_arrays,
+                               const pivot_rows* arrays, const pivot_row_map* map, void* stream) {
+  if (batch < 1 || n < 0) return fail(PIVOT_ERR_INVALID_ARG, "batch must be >= 1 and n >= 0");
+  if (n > PIVOT_TREE_MAX_NODES) return fail(PIVOT_ERR_UNSUPPORTED, "n=%d exceeds %d nodes", n, PIVOT_TREE_MAX_NODES);
+  if (!pos0 || !map) return fail(PIVOT_ERR_INVALID_ARG, "pos0 (host array) and map are required");
+  int64_t longest = 0;
+  for (int b = 0; b < batch; ++b) {
+    if (pos0[b] < 0) return fail(PIVOT_ERR_INVALID_ARG, "position %d of sequence %d is negative", pos0[b], b);
+    if (pos0[b] > PIVOT_MAX_KEYS) return fail(PIVOT_ERR_UNSUPPORTED, "sequence %d exceeds PIVOT_MAX_KEYS=%d", b, PIVOT_MAX_KEYS);
+    longest = std::max<int64_t>(longest, pos0[b]);
   }
-  if (rows == 0) return PIVOT_OK;
-  s = check_cache(a->cache, a->batch, longest);
+  pivot_status s = check_map(*map, batch, longest, "map");
   if (s != PIVOT_OK) return s;
-  if (!a->q || !a->out) return fail(PIVOT_ERR_INVALID_ARG, "q and out are required");
-  if (!aligned(a->q, 16) || !aligned(a->out, 16)) return fail(PIVOT_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
-  if (a->q_head_stride < kAttnDim || a->q_head_stride % 8 || a->q_row_stride % 8 ||
-      a->q_row_stride < (int64_t)(a->heads - 1) * a->q_head_stride + kAttnDim)
-    return fail(PIVOT_ERR_INVALID_ARG, "q strides (%lld, %lld): multiples of 8 values that keep rows apart",
-                (long long)a->q_row_stride, (long long)a->q_head_stride);
-  if (a->acc && a->acc_stride < longest)
-    return fail(PIVOT_ERR_INVALID_ARG, "acc_stride=%lld < %lld tokens", (long long)a->acc_stride, (long long)longest);
-  const size_t need = pivot_cache4_attend_workspace_size(a);
-  if (need > 0) {
-    if (!a->workspace || a->workspace_bytes < need)
-      return fail(PIVOT_ERR_WORKSPACE, "the call needs %zu workspace bytes", need);
-    if (!aligned(a->workspace, kAlign)) return fail(PIVOT_ERR_INVALID_ARG, "workspace must be %zu-byte aligned", kAlign);
-  }
-  return attend_pieces(a, [&](const RunTable& t, int b0, int64_t row0) -> pivot_status {
-    AttendArgs k = attend_shape(a);
+  s = check_rows(n_arrays, arrays);
+  if (s != PIVOT_OK || n == 0) return s;
+  if (!path || !aligned(path, 4)) return fail(PIVOT_ERR_INVALID_ARG, "path is required, 4-byte aligned");
+  for (int b0 = 0; b0 < batch; b0 += kMaxSeq) {
+    RunTable t{};
+    t.n = std::min(kMaxSeq, batch - b0);
+    for (int u = 0; u < t.n; ++u) t.pos0[u] = pos0[b0 + u];
+    AcceptArgs k{};
     int64_t first;
-    k.map = key_map(a->cache.map, b0, &first);
-    k.cache = cache_at(a->cache, first);
-    k.q = (const uint16_t*)a->q + row0 * a->q_row_stride;
-    k.q_row = a->q_row_stride;
-    k.q_head = a->q_head_stride;
-    if (a->idx) k.idx = a->idx + row0 * a->topk;
-    k.out = (uint16_t*)a->out + row0 * a->heads * kLatent;
-    k.lse = a->lse ? a->lse + row0 * a->heads : nullptr;
-    k.acc = a->acc ? a->acc + (int64_t)b0 * a->acc_stride : nullptr;
-    k.acc_stride = a->acc_stride;
-    k.workspace = a->workspace;
-    return hip_check(launch_attend(k, t, (hipStream_t)a->stream), "attention kernels");
-  });
+    k.path = path + (int64_t)b0 * n;
+    k.n = n;
+    k.limit = capacity(*map);
+    k.map = key_map(*map, b0, &first);
+    k.n_arrays = n_arrays;
+    for (int i = 0; i < n_arrays; ++i) {
+      k.rows[i] = (uint8_t*)arrays[i].rows + first * arrays[i].row_bytes;
+      k.row_bytes[i] = arrays[i].row_bytes;
+    }
+    s = hip_check(launch_accept(k, t, (hipStream_t)stream), "accept kernel");
+    if (s != PIVOT_OK) return s;
+  }
+  return PIVOT_OK;
 }
 
 size_t pivot_evict_workspace_size(const pivot_evict_args* a) {
@@ -399,6 +596,150 @@ pivot_status pivot_evict(const pivot_evict_args* a) {
     m.row_bytes[i] = a->arrays[i].row_bytes;
   }
   return hip_check(launch_move(m, from, to, a->out_keep, a->batch, a->keep, (hipStream_t)a->stream), "move kernel");
+}
+
+size_t pivot_linear4_workspace_size(const pivot_linear4_args* a) {
+  if (check_linear4(a) != PIVOT_OK) return 0;
+  size_t need = 0;
+  linear4_pieces(a, [&](const Linear4Args& k, int64_t) -> pivot_status {
+    need = std::max(need, linear4_workspace(k));
+    return PIVOT_OK;
+  });
+  return need;
+}
+
+pivot_status pivot_linear4(const pivot_linear4_args* a) {
+  const pivot_status s = check_linear4(a);
+  if (s != PIVOT_OK) return s;
+  if (a->n_rows == 0 || a->n == 0) return PIVOT_OK;
+  const bool fp8 = a->x_dtype == PIVOT_DT_FP8_E4M3, fp32 = a->out_dtype == PIVOT_DT_FP32;
+  if (!a->x || !a->codes || !a->scales || !a->out || (fp8 && !a->x_scale))
+    return fail(PIVOT_ERR_INVALID_ARG, "x, codes, scales, out and fp8's x_scale are required");
+  if (!aligned(a->codes, 16)) return fail(PIVOT_ERR_INVALID_ARG, "codes must be 16-byte aligned");
+  if ((!fp8 && !aligned(a->x, 2)) || (fp8 && !aligned(a->x_scale, 4)) || !aligned(a->out, fp32 ? 4 : 2))
+    return fail(PIVOT_ERR_INVALID_ARG, "a pointer is not aligned to its elements");
+  const size_t need = pivot_linear4_workspace_size(a);
+  if (need > 0) {
+    if (!a->workspace || a->workspace_bytes < need)
+      return fail(PIVOT_ERR_WORKSPACE, "the call needs %zu workspace bytes", need);
+    if (!aligned(a->workspace, kAlign)) return fail(PIVOT_ERR_INVALID_ARG, "workspace must be %zu-byte aligned", kAlign);
+  }
+  return linear4_pieces(a, [&](Linear4Args k, int64_t r) -> pivot_status {
+    const int64_t scales = a->group ? (a->k + 127) / 128 : 1;
+    k.x = (const uint8_t*)a->x + r * a->ld_x * (fp8 ? 1 : 2);
+    k.x_scale = fp8 ? a->x_scale + r * scales : nullptr;
+    k.out = (uint8_t*)a->out + r * a->ld_out * (fp32 ? 4 : 2);
+    return hip_check(launch_linear4(k, a->workspace, (hipStream_t)a->stream), "linear kernels");
+  });
+}
+
+pivot_status pivot_linear4_pack(int32_t dtype, int32_t n, int32_t k, const void* w, int64_t ld_w, void* codes,
+                                void* scales, void* stream) {
+  if (dtype != PIVOT_DT_BF16 && dtype != PIVOT_DT_FP32)
+    return fail(PIVOT_ERR_UNSUPPORTED, "dtype %d: weights are bf16 or fp32", dtype);
+  if (n < 0 || k < 1) return fail(PIVOT_ERR_INVALID_ARG, "n must be >= 0 and k >= 1");
+  if (k % kBlk || k > PIVOT_LINEAR4_MAX_K)
+    return fail(PIVOT_ERR_UNSUPPORTED, "k=%d must be a multiple of %d up to %d", k, kBlk, PIVOT_LINEAR4_MAX_K);
+  if (ld_w < k) return fail(PIVOT_ERR_INVALID_ARG, "rows overlap (ld_w=%lld)", (long long)ld_w);
+  if (n == 0) return PIVOT_OK;
+  if (!w || !codes || !scales) return fail(PIVOT_ERR_INVALID_ARG, "w, codes and scales are required");
+  if (!aligned(w, dtype == PIVOT_DT_BF16 ? 2 : 4) || !aligned(codes, 4))
+    return fail(PIVOT_ERR_INVALID_ARG, "w must be aligned to its elements, codes to 4 bytes");
+  return hip_check(launch_linear4_pack(dtype == PIVOT_DT_FP32, n, k, w, ld_w, (uint8_t*)codes, (uint8_t*)scales,
+                                       (hipStream_t)stream),
+                   "pack kernel");
+}
+
+pivot_status pivot_pages_fork(const pivot_pages* p, int32_t n, const int32_t* src, const int32_t* dst,
+                              const int32_t* tokens, void* stream) {
+  pivot_status s = check_list(p, n);
+  if (s != PIVOT_OK) return s;
+  if (n == 0) return PIVOT_OK;
+  int32_t sorted[PIVOT_PAGES_MAX_LIST];
+  if ((s = check_slots(p, n, src, nullptr, "src")) != PIVOT_OK) return s;
+  if ((s = check_slots(p, n, dst, sorted, "dst")) != PIVOT_OK) return s;
+  for (int i = 0; i < n; ++i)
+    if (std::binary_search(sorted, sorted + n, src[i]))
+      return fail(PIVOT_ERR_INVALID_ARG, "slot %d is both src and dst", src[i]);
+  if ((s = check_tokens(p, n, nullptr, tokens)) != PIVOT_OK) return s;
+  if ((s = check_pool(p)) != PIVOT_OK) return s;
+  return hip_check(launch_pages_fork(pages_at(p), page_list(n, src, dst, tokens), (hipStream_t)stream), "fork kernel");
+}
+
+pivot_status pivot_pages_free(const pivot_pages* p, int32_t n, const int32_t* slot, const int32_t* tokens,
+                              const int32_t* keep, void* stream) {
+  pivot_status s = check_list(p, n);
+  if (s != PIVOT_OK) return s;
+  if (n == 0) return PIVOT_OK;
+  int32_t sorted[PIVOT_PAGES_MAX_LIST];
+  if ((s = check_slots(p, n, slot, sorted, "slot")) != PIVOT_OK) return s;
+  if (!keep) return fail(PIVOT_ERR_INVALID_ARG, "the numbers of tokens (host arrays) are required");
+  if ((s = check_tokens(p, n, keep, tokens)) != PIVOT_OK) return s;
+  if ((s = check_pool(p)) != PIVOT_OK) return s;
+  return hip_check(launch_pages_free(pages_at(p), page_list(n, slot, tokens, keep), (hipStream_t)stream), "free kernel");
+}
+
+size_t pivot_pages_grow_workspace_size(const pivot_pages* p, int32_t n, const int32_t* tokens, const int32_t* new_tokens) {
+  if (check_list(p, n) != PIVOT_OK || n == 0 || !tokens || check_tokens(p, n, tokens, new_tokens) != PIVOT_OK) return 0;
+  return pages_grow_workspace(pages_at(p), pages_wanted(p, n, tokens, new_tokens));
+}
+
+pivot_status pivot_pages_grow(const pivot_pages* p, int32_t n, const int32_t* slot, const int32_t* tokens,
+                              const int32_t* new_tokens, int32_t* copies, int32_t* state, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+  pivot_status s = check_list(p, n);
+  if (s != PIVOT_OK) return s;
+  if (n == 0) return fail(PIVOT_ERR_INVALID_ARG, "n must be >= 1");
+  int32_t sorted[PIVOT_PAGES_MAX_LIST];
+  if ((s = check_slots(p, n, slot, sorted, "slot")) != PIVOT_OK) return s;
+  if (!tokens) return fail(PIVOT_ERR_INVALID_ARG, "the numbers of tokens (host arrays) are required");
+  if ((s = check_tokens(p, n, tokens, new_tokens)) != PIVOT_OK) return s;
+  if ((s = check_pool(p)) != PIVOT_OK) return s;
+  if (!copies || !state || !aligned(copies, 4) || !aligned(state, 4))
+    return fail(PIVOT_ERR_INVALID_ARG, "copies and state are required, 4-byte aligned");
+  const size_t need = pivot_pages_grow_workspace_size(p, n, tokens, new_tokens);
+  if (!workspace || workspace_bytes < need) return fail(PIVOT_ERR_WORKSPACE, "the call needs %zu workspace bytes", need);
+  if (!aligned(workspace, kAlign)) return fail(PIVOT_ERR_INVALID_ARG, "workspace must be %zu-byte aligned", kAlign);
+  return hip_check(launch_pages_grow(pages_at(p), page_list(n, slot, tokens, new_tokens), copies, state, workspace,
+                                     (hipStream_t)stream),
+                   "grow kernels");
+}
+
+size_t pivot_pages_compact_workspace_size(const pivot_pages* p) {
+  return check_pages(p) == PIVOT_OK ? pages_compact_workspace(pages_at(p)) : 0;
+}
+
+pivot_status pivot_pages_compact(const pivot_pages* p, int32_t max_moves, int32_t* moves, int32_t* state, void* workspace,
+                                 size_t workspace_bytes, void* stream) {
+  pivot_status s = check_pages(p);
+  if (s != PIVOT_OK) return s;
+  if (max_moves < 0) return fail(PIVOT_ERR_INVALID_ARG, "max_moves must be >= 0");
+  if ((s = check_pool(p)) != PIVOT_OK) return s;
+  if (!state || (!moves && max_moves > 0) || !aligned(moves, 4) || !aligned(state, 4))
+    return fail(PIVOT_ERR_INVALID_ARG, "moves and state are required, 4-byte aligned");
+  const size_t need = pivot_pages_compact_workspace_size(p);
+  if (!workspace || workspace_bytes < need) return fail(PIVOT_ERR_WORKSPACE, "the call needs %zu workspace bytes", need);
+  if (!aligned(workspace, kAlign)) return fail(PIVOT_ERR_INVALID_ARG, "workspace must be %zu-byte aligned", kAlign);
+  return hip_check(launch_pages_compact(pages_at(p), p->slots, max_moves, moves, state, workspace, (hipStream_t)stream),
+                   "compact kernels");
+}
+
+pivot_status pivot_pages_copy(const pivot_pages* p, int32_t n, const int32_t* pairs, int32_t n_arrays,
+                              const pivot_rows* arrays, void* stream) {
+  pivot_status s = check_pages(p);
+  if (s != PIVOT_OK) return s;
+  if (n < 0) return fail(PIVOT_ERR_INVALID_ARG, "n must be >= 0");
+  if ((s = check_rows(n_arrays, arrays)) != PIVOT_OK || n == 0) return s;
+  if (!pairs || !aligned(pairs, 4)) return fail(PIVOT_ERR_INVALID_ARG, "pairs is required, 4-byte aligned");
+  PageRows k{};
+  k.n_pages = p->n_pages;
+  k.shift = __builtin_ctz((unsigned)p->page_size);
+  k.n = n_arrays;
+  for (int i = 0; i < n_arrays; ++i) {
+    k.rows[i] = (uint8_t*)arrays[i].rows;
+    k.row_bytes[i] = arrays[i].row_bytes;
+  }
+  return hip_check(launch_pages_copy(k, n, pairs, (hipStream_t)stream), "copy kernel");
 }
 
 }  // extern "C"

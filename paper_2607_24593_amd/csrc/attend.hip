@@ -5,10 +5,13 @@
 //   acc[b, s] += sum_{r, h} softmax(z[r, h])[s]             optional
 //
 // A row with no key (an empty set, or only scores of -infinity) has o = 0 and
-// lse = -infinity and adds nothing to acc.
+// lse = -infinity and adds nothing to acc.  Rows that are a tree of drafted tokens
+// attend to the positions before the tree's first, and to those of its nodes that
+// their masks name.
 //
 // Scores are kept in base 2 (z log2 e), statistics and sums in fp32.
 #include <algorithm>
+#include <type_traits>
 #include <utility>
 
 #include "cache4.h"
@@ -199,13 +202,17 @@ __device__ __forceinline__ int owner_of(const int32_t* first, int n, int i) {
 }
 // splits of a sequence's keys
 __host__ __device__ inline int splits_of(const RunTable& t, int b, int tiles_per_split) {
-  const int tiles = (t.pos0[b] + t.n_rows[b] + kTileKeys - 1) / kTileKeys;
+  const int tiles = (t.n_k[b] + kTileKeys - 1) / kTileKeys;
   return tiles > tiles_per_split ? (tiles + tiles_per_split - 1) / tiles_per_split : 1;
 }
 
-template <int RG>
-__global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, RunTable t, ScoreMap sm,
-                                                                              Work wk) {
+struct NoTree {};
+template <bool TREE>
+using TreeOf = std::conditional_t<TREE, TreeMask, NoTree>;
+
+template <int RG, bool TREE>
+__global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, RunTable t, ScoreMap sm, Work wk,
+                                                                TreeOf<TREE> tree) {
   constexpr bool ONE = RG == 8;                // one barrier per tile
   constexpr int ROWS = 16 * RG;
   constexpr int KT = kTileKeys;
@@ -231,6 +238,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
   __shared__ __attribute__((aligned(16))) float s_part[ONE ? 4 : 2 * DG * ROWS * PR];
   __shared__ int s_entry[ONE ? 1 : 4 * 64], s_page[ONE ? 1 : 4 * 64];  // of 8 tiles' keys, on their way
   __shared__ float s_alpha[2][ROWS], s_max[ROWS], s_sum[ROWS];
+  // of a tree: the word that a row's mask starts at (prefix calls), the mask of the
+  // unit's query (index sets)
+  __shared__ int s_tree[TREE ? ROWS : 1];
+  __shared__ uint32_t s_mask[TREE ? kTreeWords : 1];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -246,9 +257,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
   const int first = rt * ROWS;
   const int rows = min(ROWS, unit_rows - first);
   const int i_first = sets ? unit - t.row0[b] : 0;                       // the unit's first query in its sequence
-  const int pos_last = t.pos0[b] + (sets ? i_first : (first + rows - 1) / a.heads);
+  const int pos_last = TREE ? t.n_k[b] - 1 : t.pos0[b] + (sets ? i_first : (first + rows - 1) / a.heads);
   // kept scores cover the unit's keys for every row
-  const int n = sets ? a.topk : sm.s2 ? t.pos0[b] + t.n_rows[b] : pos_last + 1;
+  const int n = sets ? a.topk : sm.s2 ? t.n_k[b] : pos_last + 1;
   const int all_tiles = (n + KT - 1) / KT;
   const int t0 = split * wk.tiles_per_split, t1 = min(all_tiles, t0 + wk.tiles_per_split);
   if (t0 >= t1 && splits > 1) {
@@ -388,7 +399,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
   {
     const int mine = row0 + (lane & 15), flat = first + min(mine, rows - 1), g = lane >> 4;
     const int i = sets ? 0 : flat / a.heads, head = flat - i * a.heads;
-    if constexpr (ONE) {
+    if constexpr (TREE) {  // the last position before the tree
+      limit = (ONE ? mine : tid / LPR) < rows ? tree.base[b] - 1 : -1;
+      const int r = min(tid, rows - 1);
+      if (tid < ROWS) s_tree[tid] = (t.row0[b] + i_first + (sets ? 0 : (first + r) / a.heads)) * tree.words;
+      if (sets && tid < tree.words) s_mask[tid] = tree.bits[(int64_t)(t.row0[b] + i_first) * tree.words + tid];
+    } else if constexpr (ONE) {
       limit = mine < rows ? t.pos0[b] + i_first + i : -1;
     } else {
       const int r = tid / LPR;
@@ -519,18 +535,49 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
     });
   };
 
+  // whether a key's masking position is a node of the tree, and whether a row's mask
+  // names it (padded rows share the last row's mask: nothing of theirs is put out)
+  auto is_draft = [&](int key_at) {
+    if constexpr (TREE) return key_at >= tree.base[b] && key_at != 0x7FFFFFFF;
+    return false;
+  };
+  auto named = [&](int row, int key_at) {
+    if constexpr (TREE) {
+      const int node = key_at - tree.base[b];
+      if ((uint32_t)node >= (uint32_t)(32 * tree.words)) return false;
+      const uint32_t word = sets ? s_mask[node >> 5] : tree.bits[s_tree[row] + (node >> 5)];
+      return (word >> (node & 31) & 1u) != 0u;
+    }
+    return false;
+  };
+
   // the scores in base 2, masked, and the row's largest; tile: the unit's tile, for the kept scores
   float top = 0.f;
   auto finish_scores = [&](int ln, int tile, int slot) {
     const int key = ln & 15, g = ln >> 4;
     top = -INFINITY;
+    bool drafts = false;
+    if constexpr (TREE) drafts = !sets && (tile + 1) * KT > tree.base[b];
+    if (TREE && sets) {
+      bool any = false;
+#pragma unroll
+      for (int j = 0; j < NKT; ++j) {
+        const v4i key_at = *reinterpret_cast<const v4i*>(&s_pos[slot * KT + 16 * j + 4 * g]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) any = any || is_draft(key_at[i]);
+      }
+      drafts = any;
+    }
+    drafts = TREE && __any(drafts);
 #pragma unroll
     for (int j = 0; j < NKT; ++j) {
       const int k4 = 16 * j + 4 * g;
       const v4i key_at = *reinterpret_cast<const v4i*>(&s_pos[slot * KT + k4]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        s[j][i] = key_at[i] <= limit ? s[j][i] * c : -INFINITY;
+        bool seen = key_at[i] <= limit;
+        if (TREE && drafts) seen = seen || named(row0 + key, key_at[i]);
+        s[j][i] = seen ? s[j][i] * c : -INFINITY;
         top = fmaxf(top, s[j][i]);
       }
       if (s2 && tile < t1 && row0 + key < rows)
@@ -628,12 +675,20 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
   auto weigh_part = [&](int td, int wslot) {
     const int row = td / LPR, k0 = td % LPR * KPT;
     float z[KPT], e[KPT], top = -INFINITY;
+    bool drafts = false;
+    if constexpr (TREE) {
+#pragma unroll
+      for (int i = 0; i < KPT; ++i) drafts = drafts || is_draft(key_at[i]);
+      drafts = __any(drafts);
+    }
 #pragma unroll
     for (int i = 0; i < KPT; ++i) {
       z[i] = zp[i][0];
 #pragma unroll
       for (int d = 1; d < DG; ++d) z[i] += zp[i][d];
-      z[i] = key_at[i] <= limit ? z[i] * c : -INFINITY;
+      bool seen = key_at[i] <= limit;
+      if (TREE && drafts) seen = seen || named(row, key_at[i]);
+      z[i] = seen ? z[i] * c : -INFINITY;
       top = fmaxf(top, z[i]);
     }
     top = row_reduce<LPR>(top, [](float x, float y) { return fmaxf(x, y); });
@@ -1081,13 +1136,16 @@ __global__ __launch_bounds__(64 * kWaves) void join_kernel(AttendArgs a, RunTabl
 
 // Sum over a tile's rows from `least` on, those that attend to the thread's key,
 // of the softmax weights of its 32 keys: 8 rows at a time, each thread one key,
-// the rows of a thread in ascending order.  The rows before are left out, not
-// added as zeros: the masked scores of a NaN row give NaN.
+// the rows of a thread in ascending order.  The rows before (and those that skip(r)
+// holds for) are left out, not added as zeros: the masked scores of a NaN row give
+// NaN.
+template <class Skip>
 __device__ __forceinline__ float tile_weight(const float* tile, const float2* stat, int least, int rows, float* red,
-                                             int tid) {
+                                             int tid, Skip skip) {
   const int k = tid & 31, first = tid >> 5;
   float w = 0.f;
   for (int r = first + (max(least - first, 0) + 7) / 8 * 8; r < rows; r += 8) {
+    if (skip(r)) continue;
     const float2 st = stat[r];
     w = fmaf(exp2f(tile[r * kTileKeys + k] - st.x), st.y, w);
   }
@@ -1100,14 +1158,25 @@ __device__ __forceinline__ float tile_weight(const float* tile, const float2* st
   return w;
 }
 
-__global__ __launch_bounds__(256) void dense_weights_kernel(AttendArgs a, RunTable t, ScoreMap sm) {
+template <bool TREE>
+__global__ __launch_bounds__(256) void dense_weights_kernel(AttendArgs a, RunTable t, ScoreMap sm, TreeOf<TREE> tree) {
   __shared__ float red[256];
   const int b = blockIdx.y, tile = blockIdx.x, tid = threadIdx.x;
-  const int n = t.pos0[b] + t.n_rows[b], rows = t.n_rows[b] * a.heads;
+  const int n = t.n_k[b], rows = t.n_rows[b] * a.heads;
   if (rows == 0 || tile * kTileKeys >= n) return;
-  const int least = max(tile * kTileKeys + (tid & 31) - t.pos0[b], 0) * a.heads;
-  const float w = tile_weight(sm.s2 + sm.base[b] + (int64_t)tile * rows * kTileKeys,
-                              sm.stat + (int64_t)t.row0[b] * a.heads, least, rows, red, tid);
+  const float* scores = sm.s2 + sm.base[b] + (int64_t)tile * rows * kTileKeys;
+  const float2* stat = sm.stat + (int64_t)t.row0[b] * a.heads;
+  const int key = tile * kTileKeys + (tid & 31);
+  float w;
+  if constexpr (TREE) {
+    const int node = key - tree.base[b];
+    const bool draft = node >= 0 && key < n;
+    const uint32_t* bits = tree.bits + (int64_t)t.row0[b] * tree.words + (draft ? node >> 5 : 0);
+    w = tile_weight(scores, stat, 0, rows, red, tid,
+                    [&](int r) { return draft && (bits[(int64_t)(r / a.heads) * tree.words] >> (node & 31) & 1u) == 0u; });
+  } else {
+    w = tile_weight(scores, stat, max(key - t.pos0[b], 0) * a.heads, rows, red, tid, [](int) { return false; });
+  }
   const int s = tile * kTileKeys + tid;
   if (tid < kTileKeys && s < n) a.acc[(int64_t)b * a.acc_stride + s] += w;
 }
@@ -1117,7 +1186,7 @@ __global__ __launch_bounds__(256) void slot_weights_kernel(AttendArgs a, ScoreMa
   __shared__ float red[256];
   const int r = blockIdx.y, tile = blockIdx.x, tid = threadIdx.x;
   const float w = tile_weight(sm.s2 + ((int64_t)r * padded + tile * kTileKeys) * a.heads,
-                              sm.stat + (int64_t)r * a.heads, 0, a.heads, red, tid);
+                              sm.stat + (int64_t)r * a.heads, 0, a.heads, red, tid, [](int) { return false; });
   if (tid < kTileKeys) slots[(int64_t)r * padded + tile * kTileKeys + tid] = w;
 }
 
@@ -1130,11 +1199,12 @@ __global__ __launch_bounds__(256) void slot_weights_kernel(AttendArgs a, ScoreMa
 constexpr int kRange = 8192;
 constexpr int kAddThreads = 1024;
 constexpr int kAhead = 4;
+template <bool TREE>
 __global__ __launch_bounds__(kAddThreads) void slot_add_kernel(AttendArgs a, RunTable t, const float* __restrict__ slots,
-                                                               int padded, int groups, float* parts) {
+                                                               int padded, int groups, float* parts, TreeOf<TREE> tree) {
   __shared__ float sum[kRange];
   const int b = blockIdx.y, tid = threadIdx.x, group = blockIdx.x % groups;
-  const int lo = blockIdx.x / groups * kRange, n = t.pos0[b] + t.n_rows[b];
+  const int lo = blockIdx.x / groups * kRange, n = t.n_k[b];
   if (t.n_rows[b] == 0 || lo >= n) return;
   const int each = (t.n_rows[b] + groups - 1) / groups, row0 = group * each;
   const int rows = max(0, min(each, t.n_rows[b] - row0));
@@ -1163,7 +1233,14 @@ __global__ __launch_bounds__(kAddThreads) void slot_add_kernel(AttendArgs a, Run
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int at = keys[j][e];
-        if (at >= 0 && at <= pos && (uint32_t)(at - lo) < (uint32_t)kRange) atomicAdd(&sum[at - lo], ws[j][e]);
+        bool seen = at >= 0 && at <= pos;
+        if constexpr (TREE) {
+          const int node = at - tree.base[b];
+          seen = at >= 0 && at < n;
+          if (seen && node >= 0)
+            seen = (tree.bits[(int64_t)(t.row0[b] + row0 + i) * tree.words + (node >> 5)] >> (node & 31) & 1u) != 0u;
+        }
+        if (seen && (uint32_t)(at - lo) < (uint32_t)kRange) atomicAdd(&sum[at - lo], ws[j][e]);
       }
       __syncthreads();
     }
@@ -1189,7 +1266,7 @@ __global__ __launch_bounds__(kAddThreads) void slot_add_kernel(AttendArgs a, Run
 __global__ __launch_bounds__(256) void group_add_kernel(AttendArgs a, RunTable t, int groups, const float* parts,
                                                         int64_t stride) {
   const int b = blockIdx.y, at = blockIdx.x * 256 + threadIdx.x;
-  if (t.n_rows[b] == 0 || at >= t.pos0[b] + t.n_rows[b]) return;
+  if (t.n_rows[b] == 0 || at >= t.n_k[b]) return;
   float sum = 0.f;
 #pragma unroll 8
   for (int g = 0; g < groups; ++g) sum += parts[((int64_t)b * groups + g) * stride + at];
@@ -1221,7 +1298,7 @@ Plan plan_of(const AttendArgs& a, const RunTable& t) {
   int max_rows = 0;
   p.padded = (a.topk + kTileKeys - 1) / kTileKeys * kTileKeys;
   for (int b = 0; b < t.n; ++b) {
-    const int n = t.pos0[b] + t.n_rows[b];
+    const int n = t.n_k[b];
     p.base[b] = words;
     if (t.n_rows[b]) {
       words += (int64_t)((n + kTileKeys - 1) / kTileKeys) * kTileKeys * t.n_rows[b] * a.heads;
@@ -1282,10 +1359,10 @@ Plan plan_of(const AttendArgs& a, const RunTable& t) {
   return p;
 }
 
-template <int RG>
+template <int RG, bool TREE>
 hipError_t launch_rows(const AttendArgs& a, const RunTable& t, const ScoreMap& sm, const Work& wk, unsigned workgroups,
-                       hipStream_t stream) {
-  hipLaunchKernelGGL(attend_kernel<RG>, dim3(workgroups), dim3(64 * kWaves), 0, stream, a, t, sm, wk);
+                       const TreeOf<TREE>& tree, hipStream_t stream) {
+  hipLaunchKernelGGL((attend_kernel<RG, TREE>), dim3(workgroups), dim3(64 * kWaves), 0, stream, a, t, sm, wk, tree);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || wk.splits == 1) return e;
   using J = Join<RG>;
@@ -1299,7 +1376,10 @@ hipError_t launch_rows(const AttendArgs& a, const RunTable& t, const ScoreMap& s
 
 size_t attend_workspace(const AttendArgs& a, const RunTable& t) { return plan_of(a, t).bytes(); }
 
-hipError_t launch_attend(const AttendArgs& a, const RunTable& t, hipStream_t stream) {
+namespace {
+
+template <bool TREE>
+hipError_t launch_call(const AttendArgs& a, const RunTable& t, const TreeOf<TREE>& tree, hipStream_t stream) {
   Plan p = plan_of(a, t);
   if (p.rows == 0) return hipSuccess;
   ScoreMap sm{};
@@ -1314,27 +1394,34 @@ hipError_t launch_attend(const AttendArgs& a, const RunTable& t, hipStream_t str
   uint8_t* parts = (uint8_t*)sums + round256(p.sums);
   p.wk.part_o = (float4*)parts;
   p.wk.part_ml = (float2*)(parts + round256(p.part_o));
-  hipError_t e = p.rg == 8   ? launch_rows<8>(a, t, sm, p.wk, (unsigned)p.workgroups, stream)
-                 : p.rg == 4 ? launch_rows<4>(a, t, sm, p.wk, (unsigned)p.workgroups, stream)
-                 : p.rg == 2 ? launch_rows<2>(a, t, sm, p.wk, (unsigned)p.workgroups, stream)
-                             : launch_rows<1>(a, t, sm, p.wk, (unsigned)p.workgroups, stream);
+  const unsigned wgs = (unsigned)p.workgroups;
+  hipError_t e = p.rg == 8   ? launch_rows<8, TREE>(a, t, sm, p.wk, wgs, tree, stream)
+                 : p.rg == 4 ? launch_rows<4, TREE>(a, t, sm, p.wk, wgs, tree, stream)
+                 : p.rg == 2 ? launch_rows<2, TREE>(a, t, sm, p.wk, wgs, tree, stream)
+                             : launch_rows<1, TREE>(a, t, sm, p.wk, wgs, tree, stream);
   if (e != hipSuccess || !a.acc || (a.idx && a.topk == 0)) return e;
   if (!a.idx) {
     const unsigned tiles = (unsigned)((p.max_n + kTileKeys - 1) / kTileKeys);
-    hipLaunchKernelGGL(dense_weights_kernel, dim3(tiles, (unsigned)t.n), dim3(256), 0, stream, a, t, sm);
+    hipLaunchKernelGGL(dense_weights_kernel<TREE>, dim3(tiles, (unsigned)t.n), dim3(256), 0, stream, a, t, sm, tree);
     return hipGetLastError();
   }
   hipLaunchKernelGGL(slot_weights_kernel, dim3((unsigned)(p.padded / kTileKeys), (unsigned)p.rows), dim3(256), 0, stream,
                      a, sm, slots, p.padded);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(slot_add_kernel, dim3((unsigned)(p.ranges * p.groups), (unsigned)t.n), dim3(kAddThreads), 0, stream,
-                     a, t, slots, p.padded, p.groups, sums);
+  hipLaunchKernelGGL(slot_add_kernel<TREE>, dim3((unsigned)(p.ranges * p.groups), (unsigned)t.n), dim3(kAddThreads), 0,
+                     stream, a, t, slots, p.padded, p.groups, sums, tree);
   e = hipGetLastError();
   if (e != hipSuccess || p.groups == 1) return e;
   hipLaunchKernelGGL(group_add_kernel, dim3((unsigned)((p.max_n + 255) / 256), (unsigned)t.n), dim3(256), 0, stream, a, t,
                      p.groups, sums, (int64_t)p.ranges * kRange);
   return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attend(const AttendArgs& a, const RunTable& t, const TreeMask* tree, hipStream_t stream) {
+  return tree ? launch_call<true>(a, t, *tree, stream) : launch_call<false>(a, t, NoTree{}, stream);
 }
 
 }  // namespace pivot

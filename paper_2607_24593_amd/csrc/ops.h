@@ -1,5 +1,6 @@
 // Host-side launchers of the operators around the index calls (internal to
-// libpivot.so): norm, 4-bit cache, attention over it, eviction.
+// libpivot.so): norm, 4-bit cache, attention over it, eviction, products with
+// 4-bit weights, shared pages.
 #pragma once
 
 #include "cache4.h"
@@ -65,9 +66,51 @@ struct AttendArgs {
   int64_t acc_stride;
   void* workspace;
 };
-// Workspace bytes of one launch over the table's sequences.
+// Rows that are trees of drafted tokens: row r of the launch attends to positions
+// below base[b], and to node j of its sequence, at position base[b] + j, where bit
+// j mod 32 of word r * words + j / 32 is set.
+constexpr int kTreeWords = PIVOT_TREE_MAX_NODES / 32;
+struct TreeMask {
+  const uint32_t* bits;
+  int32_t words;
+  int32_t base[kMaxSeq];
+};
+// Workspace bytes of one launch over the table's sequences, n_k[b] the positions
+// that the launch's rows of sequence b may attend to (0 .. n_k[b] - 1).
 size_t attend_workspace(const AttendArgs& a, const RunTable& t);
-hipError_t launch_attend(const AttendArgs& a, const RunTable& t, hipStream_t stream);
+hipError_t launch_attend(const AttendArgs& a, const RunTable& t, const TreeMask* tree, hipStream_t stream);
+
+// Rows of accepted nodes, moved within their arrays: row pos0[b] + path[b][j] of
+// sequence b to row pos0[b] + j, up to the first j whose entry is not in
+// [j, limit - pos0[b]) or not above the entry before it.
+struct AcceptArgs {
+  const int32_t* path;  // [sequences, n]
+  int32_t n;
+  int64_t limit;        // positions of a sequence that the map holds
+  KeyMap map;
+  int32_t n_arrays;
+  uint8_t* rows[PIVOT_EVICT_MAX_ARRAYS];
+  int32_t row_bytes[PIVOT_EVICT_MAX_ARRAYS];
+};
+hipError_t launch_accept(const AcceptArgs& a, const RunTable& t, hipStream_t stream);
+
+// y = x w^T with weights in 4 bits (linear4.hip), at most kLinearRows rows.
+constexpr int kLinearRows = 1024;
+struct Linear4Args {
+  const void* x;
+  int64_t ld_x;
+  const float* x_scale;
+  int32_t x_fp8, group, rows, n, k;
+  const uint8_t* codes;
+  const uint8_t* scales;
+  void* out;
+  int64_t ld_out;
+  int32_t out_fp32;
+};
+size_t linear4_workspace(const Linear4Args& a);
+hipError_t launch_linear4(const Linear4Args& a, void* workspace, hipStream_t stream);
+hipError_t launch_linear4_pack(bool fp32, int32_t n, int32_t k, const void* w, int64_t ld, uint8_t* codes,
+                               uint8_t* scales, hipStream_t stream);
 
 // Which tokens stay (evict.hip): per sequence, the first `sink`, the last
 // `recent` and the largest acc of the others, `keep` in all, ascending.
@@ -91,5 +134,34 @@ struct MoveArrays {
 };
 hipError_t launch_move(const MoveArrays& m, const KeyMap& from, const KeyMap& to, const int32_t* kept, int batch,
                        int keep, hipStream_t stream);
+
+// Pages that sequences share (pages.hip).
+constexpr int kMaxPageList = PIVOT_PAGES_MAX_LIST;
+struct Pages {
+  int32_t* table;   // [slots, max_pages]
+  int32_t* refs;    // [n_pages]
+  int32_t max_pages, n_pages, shift;
+};
+// Entries of a call, passed by value: a fork from slot[i] to slot a[i] of b[i]
+// tokens; a growth of slot[i] from a[i] to b[i] tokens; a freeing of slot[i] from
+// a[i] tokens to b[i].
+struct PageList {
+  int32_t n;
+  int32_t slot[kMaxPageList], a[kMaxPageList], b[kMaxPageList];
+};
+struct PageRows {
+  int32_t n_pages, shift, n;
+  uint8_t* rows[PIVOT_EVICT_MAX_ARRAYS];
+  int32_t row_bytes[PIVOT_EVICT_MAX_ARRAYS];
+};
+hipError_t launch_pages_fork(const Pages& p, const PageList& l, hipStream_t stream);
+hipError_t launch_pages_free(const Pages& p, const PageList& l, hipStream_t stream);
+size_t pages_grow_workspace(const Pages& p, int64_t wanted);  // wanted: pages at most, one more a sequence among them
+hipError_t launch_pages_grow(const Pages& p, const PageList& l, int32_t* pairs, int32_t* state, void* workspace,
+                             hipStream_t stream);
+size_t pages_compact_workspace(const Pages& p);
+hipError_t launch_pages_compact(const Pages& p, int32_t slots, int32_t most, int32_t* pairs, int32_t* state,
+                                void* workspace, hipStream_t stream);
+hipError_t launch_pages_copy(const PageRows& a, int32_t n, const int32_t* pairs, hipStream_t stream);
 
 }  // namespace pivot
