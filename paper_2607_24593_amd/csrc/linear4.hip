@@ -18,6 +18,7 @@ namespace {
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 
+constexpr int kCus = 256;
 constexpr int kWaves = 8;
 constexpr int kChunk = 128;  // values of k that a wave multiplies at a time: one scale per lane
 
@@ -41,16 +42,68 @@ __device__ __forceinline__ uint4 widen8(const Fp8x8& v) {
 }
 
 // How a launch is cut: `kw` of a workgroup's 8 waves share k, the others take
-// other tiles of 16 weight rows; `splits` workgroups share k.
+// other tiles of 16 weight rows; `splits` workgroups share k; `groups` share the
+// tiles.
 struct Cut {
-  int kw, splits;
-  int tiles;   // of 16 weight rows
-  int groups;  // workgroups along n
+  int kw, splits, tiles, groups;
 };
 
-template <int MT, int KC, bool GROUPS>
+// Sixteen bytes (four; one, as a word) of every lane from base + off into LDS at byte
+// address dst + 16 (4) * lane, base and dst the same in all lanes of the wave.  The
+// waves wait for these loads themselves.  A scalar register that a vector instruction
+// wrote (readfirstlane) may be read by a memory instruction five wait states later;
+// the compiler does not see into the statement, so it waits itself.
+__device__ __forceinline__ const void* uniform(const void* p) {
+  const uint64_t v = (uint64_t)p;
+  return (const void*)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)v) |
+                       (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32);
+}
+__device__ __forceinline__ void load_lds16(const void* base, uint32_t off, uint32_t dst) {
+  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(dst), "v"(off), "s"(uniform(base)) : "memory");
+}
+__device__ __forceinline__ void load_lds4(const void* base, uint32_t off, uint32_t dst) {
+  asm volatile("s_nop 4\n\tglobal_load_lds_dword %1, %2" ::"{m0}"(dst), "v"(off), "s"(uniform(base)) : "memory");
+}
+__device__ __forceinline__ void load_lds1(const void* base, uint32_t off, uint32_t dst) {
+  asm volatile("s_nop 4\n\tglobal_load_lds_ubyte %1, %2" ::"{m0}"(dst), "v"(off), "s"(uniform(base)) : "memory");
+}
+
+// A workgroup of 8 waves keeps its part of x in registers, KC chunks of 128 values
+// of 16 MT rows a wave, and passes all of its weight tiles by it.  A wave's part of a
+// tile (16 rows x KC chunks: 1 KB of codes a chunk, then the scales) is loaded into
+// its own ring in LDS, four lanes a row's 64 bytes, some tiles ahead.  It is read as
+// the first operand of the matrix instruction (lane: row r, block g; the blocks of a
+// row change places by two bits of the row, so that 8 rows lie in different banks)
+// and its place is loaded again at once.
+// The waves' sums over k meet in LDS.  The waves do not wait for each other there:
+// sums of kSums tiles have room, a wave counts its arrival at a tile, and the wave
+// whose turn it is adds a tile's sums up kLag tiles later.
+// WORDS: the scales of a row's chunk are an aligned word (k a multiple of 128, the
+// array 4-byte aligned), else single bytes, each a word in LDS.
+constexpr int kLds = 160 * 1024 - 256;
+template <int MT, int KC, bool WORDS>
+struct Ring {
+  static constexpr int kSums = MT == 1 ? 4 : MT == 2 ? 3 : 2, kLag = kSums > 2 ? kSums - 2 : 1;
+  static constexpr int kSumBytes = kSums * kWaves * MT * 1024;
+  static constexpr int kScaleLoads = WORDS ? (KC + 3) / 4 : KC;
+  static constexpr int kLoads = KC + kScaleLoads;  // of a tile
+  static constexpr int kTile = 1024 * KC + 256 * kScaleLoads;
+  static constexpr int kFit = (kLds - kSumBytes) / (kWaves * kTile);
+  static constexpr int T = kFit > 6 ? 6 : kFit;  // tiles on their way
+  static_assert(T >= 1 && (T - 1) * kLoads < 64, "the wait's counter has 6 bits");
+};
+constexpr int kDirectRows = 4;  // up to here x is loaded straight into registers
+constexpr int64_t kMaxStride = 1 << 24;  // 64 rows so far apart have offsets of 32 bits
+constexpr int kXBlocks = 5;     // else blocks of 16 rows x 128 values on their way through LDS
+
+template <int MT, int KC, bool GROUPS, bool WORDS>
 __global__ __launch_bounds__(64 * kWaves, 2) void linear4_kernel(Linear4Args a, Cut cut, float* parts) {
-  __shared__ __attribute__((aligned(16))) v4f s_part[2][kWaves][MT][64];
+  using R = Ring<MT, KC, WORDS>;
+  constexpr int T = R::T;
+  constexpr int CHAINS = MT == 1 ? 4 : MT == 2 ? 2 : 1;  // sums that do not wait for each other
+  __shared__ __attribute__((aligned(16))) uint8_t s_lds[kLds];
+  __shared__ uint32_t s_arrived[R::kSums], s_added[R::kSums];
+  uint8_t* s_ring = s_lds + R::kSumBytes;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
   const int nw = kWaves / cut.kw, wk = w % cut.kw, wn = w / cut.kw;
@@ -58,107 +111,248 @@ __global__ __launch_bounds__(64 * kWaves, 2) void linear4_kernel(Linear4Args a, 
   const int k0 = ((int)blockIdx.y * cut.kw + wk) * KC * kChunk;
   const int blocks = a.k / kBlk;  // scales of a weight row
 
+  // the tiles that do not divide go to the first workgroups
+  const int each = cut.tiles / cut.groups, rest = cut.tiles % cut.groups, group = blockIdx.x;
+  const int first = group * each + min(group, rest), last = first + each + (group < rest);
+  const int steps = (last - first + nw - 1) / nw;
+  if (threadIdx.x < R::kSums) s_arrived[threadIdx.x] = s_added[threadIdx.x] = 0;
+
+  // a load's bytes of a lane: row lane / 4, and of its four blocks (words) one
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)s_lds;
+  const uint32_t ring = lds + R::kSumBytes + w * T * R::kTile;
+  const int lrow = lane >> 2, turned = (lane & 3) ^ (lrow >> 1 & 3);
+  auto load = [&](int i, int slot) {
+    const int tile = min(first + i * nw + wn, cut.tiles - 1);
+    const int at_row = min(lrow, a.n - 1 - 16 * tile) * blocks;
+    const int64_t at = (int64_t)16 * tile * blocks;
+    const uint32_t to = ring + slot * R::kTile;
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+      const int block = min(k0 / kBlk + 4 * c + turned, blocks - 1);
+      load_lds16(a.codes + at * 16, (uint32_t)((at_row + block) * 16), to + 1024 * c);
+    }
+#pragma unroll
+    for (int c = 0; c < R::kScaleLoads; ++c) {
+      if constexpr (WORDS) {
+        const int block = min(k0 / kBlk + 4 * (4 * c + (lane & 3)), blocks - 4);
+        load_lds4(a.scales + at, (uint32_t)(at_row + block), to + 1024 * KC + 256 * c);
+      } else {
+        const int block = min(k0 / kBlk + 4 * c + (lane & 3), blocks - 1);
+        load_lds1(a.scales + at, (uint32_t)(at_row + block), to + 1024 * KC + 256 * c);
+      }
+    }
+  };
+  auto load_first = [&] {
+#pragma unroll
+    for (int i = 0; i < T; ++i)
+      if (i < steps) load(i, i);
+  };
+
   // the wave's part of x: column m = lane & 15 of every product, 8 values from
   // k0 + 128 c + 32 g + 8 u on in product (c, u)
   uint4 x[MT][KC][4];
   float xs[MT][KC];
+  const int e = 2 - a.x_fp8;  // bytes of a value
+  // Of few rows most lanes read the same bytes; of more every lane would read a line
+  // of its own, 64 steps for 1 KB (64 rows of 6144: 11 us).  Those go through LDS,
+  // four lanes a row's 64 bytes, before the weights do.
+  const bool direct = a.rows <= kDirectRows || a.ld_x > kMaxStride || (((uintptr_t)a.x | (uintptr_t)(a.ld_x * e)) & 15) != 0;
+  if (direct) {
+    load_first();
 #pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    const int64_t m = min(row0 + 16 * t + r, a.rows - 1);
+    for (int t = 0; t < MT; ++t) {
+      const int64_t m = min(row0 + 16 * t + r, a.rows - 1);
 #pragma unroll
-    for (int c = 0; c < KC; ++c) {
-      const int k = k0 + kChunk * c + kBlk * g;
-      const bool in = k < a.k;
+      for (int c = 0; c < KC; ++c)
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        uint4 v = {0, 0, 0, 0};
-        if (in) {
+        for (int u = 0; u < 4; ++u) {
+          const int k = min(k0 + kChunk * c + kBlk * g, a.k - kBlk) + 8 * u;
           if (a.x_fp8) {
-            v = widen8(*reinterpret_cast<const Fp8x8*>((const uint8_t*)a.x + m * a.ld_x + k + 8 * u));
+            x[t][c][u] = widen8(*reinterpret_cast<const Fp8x8*>((const uint8_t*)a.x + m * a.ld_x + k));
           } else {
-            const Bf8 b = *reinterpret_cast<const Bf8*>((const uint16_t*)a.x + m * a.ld_x + k + 8 * u);
-            v = uint4{b.w[0], b.w[1], b.w[2], b.w[3]};
+            const Bf8 b = *reinterpret_cast<const Bf8*>((const uint16_t*)a.x + m * a.ld_x + k);
+            x[t][c][u] = uint4{b.w[0], b.w[1], b.w[2], b.w[3]};
           }
         }
-        x[t][c][u] = v;
+    }
+  } else {
+    constexpr int BLOCKS = MT * KC;
+    constexpr int AREA = kLds / kWaves / 1024 * 1024;
+    constexpr int DEPTH = kXBlocks * 4096 <= AREA ? kXBlocks : AREA / 4096;
+    auto load_x = [&](int b) {
+      const int t = b / KC, c = b % KC;
+      const int m = min(row0 + 16 * t + lrow, a.rows - 1) - row0;
+      const uint8_t* from = (const uint8_t*)a.x + (int64_t)row0 * a.ld_x * e;
+      const uint32_t to = lds + w * AREA + b % DEPTH * 4096;
+      const uint32_t at = (uint32_t)(m * (int)(a.ld_x * e));
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {  // 64 bytes of each row: 32 bf16 values, 64 fp8 values (p < 2)
+        if (a.x_fp8 && p >= 2) continue;
+        const int kb = k0 / kBlk + 4 * c + (a.x_fp8 ? 2 * p + (turned >> 1) : p);
+        const int in_block = a.x_fp8 ? turned & 1 : turned;
+        load_lds16(from, at + (uint32_t)min(kb, blocks - 1) * kBlk * e + 16 * in_block, to + 1024 * p);
       }
+    };
+#pragma unroll
+    for (int b = 0; b < DEPTH && b < BLOCKS; ++b) load_x(b);
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) {
+      constexpr int kLeft = DEPTH - 1;  // blocks that may be on their way
+      if (b + kLeft < BLOCKS) {
+        if (a.x_fp8) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLeft) : "memory");
+        else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * kLeft) : "memory");
+      } else {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      }
+      const int swap = r >> 1 & 3;
+      const uint8_t* from = s_lds + w * AREA + b % DEPTH * 4096 + 64 * r;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        uint4& to = x[b / KC][b % KC][u];
+        if (a.x_fp8) {
+          const uint2 v = *reinterpret_cast<const uint2*>(from + 1024 * (g >> 1) + ((2 * (g & 1) + (u >> 1)) ^ swap) * 16 + 8 * (u & 1));
+          to = uint4{v.x, v.y, 0, 0};
+        } else {
+          to = *reinterpret_cast<const uint4*>(from + 1024 * g + (u ^ swap) * 16);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {  // read before the place is loaded again
+        uint4& v = x[b / KC][b % KC][u];
+        asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w)::"memory");
+      }
+      if (b + DEPTH < BLOCKS) load_x(b + DEPTH);
+      if (a.x_fp8)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          uint4& v = x[b / KC][b % KC][u];
+          v = widen8(Fp8x8{{v.x, v.y}});
+        }
+    }
+    asm volatile("s_barrier" ::: "memory");  // every wave has read its rows
+    load_first();
+  }
+#pragma unroll
+  for (int c = 0; c < KC; ++c) {
+    const bool in = k0 + kChunk * c + kBlk * g < a.k;
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (!in) x[t][c][u] = uint4{0, 0, 0, 0};
       if constexpr (GROUPS) {
+        const int64_t m = min(row0 + 16 * t + r, a.rows - 1);
         const int i = k0 / kChunk + c, n = (a.k + kChunk - 1) / kChunk;
         xs[t][c] = i < n ? a.x_scale[m * n + i] : 0.f;
       }
     }
   }
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // the counters are 0
 
-  const int per = (cut.tiles + cut.groups - 1) / cut.groups;  // tiles of a workgroup
-  const int first = (int)blockIdx.x * per, last = min(first + per, cut.tiles);
-  const int steps = (last - first + nw - 1) / nw;
-  for (int i = 0; i < steps; ++i) {
-    const int tile = first + i * nw + wn;
-    const int64_t n = min(16 * tile + r, a.n - 1);
-    uint4 code[KC];
-    uint32_t byte[KC];
+  v4f* s_sum = reinterpret_cast<v4f*>(s_lds);  // [kSums][wave][MT][lane]
+  auto wait_for = [](const uint32_t* counter, uint32_t count) {
+    while ((uint32_t)__builtin_amdgcn_readfirstlane((int)__hip_atomic_load(counter, __ATOMIC_RELAXED,
+                                                                           __HIP_MEMORY_SCOPE_WORKGROUP)) < count)
+      __builtin_amdgcn_s_sleep(1);
+    asm volatile("" ::: "memory");
+  };
+  auto count = [&](uint32_t* counter) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (lane == 0) __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  };
+  const int items = nw * MT;  // (n tile, m tile) of a step
+
+  int slot = 0;
+  for (int i = 0; i < steps + R::kLag; ++i) {
+    if (i < steps) {
+      // of the loads those of the T - 1 tiles behind this one may be on their way
+      if (i + T <= steps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((T - 1) * R::kLoads) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      const uint8_t* tile = s_ring + (w * T + slot) * R::kTile;
+      uint4 code[KC];
+      uint32_t byte[KC];
 #pragma unroll
-    for (int c = 0; c < KC; ++c) {
-      const int k = k0 + kChunk * c + kBlk * g;
-      const bool in = k < a.k;
-      const int at = in ? k : 0;
-      code[c] = *reinterpret_cast<const uint4*>(a.codes + n * (a.k / 2) + at / 2);
-      byte[c] = a.scales[n * blocks + at / kBlk];
-      if (!in) {
-        code[c] = uint4{0, 0, 0, 0};
-        byte[c] = 127;
+      for (int c = 0; c < KC; ++c) {
+        code[c] = *reinterpret_cast<const uint4*>(tile + 1024 * c + (4 * r + (g ^ (r >> 1 & 3))) * 16);
+        if constexpr (WORDS)
+          byte[c] = *reinterpret_cast<const uint32_t*>(tile + 1024 * KC + 256 * (c / 4) + (4 * r + c % 4) * 4);
+        else
+          byte[c] = *reinterpret_cast<const uint32_t*>(tile + 1024 * KC + 256 * c + (4 * r + g) * 4);
       }
-    }
-    v4f sum[MT];
+      // read before the place is loaded again
 #pragma unroll
-    for (int t = 0; t < MT; ++t) sum[t] = v4f{0.f, 0.f, 0.f, 0.f};
+      for (int c = 0; c < KC; ++c)
+        asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(code[c].x), "+v"(code[c].y), "+v"(code[c].z), "+v"(code[c].w), "+v"(byte[c])::"memory");
+      if (i + T < steps) load(i + T, slot);
+      slot = slot + 1 == T ? 0 : slot + 1;
+      v4f sum[MT][CHAINS];
 #pragma unroll
-    for (int c = 0; c < KC; ++c) {
-      v4f part[MT];
+      for (int t = 0; t < MT; ++t)
 #pragma unroll
-      for (int t = 0; t < MT; ++t) part[t] = GROUPS ? v4f{0.f, 0.f, 0.f, 0.f} : sum[t];
-      const uint32_t words[4] = {code[c].x, code[c].y, code[c].z, code[c].w};
+        for (int q = 0; q < CHAINS; ++q) sum[t][q] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const v8bf wide = __builtin_bit_cast(v8bf, decode8(words[u], scale_operand(byte[c])));
+      for (int c = 0; c < KC; ++c) {
+        uint32_t scale = WORDS ? byte[c] >> (8 * g) & 255u : byte[c];
+        if (k0 + kChunk * c + kBlk * g >= a.k) {
+          code[c] = uint4{0, 0, 0, 0};
+          scale = 127;
+        }
+        const uint32_t words[4] = {code[c].x, code[c].y, code[c].z, code[c].w};
+        v4f part[MT];
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
-          part[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide, __builtin_bit_cast(v8bf, x[t][c][u]), part[t], 0, 0, 0);
-      }
+        for (int t = 0; t < MT; ++t) part[t] = GROUPS ? v4f{0.f, 0.f, 0.f, 0.f} : sum[t][c % CHAINS];
 #pragma unroll
-      for (int t = 0; t < MT; ++t) {
-        if constexpr (GROUPS) {
+        for (int u = 0; u < 4; ++u) {
+          const v8bf wide = __builtin_bit_cast(v8bf, decode8(words[u], scale_operand(scale)));
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sum[t][e] = fmaf(part[t][e], xs[t][c], sum[t][e]);
-        } else {
-          sum[t] = part[t];
+          for (int t = 0; t < MT; ++t)
+            part[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide, __builtin_bit_cast(v8bf, x[t][c][u]), part[t], 0, 0, 0);
+        }
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+          if constexpr (GROUPS) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[t][c % CHAINS][e] = fmaf(part[t][e], xs[t][c], sum[t][c % CHAINS][e]);
+          } else {
+            sum[t][c % CHAINS] = part[t];
+          }
         }
       }
-    }
+      const int at = i % R::kSums;
+      if (i >= R::kSums) wait_for(&s_added[at], (uint32_t)(i / R::kSums * items));  // the tile before here is put out
 #pragma unroll
-    for (int t = 0; t < MT; ++t) s_part[i & 1][w][t][lane] = sum[t];
-    __syncthreads();
-    // the sums over the waves that share k: items (n tile, m tile), one a wave
-    for (int item = w; item < nw * MT; item += kWaves) {
+      for (int t = 0; t < MT; ++t) {
+#pragma unroll
+        for (int q = 1; q < CHAINS; ++q) sum[t][0] += sum[t][q];
+        s_sum[((at * kWaves + w) * MT + t) * 64 + lane] = sum[t][0];
+      }
+      count(&s_arrived[at]);
+    }
+    const int done = i - R::kLag, at = done % R::kSums;
+    if (done < 0) continue;
+    for (int item = (w + done) % kWaves; item < items; item += kWaves) {
+      wait_for(&s_arrived[at], (uint32_t)((done / R::kSums + 1) * kWaves));
       const int tn = item / MT, t = item % MT;
-      v4f total = s_part[i & 1][tn * cut.kw][t][lane];
-      for (int j = 1; j < cut.kw; ++j) total += s_part[i & 1][tn * cut.kw + j][t][lane];
-      const int m = row0 + 16 * t + r, at = 16 * (first + i * nw + tn) + 4 * g;
-      if (first + i * nw + tn >= last || m >= a.rows) continue;
+      const v4f* from = s_sum + ((at * kWaves + tn * cut.kw) * MT + t) * 64 + lane;
+      v4f total = from[0];
+      for (int j = 1; j < cut.kw; ++j) total += from[j * MT * 64];
+      count(&s_added[at]);
+      const int m = row0 + 16 * t + r, n = 16 * (first + done * nw + tn) + 4 * g;
+      if (first + done * nw + tn >= last || m >= a.rows) continue;
       if (parts) {
         float* to = parts + ((int64_t)blockIdx.y * a.rows + m) * a.n;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (at + e < a.n) to[at + e] = total[e];
+          if (n + e < a.n) to[n + e] = total[e];
         continue;
       }
       const float s = a.x_fp8 && !GROUPS ? a.x_scale[m] : 1.f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        if (at + e >= a.n) break;
+        if (n + e >= a.n) break;
         const float y = total[e] * s;
-        if (a.out_fp32) ((float*)a.out)[m * a.ld_out + at + e] = y;
-        else ((uint16_t*)a.out)[m * a.ld_out + at + e] = bf16_rne(y);
+        if (a.out_fp32) ((float*)a.out)[m * a.ld_out + n + e] = y;
+        else ((uint16_t*)a.out)[m * a.ld_out + n + e] = bf16_rne(y);
       }
     }
   }
@@ -219,7 +413,7 @@ struct Plan {
 Plan plan_of(const Linear4Args& a) {
   Plan p{};
   p.mt = a.rows <= 16 ? 1 : a.rows <= 32 ? 2 : 4;
-  const int most = 8 / p.mt;  // chunks of k whose x a wave keeps
+  const int most = p.mt == 1 ? 8 : p.mt == 2 ? 5 : a.group ? 2 : 3;  // chunks of k whose x a wave has registers for
   const int chunks = (a.k + kChunk - 1) / kChunk;
   p.cut.splits = (chunks + kWaves * most - 1) / (kWaves * most);
   const int mine = (chunks + p.cut.splits - 1) / p.cut.splits;  // of a workgroup
@@ -228,17 +422,23 @@ Plan plan_of(const Linear4Args& a) {
   p.cut.kw = waves > 4 ? 8 : waves > 2 ? 4 : waves;
   p.cut.tiles = (a.n + 15) / 16;
   const int nw = kWaves / p.cut.kw;
-  p.cut.groups = std::min((p.cut.tiles + nw - 1) / nw, 512);
+  const int rows = (a.rows + 16 * p.mt - 1) / (16 * p.mt);
+  p.cut.groups = std::max(1, std::min((p.cut.tiles + nw - 1) / nw, kCus / (p.cut.splits * rows)));
   return p;
 }
 
+template <int MT, int KC, bool GROUPS>
+void launch_words(const Linear4Args& a, const Plan& p, float* parts, hipStream_t stream) {
+  const dim3 grid((unsigned)p.cut.groups, (unsigned)p.cut.splits, (unsigned)((a.rows + 16 * MT - 1) / (16 * MT)));
+  if (a.k % kChunk == 0 && ((uintptr_t)a.scales & 3) == 0)
+    hipLaunchKernelGGL((linear4_kernel<MT, KC, GROUPS, true>), grid, dim3(64 * kWaves), 0, stream, a, p.cut, parts);
+  else
+    hipLaunchKernelGGL((linear4_kernel<MT, KC, GROUPS, false>), grid, dim3(64 * kWaves), 0, stream, a, p.cut, parts);
+}
 template <int MT, int KC>
 void launch(const Linear4Args& a, const Plan& p, float* parts, hipStream_t stream) {
-  const dim3 grid((unsigned)p.cut.groups, (unsigned)p.cut.splits, (unsigned)((a.rows + 16 * MT - 1) / (16 * MT)));
-  if (a.group)
-    hipLaunchKernelGGL((linear4_kernel<MT, KC, true>), grid, dim3(64 * kWaves), 0, stream, a, p.cut, parts);
-  else
-    hipLaunchKernelGGL((linear4_kernel<MT, KC, false>), grid, dim3(64 * kWaves), 0, stream, a, p.cut, parts);
+  if (a.group) launch_words<MT, KC, true>(a, p, parts, stream);
+  else launch_words<MT, KC, false>(a, p, parts, stream);
 }
 
 }  // namespace
@@ -264,8 +464,10 @@ hipError_t launch_linear4(const Linear4Args& a, void* workspace, hipStream_t str
     case 22: launch<2, 2>(a, p, parts, stream); break;
     case 23: launch<2, 3>(a, p, parts, stream); break;
     case 24: launch<2, 4>(a, p, parts, stream); break;
+    case 25: launch<2, 5>(a, p, parts, stream); break;
     case 41: launch<4, 1>(a, p, parts, stream); break;
-    default: launch<4, 2>(a, p, parts, stream); break;
+    case 42: launch<4, 2>(a, p, parts, stream); break;
+    default: launch_words<4, 3, false>(a, p, parts, stream); break;
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !parts) return e;
