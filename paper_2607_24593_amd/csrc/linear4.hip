@@ -71,10 +71,12 @@ __device__ __forceinline__ void load_lds1(const void* base, uint32_t off, uint32
 // A workgroup of 8 waves keeps its part of x in registers, KC chunks of 128 values
 // of 16 MT rows a wave, and passes all of its weight tiles by it.  A wave's part of a
 // tile (16 rows x KC chunks: 1 KB of codes a chunk, then the scales) is loaded into
-// its own ring in LDS, four lanes a row's 64 bytes, some tiles ahead.  It is read as
-// the first operand of the matrix instruction (lane: row r, block g; the blocks of a
-// row change places by two bits of the row, so that 8 rows lie in different banks)
-// and its place is loaded again at once.
+// its own ring in LDS, some tiles ahead.  It is read as the first operand of the
+// matrix instruction (lane: row r, block g; the blocks of a row change places by bits
+// of the row, so that 8 rows lie in different banks) and its place is loaded again at
+// once.
+// Chunks of a wave come in pairs, neighbours in k, loaded as 8 rows x 128 bytes, whole
+// lines of memory; an odd last one as 16 rows x 64.
 // The waves' sums over k meet in LDS.  The waves do not wait for each other there:
 // sums of kSums tiles have room, a wave counts its arrival at a tile, and the wave
 // whose turn it is adds a tile's sums up kLag tiles later.
@@ -91,24 +93,32 @@ struct Ring {
   static constexpr int kFit = (kLds - kSumBytes) / (kWaves * kTile);
   static constexpr int T = kFit > 6 ? 6 : kFit;  // tiles on their way
   static_assert(T >= 1 && (T - 1) * kLoads < 64, "the wait's counter has 6 bits");
+  static_assert(kWaves * kTile + kWaves * 4096 <= kLds, "a block of x has room behind slot 0");
 };
 constexpr int kDirectRows = 4;  // up to here x is loaded straight into registers
 constexpr int64_t kMaxStride = 1 << 24;  // 64 rows so far apart have offsets of 32 bits
-constexpr int kXBlocks = 5;     // else blocks of 16 rows x 128 values on their way through LDS
 
-template <int MT, int KC, bool GROUPS, bool WORDS>
+// What x holds.
+enum Rows : int { kRowsBf16, kRowsFp8, kRowsGroups };
+
+template <int MT, int KC, int X, bool WORDS>
 __global__ __launch_bounds__(64 * kWaves, 2) void linear4_kernel(Linear4Args a, Cut cut, float* parts) {
   using R = Ring<MT, KC, WORDS>;
+  constexpr bool GROUPS = X == kRowsGroups, FP8 = X != kRowsBf16;
+  constexpr int PAIRED = KC / 2 * 2;  // chunks that come in pairs
   constexpr int T = R::T;
   constexpr int CHAINS = MT == 1 ? 4 : MT == 2 ? 2 : 1;  // sums that do not wait for each other
   __shared__ __attribute__((aligned(16))) uint8_t s_lds[kLds];
   __shared__ uint32_t s_arrived[R::kSums], s_added[R::kSums];
-  uint8_t* s_ring = s_lds + R::kSumBytes;
+  // slot 0 of all waves, the sums, the other slots
+  constexpr int SUMS = kWaves * R::kTile;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
   const int nw = kWaves / cut.kw, wk = w % cut.kw, wn = w / cut.kw;
   const int row0 = blockIdx.z * 16 * MT;
-  const int k0 = ((int)blockIdx.y * cut.kw + wk) * KC * kChunk;
+  auto chunk = [&](int c) {  // the wave's c-th
+    return (int)blockIdx.y * cut.kw * KC + (c < PAIRED ? wk * PAIRED + c : cut.kw * PAIRED + wk);
+  };
   const int blocks = a.k / kBlk;  // scales of a weight row
 
   // the tiles that do not divide go to the first workgroups
@@ -117,48 +127,46 @@ __global__ __launch_bounds__(64 * kWaves, 2) void linear4_kernel(Linear4Args a, 
   const int steps = (last - first + nw - 1) / nw;
   if (threadIdx.x < R::kSums) s_arrived[threadIdx.x] = s_added[threadIdx.x] = 0;
 
-  // a load's bytes of a lane: row lane / 4, and of its four blocks (words) one
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)s_lds;
-  const uint32_t ring = lds + R::kSumBytes + w * T * R::kTile;
-  const int lrow = lane >> 2, turned = (lane & 3) ^ (lrow >> 1 & 3);
+  auto slot_at = [&](int slot) { return (slot * kWaves + w) * R::kTile + (slot ? R::kSumBytes : 0); };
+  // a load's bytes of a lane: row lane / 8 (or / 4), and one of the row's pieces
+  const int row8 = lane >> 3, piece8 = (lane & 7) ^ row8, row4 = lane >> 2, piece4 = (lane & 3) ^ (row4 >> 1 & 3);
   auto load = [&](int i, int slot) {
-    const int tile = min(first + i * nw + wn, cut.tiles - 1);
-    const int at_row = min(lrow, a.n - 1 - 16 * tile) * blocks;
+    const int tile = min(first + i * nw + wn, cut.tiles - 1), most = a.n - 1 - 16 * tile;
     const int64_t at = (int64_t)16 * tile * blocks;
-    const uint32_t to = ring + slot * R::kTile;
+    const uint32_t to = lds + slot_at(slot);
 #pragma unroll
     for (int c = 0; c < KC; ++c) {
-      const int block = min(k0 / kBlk + 4 * c + turned, blocks - 1);
-      load_lds16(a.codes + at * 16, (uint32_t)((at_row + block) * 16), to + 1024 * c);
+      const bool pair = c < PAIRED;  // c even: rows 0 .. 7 of both chunks, c odd: rows 8 .. 15
+      const int row = min(pair ? row8 + 8 * (c & 1) : row4, most);
+      const int block = min(4 * chunk(pair ? c & ~1 : c) + (pair ? piece8 : piece4), blocks - 1);
+      load_lds16(a.codes + at * 16, (uint32_t)((row * blocks + block) * 16), to + 1024 * c);
     }
 #pragma unroll
     for (int c = 0; c < R::kScaleLoads; ++c) {
-      if constexpr (WORDS) {
-        const int block = min(k0 / kBlk + 4 * (4 * c + (lane & 3)), blocks - 4);
-        load_lds4(a.scales + at, (uint32_t)(at_row + block), to + 1024 * KC + 256 * c);
+      const int row = min(row4, most) * blocks;
+      if constexpr (WORDS) {  // words of chunks 4 c ..
+        int mine = chunk(4 * c);
+#pragma unroll
+        for (int e = 1; e < 4; ++e)
+          if (4 * c + e < KC) mine = (lane & 3) == e ? chunk(4 * c + e) : mine;
+        load_lds4(a.scales + at, (uint32_t)(row + min(4 * mine, blocks - 4)), to + 1024 * KC + 256 * c);
       } else {
-        const int block = min(k0 / kBlk + 4 * c + (lane & 3), blocks - 1);
-        load_lds1(a.scales + at, (uint32_t)(at_row + block), to + 1024 * KC + 256 * c);
+        load_lds1(a.scales + at, (uint32_t)(row + min(4 * chunk(c) + (lane & 3), blocks - 1)), to + 1024 * KC + 256 * c);
       }
     }
   };
-  auto load_first = [&] {
-#pragma unroll
-    for (int i = 0; i < T; ++i)
-      if (i < steps) load(i, i);
-  };
-
   // the wave's part of x: column m = lane & 15 of every product, 8 values from
-  // k0 + 128 c + 32 g + 8 u on in product (c, u)
+  // 128 chunk(c) + 32 g + 8 u on in product (c, u)
   uint4 x[MT][KC][4];
   float xs[MT][KC];
-  const int e = 2 - a.x_fp8;  // bytes of a value
+  constexpr int E = FP8 ? 1 : 2;  // bytes of a value
   // Of few rows most lanes read the same bytes; of more every lane would read a line
   // of its own, 64 steps for 1 KB (64 rows of 6144: 11 us).  Those go through LDS,
-  // four lanes a row's 64 bytes, before the weights do.
-  const bool direct = a.rows <= kDirectRows || a.ld_x > kMaxStride || (((uintptr_t)a.x | (uintptr_t)(a.ld_x * e)) & 15) != 0;
+  // four lanes a row's 64 bytes.
+  const bool direct = a.rows <= kDirectRows || a.ld_x > kMaxStride || (((uintptr_t)a.x | (uintptr_t)(a.ld_x * E)) & 15) != 0;
+  if (steps > 0) load(0, 0);
   if (direct) {
-    load_first();
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
       const int64_t m = min(row0 + 16 * t + r, a.rows - 1);
@@ -166,9 +174,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void linear4_kernel(Linear4Args a, 
       for (int c = 0; c < KC; ++c)
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          const int k = min(k0 + kChunk * c + kBlk * g, a.k - kBlk) + 8 * u;
-          if (a.x_fp8) {
-            x[t][c][u] = widen8(*reinterpret_cast<const Fp8x8*>((const uint8_t*)a.x + m * a.ld_x + k));
+          const int k = min(kChunk * chunk(c) + kBlk * g, a.k - kBlk) + 8 * u;
+          if constexpr (FP8) {
+            const Fp8x8 b = *reinterpret_cast<const Fp8x8*>((const uint8_t*)a.x + m * a.ld_x + k);
+            x[t][c][u] = uint4{b.w[0], b.w[1], 0, 0};
           } else {
             const Bf8 b = *reinterpret_cast<const Bf8*>((const uint16_t*)a.x + m * a.ld_x + k);
             x[t][c][u] = uint4{b.w[0], b.w[1], b.w[2], b.w[3]};
@@ -177,79 +186,73 @@ __global__ __launch_bounds__(64 * kWaves, 2) void linear4_kernel(Linear4Args a, 
     }
   } else {
     constexpr int BLOCKS = MT * KC;
-    constexpr int AREA = kLds / kWaves / 1024 * 1024;
-    constexpr int DEPTH = kXBlocks * 4096 <= AREA ? kXBlocks : AREA / 4096;
+    constexpr int PIECES = FP8 ? 2 : 4;  // loads of 16 rows x 64 bytes
+    constexpr int AREA = (kLds - SUMS) / kWaves / 1024;  // of a wave, behind slot 0
+    constexpr int DEPTH = AREA / PIECES < BLOCKS ? AREA / PIECES : BLOCKS;
     auto load_x = [&](int b) {
-      const int t = b / KC, c = b % KC;
-      const int m = min(row0 + 16 * t + lrow, a.rows - 1) - row0;
-      const uint8_t* from = (const uint8_t*)a.x + (int64_t)row0 * a.ld_x * e;
-      const uint32_t to = lds + w * AREA + b % DEPTH * 4096;
-      const uint32_t at = (uint32_t)(m * (int)(a.ld_x * e));
+      const int m = min(row0 + 16 * (b / KC) + row4, a.rows - 1) - row0;
+      const uint8_t* from = (const uint8_t*)a.x + (int64_t)row0 * a.ld_x * E;
+      const uint32_t to = lds + SUMS + (w * AREA + b % DEPTH * PIECES) * 1024;
 #pragma unroll
-      for (int p = 0; p < 4; ++p) {  // 64 bytes of each row: 32 bf16 values, 64 fp8 values (p < 2)
-        if (a.x_fp8 && p >= 2) continue;
-        const int kb = k0 / kBlk + 4 * c + (a.x_fp8 ? 2 * p + (turned >> 1) : p);
-        const int in_block = a.x_fp8 ? turned & 1 : turned;
-        load_lds16(from, at + (uint32_t)min(kb, blocks - 1) * kBlk * e + 16 * in_block, to + 1024 * p);
+      for (int p = 0; p < PIECES; ++p) {  // 32 bf16 values, 64 fp8 values of a row
+        const int kb = 4 * chunk(b % KC) + (FP8 ? 2 * p + (piece4 >> 1) : p);
+        load_lds16(from, (uint32_t)(m * (int)(a.ld_x * E) + min(kb, blocks - 1) * kBlk * E + 16 * (FP8 ? piece4 & 1 : piece4)),
+                   to + 1024 * p);
       }
     };
 #pragma unroll
-    for (int b = 0; b < DEPTH && b < BLOCKS; ++b) load_x(b);
+    for (int b = 0; b < DEPTH; ++b) load_x(b);
+    const int swap = r >> 1 & 3;
 #pragma unroll
     for (int b = 0; b < BLOCKS; ++b) {
-      constexpr int kLeft = DEPTH - 1;  // blocks that may be on their way
-      if (b + kLeft < BLOCKS) {
-        if (a.x_fp8) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLeft) : "memory");
-        else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * kLeft) : "memory");
-      } else {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      }
-      const int swap = r >> 1 & 3;
-      const uint8_t* from = s_lds + w * AREA + b % DEPTH * 4096 + 64 * r;
+      // of the loads those of the DEPTH - 1 blocks behind this one may be on their way
+      if (b + DEPTH <= BLOCKS) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((DEPTH - 1) * PIECES < 63 ? (DEPTH - 1) * PIECES : 63) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      const uint8_t* from = s_lds + SUMS + (w * AREA + b % DEPTH * PIECES) * 1024 + 64 * r;
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         uint4& to = x[b / KC][b % KC][u];
-        if (a.x_fp8) {
+        if constexpr (FP8) {
           const uint2 v = *reinterpret_cast<const uint2*>(from + 1024 * (g >> 1) + ((2 * (g & 1) + (u >> 1)) ^ swap) * 16 + 8 * (u & 1));
           to = uint4{v.x, v.y, 0, 0};
         } else {
           to = *reinterpret_cast<const uint4*>(from + 1024 * g + (u ^ swap) * 16);
         }
       }
+      if (b + DEPTH < BLOCKS) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {  // read before the place is loaded again
-        uint4& v = x[b / KC][b % KC][u];
-        asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w)::"memory");
-      }
-      if (b + DEPTH < BLOCKS) load_x(b + DEPTH);
-      if (a.x_fp8)
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < 4; ++u) {  // read before the place is loaded again
           uint4& v = x[b / KC][b % KC][u];
-          v = widen8(Fp8x8{{v.x, v.y}});
+          asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w)::"memory");
         }
+        load_x(b + DEPTH);
+      }
     }
-    asm volatile("s_barrier" ::: "memory");  // every wave has read its rows
-    load_first();
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // every wave has read its rows
   }
 #pragma unroll
+  for (int i = 1; i < T; ++i)
+    if (i < steps) load(i, i);
+#pragma unroll
   for (int c = 0; c < KC; ++c) {
-    const bool in = k0 + kChunk * c + kBlk * g < a.k;
+    const bool in = 4 * chunk(c) + g < blocks;
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+      for (int u = 0; u < 4; ++u) {
+        if constexpr (FP8) x[t][c][u] = widen8(Fp8x8{{x[t][c][u].x, x[t][c][u].y}});
         if (!in) x[t][c][u] = uint4{0, 0, 0, 0};
+      }
       if constexpr (GROUPS) {
         const int64_t m = min(row0 + 16 * t + r, a.rows - 1);
-        const int i = k0 / kChunk + c, n = (a.k + kChunk - 1) / kChunk;
-        xs[t][c] = i < n ? a.x_scale[m * n + i] : 0.f;
+        const int n = (a.k + kChunk - 1) / kChunk;
+        xs[t][c] = chunk(c) < n ? a.x_scale[m * n + chunk(c)] : 0.f;
       }
     }
   }
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // the counters are 0
 
-  v4f* s_sum = reinterpret_cast<v4f*>(s_lds);  // [kSums][wave][MT][lane]
+  v4f* s_sum = reinterpret_cast<v4f*>(s_lds + SUMS);  // [kSums][wave][MT][lane]
   auto wait_for = [](const uint32_t* counter, uint32_t count) {
     while ((uint32_t)__builtin_amdgcn_readfirstlane((int)__hip_atomic_load(counter, __ATOMIC_RELAXED,
                                                                            __HIP_MEMORY_SCOPE_WORKGROUP)) < count)
@@ -268,12 +271,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void linear4_kernel(Linear4Args a, 
       // of the loads those of the T - 1 tiles behind this one may be on their way
       if (i + T <= steps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((T - 1) * R::kLoads) : "memory");
       else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      const uint8_t* tile = s_ring + (w * T + slot) * R::kTile;
+      const uint8_t* tile = s_lds + slot_at(slot);
       uint4 code[KC];
       uint32_t byte[KC];
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
-        code[c] = *reinterpret_cast<const uint4*>(tile + 1024 * c + (4 * r + (g ^ (r >> 1 & 3))) * 16);
+        if (c < PAIRED)
+          code[c] = *reinterpret_cast<const uint4*>(tile + 1024 * ((c & ~1) + (r >> 3)) + 128 * (r & 7) + ((4 * (c & 1) + g) ^ (r & 7)) * 16);
+        else
+          code[c] = *reinterpret_cast<const uint4*>(tile + 1024 * c + (4 * r + (g ^ (r >> 1 & 3))) * 16);
         if constexpr (WORDS)
           byte[c] = *reinterpret_cast<const uint32_t*>(tile + 1024 * KC + 256 * (c / 4) + (4 * r + c % 4) * 4);
         else
@@ -293,7 +299,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void linear4_kernel(Linear4Args a, 
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
         uint32_t scale = WORDS ? byte[c] >> (8 * g) & 255u : byte[c];
-        if (k0 + kChunk * c + kBlk * g >= a.k) {
+        if (4 * chunk(c) + g >= blocks) {
           code[c] = uint4{0, 0, 0, 0};
           scale = 127;
         }
@@ -346,7 +352,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void linear4_kernel(Linear4Args a, 
           if (n + e < a.n) to[n + e] = total[e];
         continue;
       }
-      const float s = a.x_fp8 && !GROUPS ? a.x_scale[m] : 1.f;
+      const float s = X == kRowsFp8 ? a.x_scale[m] : 1.f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if (n + e >= a.n) break;
@@ -427,18 +433,19 @@ Plan plan_of(const Linear4Args& a) {
   return p;
 }
 
-template <int MT, int KC, bool GROUPS>
+template <int MT, int KC, int X>
 void launch_words(const Linear4Args& a, const Plan& p, float* parts, hipStream_t stream) {
   const dim3 grid((unsigned)p.cut.groups, (unsigned)p.cut.splits, (unsigned)((a.rows + 16 * MT - 1) / (16 * MT)));
   if (a.k % kChunk == 0 && ((uintptr_t)a.scales & 3) == 0)
-    hipLaunchKernelGGL((linear4_kernel<MT, KC, GROUPS, true>), grid, dim3(64 * kWaves), 0, stream, a, p.cut, parts);
+    hipLaunchKernelGGL((linear4_kernel<MT, KC, X, true>), grid, dim3(64 * kWaves), 0, stream, a, p.cut, parts);
   else
-    hipLaunchKernelGGL((linear4_kernel<MT, KC, GROUPS, false>), grid, dim3(64 * kWaves), 0, stream, a, p.cut, parts);
+    hipLaunchKernelGGL((linear4_kernel<MT, KC, X, false>), grid, dim3(64 * kWaves), 0, stream, a, p.cut, parts);
 }
 template <int MT, int KC>
 void launch(const Linear4Args& a, const Plan& p, float* parts, hipStream_t stream) {
-  if (a.group) launch_words<MT, KC, true>(a, p, parts, stream);
-  else launch_words<MT, KC, false>(a, p, parts, stream);
+  if (!a.x_fp8) launch_words<MT, KC, kRowsBf16>(a, p, parts, stream);
+  else if (!a.group) launch_words<MT, KC, kRowsFp8>(a, p, parts, stream);
+  else if constexpr (MT * KC <= 10) launch_words<MT, KC, kRowsGroups>(a, p, parts, stream);
 }
 
 }  // namespace
@@ -467,7 +474,7 @@ hipError_t launch_linear4(const Linear4Args& a, void* workspace, hipStream_t str
     case 25: launch<2, 5>(a, p, parts, stream); break;
     case 41: launch<4, 1>(a, p, parts, stream); break;
     case 42: launch<4, 2>(a, p, parts, stream); break;
-    default: launch_words<4, 3, false>(a, p, parts, stream); break;
+    default: launch<4, 3>(a, p, parts, stream); break;
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !parts) return e;
