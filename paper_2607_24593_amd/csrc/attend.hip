@@ -206,13 +206,18 @@ __host__ __device__ inline int splits_of(const RunTable& t, int b, int tiles_per
   return tiles > tiles_per_split ? (tiles + tiles_per_split - 1) / tiles_per_split : 1;
 }
 
+// What a kernel is compiled for: causal calls of both kinds, trees over the prefix,
+// trees over index sets (with one kernel for both, three registers of its tile loop
+// are spilled, which costs 20%).
+enum Call : int { kCausal, kTreePrefix, kTreeSets };
 struct NoTree {};
 template <bool TREE>
 using TreeOf = std::conditional_t<TREE, TreeMask, NoTree>;
 
-template <int RG, bool TREE>
+template <int RG, int CALL>
 __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, RunTable t, ScoreMap sm, Work wk,
-                                                                TreeOf<TREE> tree) {
+                                                                TreeOf<CALL != kCausal> tree) {
+  constexpr bool TREE = CALL != kCausal;
   constexpr bool ONE = RG == 8;                // one barrier per tile
   constexpr int ROWS = 16 * RG;
   constexpr int KT = kTileKeys;
@@ -239,13 +244,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
   __shared__ int s_entry[ONE ? 1 : 4 * 64], s_page[ONE ? 1 : 4 * 64];  // of 8 tiles' keys, on their way
   __shared__ float s_alpha[2][ROWS], s_max[ROWS], s_sum[ROWS];
   // of a tree: the word that a row's mask starts at (prefix calls), the mask of the
-  // unit's query (index sets)
+  // unit's query (index sets), the masks and their words; here, and not in registers,
+  // because few tiles need them (held in registers they cost the tile loop 20%)
   __shared__ int s_tree[TREE ? ROWS : 1];
   __shared__ uint32_t s_mask[TREE ? kTreeWords : 1];
+  __shared__ const uint32_t* s_bits;
+  __shared__ int s_words;
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const bool sets = a.idx != nullptr;
+  const bool sets = CALL == kCausal ? a.idx != nullptr : CALL == kTreeSets;
   const int part = blockIdx.x;
   const int unit = sets ? part / (wk.row_tiles * wk.splits) : owner_of(wk.first, t.n, part);
   const int b = sets ? run_of(t, unit) : unit;
@@ -399,11 +407,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
   {
     const int mine = row0 + (lane & 15), flat = first + min(mine, rows - 1), g = lane >> 4;
     const int i = sets ? 0 : flat / a.heads, head = flat - i * a.heads;
-    if constexpr (TREE) {  // the last position before the tree
-      limit = (ONE ? mine : tid / LPR) < rows ? tree.base[b] - 1 : -1;
+    if constexpr (TREE) {  // the last position before the tree, for padded rows too
+      limit = tree.base[b] - 1;
       const int r = min(tid, rows - 1);
       if (tid < ROWS) s_tree[tid] = (t.row0[b] + i_first + (sets ? 0 : (first + r) / a.heads)) * tree.words;
       if (sets && tid < tree.words) s_mask[tid] = tree.bits[(int64_t)(t.row0[b] + i_first) * tree.words + tid];
+      if (tid == 0) {
+        s_bits = tree.bits;
+        s_words = tree.words;
+      }
+      asm volatile("" : "+v"(limit));  // kept as it is, not as the base
     } else if constexpr (ONE) {
       limit = mine < rows ? t.pos0[b] + i_first + i : -1;
     } else {
@@ -535,20 +548,23 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
     });
   };
 
-  // whether a key's masking position is a node of the tree, and whether a row's mask
-  // names it (padded rows share the last row's mask: nothing of theirs is put out)
-  auto is_draft = [&](int key_at) {
-    if constexpr (TREE) return key_at >= tree.base[b] && key_at != 0x7FFFFFFF;
-    return false;
-  };
-  auto named = [&](int row, int key_at) {
+  // Of the keys at s_pos[first + 16 (e / 4) + e % 4], e < n, the nodes of the tree that
+  // a row's mask names, as bits (padded rows share the last row's mask: nothing of
+  // theirs is put out).  A loop that is not unrolled: few tiles need it, and no
+  // registers are left around it.
+  auto named = [&](int row, int first_key, int n_keys) {
+    uint32_t bits = 0;
     if constexpr (TREE) {
-      const int node = key_at - tree.base[b];
-      if ((uint32_t)node >= (uint32_t)(32 * tree.words)) return false;
-      const uint32_t word = sets ? s_mask[node >> 5] : tree.bits[s_tree[row] + (node >> 5)];
-      return (word >> (node & 31) & 1u) != 0u;
+#pragma unroll 1
+      for (int e = 0; e < n_keys; ++e) {
+        const int node = s_pos[first_key + 16 * (e >> 2) + (e & 3)] - limit - 1;
+        if ((uint32_t)node < (uint32_t)(32 * s_words)) {
+          const uint32_t word = sets ? s_mask[node >> 5] : s_bits[s_tree[row] + (node >> 5)];
+          bits |= (word >> (node & 31) & 1u) << e;
+        }
+      }
     }
-    return false;
+    return bits;
   };
 
   // the scores in base 2, masked, and the row's largest; tile: the unit's tile, for the kept scores
@@ -556,28 +572,28 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
   auto finish_scores = [&](int ln, int tile, int slot) {
     const int key = ln & 15, g = ln >> 4;
     top = -INFINITY;
-    bool drafts = false;
-    if constexpr (TREE) drafts = !sets && (tile + 1) * KT > tree.base[b];
-    if (TREE && sets) {
-      bool any = false;
+    uint32_t seen = 0;  // nodes of a tree
+    if constexpr (TREE) {
+      bool drafts = tile * KT + KT - 1 > limit;
+      if (sets) {
+        drafts = false;
 #pragma unroll
-      for (int j = 0; j < NKT; ++j) {
-        const v4i key_at = *reinterpret_cast<const v4i*>(&s_pos[slot * KT + 16 * j + 4 * g]);
+        for (int j = 0; j < NKT; ++j) {
+          const v4i key_at = *reinterpret_cast<const v4i*>(&s_pos[slot * KT + 16 * j + 4 * g]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) any = any || is_draft(key_at[i]);
+          for (int i = 0; i < 4; ++i) drafts = drafts || (key_at[i] > limit && key_at[i] != 0x7FFFFFFF);
+        }
       }
-      drafts = any;
+      if (__any(drafts)) seen = named(row0 + key, slot * KT + 4 * g, 4 * NKT);
     }
-    drafts = TREE && __any(drafts);
 #pragma unroll
     for (int j = 0; j < NKT; ++j) {
       const int k4 = 16 * j + 4 * g;
       const v4i key_at = *reinterpret_cast<const v4i*>(&s_pos[slot * KT + k4]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        bool seen = key_at[i] <= limit;
-        if (TREE && drafts) seen = seen || named(row0 + key, key_at[i]);
-        s[j][i] = seen ? s[j][i] * c : -INFINITY;
+        const bool in = key_at[i] <= limit || (TREE && (seen >> (4 * j + i) & 1u));
+        s[j][i] = in ? s[j][i] * c : -INFINITY;
         top = fmaxf(top, s[j][i]);
       }
       if (s2 && tile < t1 && row0 + key < rows)
@@ -671,24 +687,24 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
       for (int d = 0; d < DG; ++d) zp[i][d] = s_part[((buf * DG + d) * ROWS + row) * PR + k0 + i];
     }
   };
-  // the weights of KPT scores of one row to s_w[wslot]
-  auto weigh_part = [&](int td, int wslot) {
+  // the weights of KPT scores of one row to s_w[wslot]; slot: of their keys
+  auto weigh_part = [&](int td, int wslot, int slot) {
     const int row = td / LPR, k0 = td % LPR * KPT;
     float z[KPT], e[KPT], top = -INFINITY;
-    bool drafts = false;
+    uint32_t seen = 0;  // nodes of a tree
     if constexpr (TREE) {
+      bool drafts = false;
 #pragma unroll
-      for (int i = 0; i < KPT; ++i) drafts = drafts || is_draft(key_at[i]);
-      drafts = __any(drafts);
+      for (int i = 0; i < KPT; ++i) drafts = drafts || (key_at[i] > limit && key_at[i] != 0x7FFFFFFF);
+      if (__any(drafts)) seen = named(row, slot * KT + k0, KPT);
     }
 #pragma unroll
     for (int i = 0; i < KPT; ++i) {
       z[i] = zp[i][0];
 #pragma unroll
       for (int d = 1; d < DG; ++d) z[i] += zp[i][d];
-      bool seen = key_at[i] <= limit;
-      if (TREE && drafts) seen = seen || named(row, key_at[i]);
-      z[i] = seen ? z[i] * c : -INFINITY;
+      const bool in = key_at[i] <= limit || (TREE && (seen >> i & 1u));
+      z[i] = in ? z[i] * c : -INFINITY;
       top = fmaxf(top, z[i]);
     }
     top = row_reduce<LPR>(top, [](float x, float y) { return fmaxf(x, y); });
@@ -902,7 +918,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
       read_score(lane, 1);
       read_part(tid, 0, 0);
       score_part(lane, 1);
-      weigh_part(tid, 0);
+      weigh_part(tid, 0, 0);
       keep_scores(tid, t0);
     }
     unroll<WIDENS>([&](auto p) { widen_piece(lane, 0, 0, p); });
@@ -939,7 +955,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
       read_codes(ln, next);
       if constexpr (RG < 4) read_output(ln, i & 1, i & 1);
       __builtin_amdgcn_sched_barrier(0);
-      weigh_part(64 * w + ln, (i + 1) & 1);
+      weigh_part(64 * w + ln, (i + 1) & 1, next);
       score_part(ln, i & 1);
       widen_codes(ln, (i + 1) & 1);
       if constexpr (RG == 4) read_output(ln, i & 1, i & 1);  // no registers for it before
@@ -1359,10 +1375,10 @@ Plan plan_of(const AttendArgs& a, const RunTable& t) {
   return p;
 }
 
-template <int RG, bool TREE>
+template <int RG, int CALL>
 hipError_t launch_rows(const AttendArgs& a, const RunTable& t, const ScoreMap& sm, const Work& wk, unsigned workgroups,
-                       const TreeOf<TREE>& tree, hipStream_t stream) {
-  hipLaunchKernelGGL((attend_kernel<RG, TREE>), dim3(workgroups), dim3(64 * kWaves), 0, stream, a, t, sm, wk, tree);
+                       const TreeOf<CALL != kCausal>& tree, hipStream_t stream) {
+  hipLaunchKernelGGL((attend_kernel<RG, CALL>), dim3(workgroups), dim3(64 * kWaves), 0, stream, a, t, sm, wk, tree);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || wk.splits == 1) return e;
   using J = Join<RG>;
@@ -1378,8 +1394,9 @@ size_t attend_workspace(const AttendArgs& a, const RunTable& t) { return plan_of
 
 namespace {
 
-template <bool TREE>
-hipError_t launch_call(const AttendArgs& a, const RunTable& t, const TreeOf<TREE>& tree, hipStream_t stream) {
+template <int CALL>
+hipError_t launch_call(const AttendArgs& a, const RunTable& t, const TreeOf<CALL != kCausal>& tree, hipStream_t stream) {
+  constexpr bool TREE = CALL != kCausal;
   Plan p = plan_of(a, t);
   if (p.rows == 0) return hipSuccess;
   ScoreMap sm{};
@@ -1395,10 +1412,10 @@ hipError_t launch_call(const AttendArgs& a, const RunTable& t, const TreeOf<TREE
   p.wk.part_o = (float4*)parts;
   p.wk.part_ml = (float2*)(parts + round256(p.part_o));
   const unsigned wgs = (unsigned)p.workgroups;
-  hipError_t e = p.rg == 8   ? launch_rows<8, TREE>(a, t, sm, p.wk, wgs, tree, stream)
-                 : p.rg == 4 ? launch_rows<4, TREE>(a, t, sm, p.wk, wgs, tree, stream)
-                 : p.rg == 2 ? launch_rows<2, TREE>(a, t, sm, p.wk, wgs, tree, stream)
-                             : launch_rows<1, TREE>(a, t, sm, p.wk, wgs, tree, stream);
+  hipError_t e = p.rg == 8   ? launch_rows<8, CALL>(a, t, sm, p.wk, wgs, tree, stream)
+                 : p.rg == 4 ? launch_rows<4, CALL>(a, t, sm, p.wk, wgs, tree, stream)
+                 : p.rg == 2 ? launch_rows<2, CALL>(a, t, sm, p.wk, wgs, tree, stream)
+                             : launch_rows<1, CALL>(a, t, sm, p.wk, wgs, tree, stream);
   if (e != hipSuccess || !a.acc || (a.idx && a.topk == 0)) return e;
   if (!a.idx) {
     const unsigned tiles = (unsigned)((p.max_n + kTileKeys - 1) / kTileKeys);
@@ -1421,7 +1438,8 @@ hipError_t launch_call(const AttendArgs& a, const RunTable& t, const TreeOf<TREE
 }  // namespace
 
 hipError_t launch_attend(const AttendArgs& a, const RunTable& t, const TreeMask* tree, hipStream_t stream) {
-  return tree ? launch_call<true>(a, t, *tree, stream) : launch_call<false>(a, t, NoTree{}, stream);
+  if (!tree) return launch_call<kCausal>(a, t, NoTree{}, stream);
+  return a.idx ? launch_call<kTreeSets>(a, t, *tree, stream) : launch_call<kTreePrefix>(a, t, *tree, stream);
 }
 
 }  // namespace pivot
