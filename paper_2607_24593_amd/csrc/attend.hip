@@ -1152,16 +1152,13 @@ __global__ __launch_bounds__(64 * kWaves) void join_kernel(AttendArgs a, RunTabl
 
 // Sum over a tile's rows from `least` on, those that attend to the thread's key,
 // of the softmax weights of its 32 keys: 8 rows at a time, each thread one key,
-// the rows of a thread in ascending order.  The rows before (and those that skip(r)
-// holds for) are left out, not added as zeros: the masked scores of a NaN row give
-// NaN.
-template <class Skip>
+// the rows of a thread in ascending order.  The rows before are left out, not
+// added as zeros: the masked scores of a NaN row give NaN.
 __device__ __forceinline__ float tile_weight(const float* tile, const float2* stat, int least, int rows, float* red,
-                                             int tid, Skip skip) {
+                                             int tid) {
   const int k = tid & 31, first = tid >> 5;
   float w = 0.f;
   for (int r = first + (max(least - first, 0) + 7) / 8 * 8; r < rows; r += 8) {
-    if (skip(r)) continue;
     const float2 st = stat[r];
     w = fmaf(exp2f(tile[r * kTileKeys + k] - st.x), st.y, w);
   }
@@ -1174,27 +1171,70 @@ __device__ __forceinline__ float tile_weight(const float* tile, const float2* st
   return w;
 }
 
-template <bool TREE>
-__global__ __launch_bounds__(256) void dense_weights_kernel(AttendArgs a, RunTable t, ScoreMap sm, TreeOf<TREE> tree) {
+__global__ __launch_bounds__(256) void dense_weights_kernel(AttendArgs a, RunTable t, ScoreMap sm) {
   __shared__ float red[256];
   const int b = blockIdx.y, tile = blockIdx.x, tid = threadIdx.x;
   const int n = t.n_k[b], rows = t.n_rows[b] * a.heads;
   if (rows == 0 || tile * kTileKeys >= n) return;
-  const float* scores = sm.s2 + sm.base[b] + (int64_t)tile * rows * kTileKeys;
-  const float2* stat = sm.stat + (int64_t)t.row0[b] * a.heads;
-  const int key = tile * kTileKeys + (tid & 31);
-  float w;
-  if constexpr (TREE) {
-    const int node = key - tree.base[b];
-    const bool draft = node >= 0 && key < n;
-    const uint32_t* bits = tree.bits + (int64_t)t.row0[b] * tree.words + (draft ? node >> 5 : 0);
-    w = tile_weight(scores, stat, 0, rows, red, tid,
-                    [&](int r) { return draft && (bits[(int64_t)(r / a.heads) * tree.words] >> (node & 31) & 1u) == 0u; });
-  } else {
-    w = tile_weight(scores, stat, max(key - t.pos0[b], 0) * a.heads, rows, red, tid, [](int) { return false; });
-  }
+  const int least = max(tile * kTileKeys + (tid & 31) - t.pos0[b], 0) * a.heads;
+  const float w = tile_weight(sm.s2 + sm.base[b] + (int64_t)tile * rows * kTileKeys,
+                              sm.stat + (int64_t)t.row0[b] * a.heads, least, rows, red, tid);
   const int s = tile * kTileKeys + tid;
   if (tid < kTileKeys && s < n) a.acc[(int64_t)b * a.acc_stride + s] += w;
+}
+
+// The same for trees, where a call has many rows: 32 rows at a time, each thread 4
+// keys, four loads on their way.  Rows whose mask does not name a node are left out,
+// not added as zeros.  Bound by the scores' bytes: 192 rows x 196000 keys in 36 us,
+// 4.2 TB/s (one key a thread: 52).
+__global__ __launch_bounds__(256) void tree_weights_kernel(AttendArgs a, RunTable t, ScoreMap sm, TreeMask tree) {
+  __shared__ float red[4][kTileKeys];
+  const int b = blockIdx.y, tile = blockIdx.x, tid = threadIdx.x;
+  const int n = t.n_k[b], rows = t.n_rows[b] * a.heads;
+  if (rows == 0 || tile * kTileKeys >= n) return;
+  const v4f* scores = reinterpret_cast<const v4f*>(sm.s2 + sm.base[b] + (int64_t)tile * rows * kTileKeys) + tid;
+  const float2* stat = sm.stat + (int64_t)t.row0[b] * a.heads;
+  v4f w = {0.f, 0.f, 0.f, 0.f};
+  if (tile * kTileKeys + kTileKeys <= tree.base[b]) {
+    for (int r = tid >> 3; r < rows; r += 128) {
+      v4f z[4];
+      float2 st[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int at = min(r + 32 * j, rows - 1);
+        z[j] = scores[(at - (tid >> 3)) * (kTileKeys / 4)];
+        st[j] = stat[at];
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (r + 32 * j < rows) w[i] = fmaf(__builtin_amdgcn_exp2f(z[j][i] - st[j].x), st[j].y, w[i]);
+    }
+  } else {
+    const int node = tile * kTileKeys + 4 * (tid & 7) - tree.base[b];
+    for (int r = tid >> 3; r < rows; r += 32) {
+      const uint32_t* mask = tree.bits + (int64_t)(t.row0[b] + r / a.heads) * tree.words;
+      const v4f z = scores[(r - (tid >> 3)) * (kTileKeys / 4)];
+      const float2 st = stat[r];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int at = node + i;
+        const bool seen = at < 0 || (at < n - tree.base[b] && (mask[at >> 5] >> (at & 31) & 1u));
+        if (seen) w[i] = fmaf(__builtin_amdgcn_exp2f(z[i] - st.x), st.y, w[i]);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {  // the wave's 8 rows, then the waves
+    w[i] += lane_xor8(w[i]);
+    w[i] = groups_sum(w[i]);
+    if ((tid & 63) < 8) red[tid >> 6][4 * (tid & 7) + i] = w[i];
+  }
+  __syncthreads();
+  const int s = tile * kTileKeys + tid;
+  if (tid < kTileKeys && s < n)
+    a.acc[(int64_t)b * a.acc_stride + s] += (red[0][tid] + red[1][tid]) + (red[2][tid] + red[3][tid]);
 }
 
 __global__ __launch_bounds__(256) void slot_weights_kernel(AttendArgs a, ScoreMap sm, float* __restrict__ slots,
@@ -1202,7 +1242,7 @@ __global__ __launch_bounds__(256) void slot_weights_kernel(AttendArgs a, ScoreMa
   __shared__ float red[256];
   const int r = blockIdx.y, tile = blockIdx.x, tid = threadIdx.x;
   const float w = tile_weight(sm.s2 + ((int64_t)r * padded + tile * kTileKeys) * a.heads,
-                              sm.stat + (int64_t)r * a.heads, 0, a.heads, red, tid, [](int) { return false; });
+                              sm.stat + (int64_t)r * a.heads, 0, a.heads, red, tid);
   if (tid < kTileKeys) slots[(int64_t)r * padded + tile * kTileKeys + tid] = w;
 }
 
@@ -1419,7 +1459,10 @@ hipError_t launch_call(const AttendArgs& a, const RunTable& t, const TreeOf<CALL
   if (e != hipSuccess || !a.acc || (a.idx && a.topk == 0)) return e;
   if (!a.idx) {
     const unsigned tiles = (unsigned)((p.max_n + kTileKeys - 1) / kTileKeys);
-    hipLaunchKernelGGL(dense_weights_kernel<TREE>, dim3(tiles, (unsigned)t.n), dim3(256), 0, stream, a, t, sm, tree);
+    if constexpr (TREE)
+      hipLaunchKernelGGL(tree_weights_kernel, dim3(tiles, (unsigned)t.n), dim3(256), 0, stream, a, t, sm, tree);
+    else
+      hipLaunchKernelGGL(dense_weights_kernel, dim3(tiles, (unsigned)t.n), dim3(256), 0, stream, a, t, sm);
     return hipGetLastError();
   }
   hipLaunchKernelGGL(slot_weights_kernel, dim3((unsigned)(p.padded / kTileKeys), (unsigned)p.rows), dim3(256), 0, stream,
