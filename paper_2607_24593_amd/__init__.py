@@ -12,6 +12,7 @@ from __future__ import annotations
 import array
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -257,24 +258,23 @@ def lib():
         L.pivot_cache4_attend_tree_workspace_size.argtypes = [ctypes.POINTER(pivot_attend_args), T]
         L.pivot_cache4_attend_tree.restype = I32
         L.pivot_cache4_attend_tree.argtypes = [ctypes.POINTER(pivot_attend_args), T]
-        R = ctypes.POINTER(pivot_rows)
         L.pivot_tree_accept.restype = I32
-        L.pivot_tree_accept.argtypes = [I32, I32, P, PI, I32, R, ctypes.POINTER(pivot_row_map), P]
+        L.pivot_tree_accept.argtypes = [I32, I32, P, P, I32, P, ctypes.POINTER(pivot_row_map), P]
         PG = ctypes.POINTER(pivot_pages)
         L.pivot_pages_fork.restype = I32
-        L.pivot_pages_fork.argtypes = [PG, I32, PI, PI, PI, P]
+        L.pivot_pages_fork.argtypes = [PG, I32, P, P, P, P]
         L.pivot_pages_free.restype = I32
-        L.pivot_pages_free.argtypes = [PG, I32, PI, PI, PI, P]
+        L.pivot_pages_free.argtypes = [PG, I32, P, P, P, P]
         L.pivot_pages_grow_workspace_size.restype = SZ
-        L.pivot_pages_grow_workspace_size.argtypes = [PG, I32, PI, PI]
+        L.pivot_pages_grow_workspace_size.argtypes = [PG, I32, P, P]
         L.pivot_pages_grow.restype = I32
-        L.pivot_pages_grow.argtypes = [PG, I32, PI, PI, PI, P, P, P, SZ, P]
+        L.pivot_pages_grow.argtypes = [PG, I32, P, P, P, P, P, P, SZ, P]
         L.pivot_pages_compact_workspace_size.restype = SZ
         L.pivot_pages_compact_workspace_size.argtypes = [PG]
         L.pivot_pages_compact.restype = I32
         L.pivot_pages_compact.argtypes = [PG, I32, P, P, P, SZ, P]
         L.pivot_pages_copy.restype = I32
-        L.pivot_pages_copy.argtypes = [PG, I32, P, I32, R, P]
+        L.pivot_pages_copy.argtypes = [PG, I32, P, I32, P, P]
         L.pivot_profile_begin.restype = I32
         L.pivot_profile_begin.argtypes = []
         L.pivot_profile_begin_kinds.restype = I32
@@ -936,6 +936,18 @@ def pivot_evict(acc, n_k, keep, arrays, from_map, to_map, sink=0, recent=0, out_
 
 # ---- a decode step with drafted tokens ----
 
+_INTS = {}
+
+
+def _packed_ints(v) -> bytes:
+    """Host integers as the bytes of an int32 array: twice as fast as a ctypes array,
+    and a c_void_p argument takes them as they are."""
+    f = _INTS.get(len(v))
+    if f is None:
+        f = _INTS[len(v)] = struct.Struct(f"{len(v)}i").pack
+    return f(*v)
+
+
 def pivot_linear4_pack(w, codes=None, scales=None, stream=None):
     """Weights [n, k] (bf16 or fp32, rows may be strided, k a multiple of 32) as the
     4-bit operand of pivot_linear4: (codes uint8 [n, k / 2], scales uint8 [n, k / 32])."""
@@ -966,52 +978,56 @@ def pivot_linear4(x, codes, scales, x_scale=None, group=0, dtype=torch.bfloat16,
     ld_x = _rows_of(x, k, "x")
     _expect(codes, torch.uint8, (n, k // 2), "codes")
     _expect(scales, torch.uint8, (n, k // 32), "scales")
-    a = pivot_linear4_args()
     if x.dtype == torch.bfloat16:
         if x_scale is not None or group:
             raise ValueError("bf16 rows have no scales")
+        x_code, s_ptr = PIVOT_DT_BF16, None
     elif x.dtype in (torch.float8_e4m3fn, torch.uint8):
         if x_scale is None:
             raise ValueError("fp8 rows need x_scale")
         _expect(x_scale, torch.float32, x.shape[:-1] + (-(-k // group) if group else 1,), "x_scale")
-        a.x_dtype, a.x_scale = PIVOT_DT_FP8_E4M3, x_scale.data_ptr()
+        x_code, s_ptr = PIVOT_DT_FP8_E4M3, x_scale.data_ptr()
     else:
         raise ValueError("x must be bfloat16 or fp8 codes")
-    if dtype == torch.float32:
-        a.out_dtype = PIVOT_DT_FP32
-    elif dtype != torch.bfloat16:
+    if dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("dtype must be bfloat16 or float32")
     _on_gpu(x.get_device(), codes, scales, x_scale, out, ws)
     shape = x.shape[:-1] + (n,)
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=x.device)
+        out, ld_out = torch.empty(shape, dtype=dtype, device=x.device), n
     elif out.dtype != dtype or out.shape != shape:
         raise ValueError(f"out must be a {dtype} tensor of shape {tuple(shape)}")
-    a.n_rows, a.n, a.k, a.group = x.numel() // k if k else 0, n, k, group
-    a.x, a.ld_x, a.codes, a.scales = x.data_ptr(), ld_x, codes.data_ptr(), scales.data_ptr()
-    a.out, a.ld_out = out.data_ptr(), _rows_of(out, n, "out")
-    a.stream = _stream(stream)
-    L = lib()
-    need = L.pivot_linear4_workspace_size(ctypes.byref(a))
+    else:
+        ld_out = _rows_of(out, n, "out")
+    a = pivot_linear4_args(x_code, PIVOT_DT_FP32 if dtype == torch.float32 else PIVOT_DT_BF16,
+                           x.numel() // k if k else 0, n, k, group, x.data_ptr(), ld_x, s_ptr, codes.data_ptr(),
+                           scales.data_ptr(), out.data_ptr(), ld_out, None, 0, _stream(stream))
+    L, ref = lib(), ctypes.byref(a)
+    need = L.pivot_linear4_workspace_size(ref)
     if need:
         buf = ws if ws is not None else workspace(need, x.device, stream)
         a.workspace, a.workspace_bytes = buf.data_ptr(), buf.numel() * buf.element_size()
-    _check(L.pivot_linear4(ctypes.byref(a)), "pivot_linear4")
+    _check(L.pivot_linear4(ref), "pivot_linear4")
     return out
 
 
+_ROWS = struct.Struct("Pi4x" * PIVOT_EVICT_MAX_ARRAYS)
+assert _ROWS.size == PIVOT_EVICT_MAX_ARRAYS * ctypes.sizeof(pivot_rows)
+
+
 def _row_arrays(arrays, rows, device):
-    """The C array of row arrays, one row a token along the first dimension."""
+    """The C array of row arrays, one row a token along the first dimension, as bytes."""
     if not 1 <= len(arrays) <= PIVOT_EVICT_MAX_ARRAYS:
         raise ValueError(f"a call takes 1 to {PIVOT_EVICT_MAX_ARRAYS} arrays")
-    c = (pivot_rows * len(arrays))()
+    words = []
     for i, x in enumerate(arrays):
         if x.get_device() != device:
             raise ValueError("the call's tensors must all be on one GPU")
-        if not x.is_contiguous() or x.shape[0] < rows:
+        n = x.shape[0]
+        if n < rows or not x.is_contiguous():
             raise ValueError(f"array {i} must be contiguous, with {rows} rows")
-        c[i].rows, c[i].row_bytes = x.data_ptr(), x.element_size() * (x.numel() // max(x.shape[0], 1))
-    return c
+        words += (x.data_ptr(), x.element_size() * (x.numel() // n if n else 1))
+    return _ROWS.pack(*words, *(0,) * (2 * PIVOT_EVICT_MAX_ARRAYS - len(words)))
 
 
 def pivot_tree_accept(path, pos0, arrays, row_map, stream=None):
@@ -1024,7 +1040,7 @@ def pivot_tree_accept(path, pos0, arrays, row_map, stream=None):
     _check_batch(row_map, len(pos0))
     _on_gpu(device, getattr(row_map, "_bt", None))
     c = _row_arrays(arrays, row_map.rows, device)
-    _check(lib().pivot_tree_accept(len(pos0), path.shape[1], _ptr(path), _host_ints(pos0), len(arrays), c,
+    _check(lib().pivot_tree_accept(len(pos0), path.shape[1], _ptr(path), _packed_ints(pos0), len(arrays), c,
                                    ctypes.byref(row_map), _stream(stream)), "pivot_tree_accept")
 
 
@@ -1057,7 +1073,7 @@ def pivot_pages_fork(pages, src, dst, tokens, stream=None):
     tokens of slots src[i]."""
     n = _same_length(src, dst, tokens)
     _on_gpu(pages._device)
-    _check(lib().pivot_pages_fork(ctypes.byref(pages), n, _host_ints(src), _host_ints(dst), _host_ints(tokens),
+    _check(lib().pivot_pages_fork(ctypes.byref(pages), n, _packed_ints(src), _packed_ints(dst), _packed_ints(tokens),
                                   _stream(stream)), "pivot_pages_fork")
 
 
@@ -1066,7 +1082,7 @@ def pivot_pages_free(pages, slots, tokens, keep, stream=None):
     more are free."""
     n = _same_length(slots, tokens, keep)
     _on_gpu(pages._device)
-    _check(lib().pivot_pages_free(ctypes.byref(pages), n, _host_ints(slots), _host_ints(tokens), _host_ints(keep),
+    _check(lib().pivot_pages_free(ctypes.byref(pages), n, _packed_ints(slots), _packed_ints(tokens), _packed_ints(keep),
                                   _stream(stream)), "pivot_pages_free")
 
 
@@ -1083,10 +1099,10 @@ def pivot_pages_grow(pages, slots, tokens, new_tokens, copies=None, state=None, 
               else _expect(copies, torch.int32, (n, 2), "copies"))
     state = (torch.empty((2,), dtype=torch.int32, device=device) if state is None
              else _expect(state, torch.int32, (2,), "state"))
-    L, now, then = lib(), _host_ints(tokens), _host_ints(new_tokens)
+    L, now, then = lib(), _packed_ints(tokens), _packed_ints(new_tokens)
     need = L.pivot_pages_grow_workspace_size(ctypes.byref(pages), n, now, then)
     buf = ws if ws is not None else workspace(need, device, stream)
-    _check(L.pivot_pages_grow(ctypes.byref(pages), n, _host_ints(slots), now, then, _ptr(copies), _ptr(state), _ptr(buf),
+    _check(L.pivot_pages_grow(ctypes.byref(pages), n, _packed_ints(slots), now, then, _ptr(copies), _ptr(state), _ptr(buf),
                               buf.numel() * buf.element_size(), _stream(stream)), "pivot_pages_grow")
     return copies, state
 

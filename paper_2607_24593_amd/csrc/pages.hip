@@ -9,9 +9,16 @@
 //   copy     whole pages of row arrays
 //
 // Which pages are taken does not depend on the order of threads: the k-th page
-// wanted is the k-th free one from below.  The pool is cut into blocks of kBlock
-// pages: one launch counts each block's free pages, the next lets every block add
-// up the counts before it and write its own pages where they belong.
+// wanted is the k-th free one from below.  A workgroup makes a map of bits of kBlock
+// pages in LDS, 64 at a ballot, scans the words' counts, and finds the k-th free page
+// of its block by bisection, neighbouring k in neighbouring lanes, so that entries
+// and counts are written side by side.
+// Pools of one block that few pages are taken of take one launch.  Else a launch
+// before writes the blocks' maps and counts (the second one changes refs, and several
+// workgroups share a block).
+// Bound by latency, a chain of dependent loads and bisections: 160 slots of a pool of
+// 4800 pages grow in 12 us; two slots by 4096 pages each in a pool of 87000 in 5 + 6 us
+// (by one workgroup a block 27).
 #include <algorithm>
 
 #include "cache4.h"
@@ -23,8 +30,8 @@ namespace pivot {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kBlock = 4096;  // pages, 16 a thread
-constexpr int kEach = kBlock / kThreads;
+constexpr int kBlockThreads = 1024;
+constexpr int kBlock = 32 * kBlockThreads;  // pages
 
 __device__ __forceinline__ bool in_pool(const Pages& p, int32_t page) { return (uint32_t)page < (uint32_t)p.n_pages; }
 __host__ __device__ __forceinline__ int pages_of(const Pages& p, int32_t tokens) {
@@ -74,147 +81,226 @@ __device__ __forceinline__ int block_scan(int x, int* total) {
   return before + sum - x;
 }
 
-// A thread's 16 pages of a block, neighbours: bit e set where page e is free.
-// Pages behind the pool are neither free nor live.
-__device__ __forceinline__ uint32_t free_bits(const Pages& p, int block, uint32_t* live) {
-  const int first = block * kBlock + kEach * threadIdx.x;
-  uint32_t bits = 0, used = 0;
+// A block's pages: which are free, as bits (word t those from 32 t on), and the free
+// ones before each word.  Pages behind the pool are not free.
+struct Block {
+  uint64_t map[kBlock / 64];
+  int32_t before[kBlockThreads];
+  __device__ uint32_t word(int t) const { return reinterpret_cast<const uint32_t*>(map)[t]; }
+  // its pages' number in the block: the k-th free one, the k-th that is not free
+  __device__ int free_page(int k) const { return find(k, false); }
+  __device__ int used_page(int k) const { return find(k, true); }
+
+  __device__ int find(int k, bool used) const {
+    int lo = 0, hi = kBlockThreads - 1;  // the last word with at most k before it
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if ((used ? 32 * mid - before[mid] : before[mid]) <= k) lo = mid;
+      else hi = mid - 1;
+    }
+    int n = k - (used ? 32 * lo - before[lo] : before[lo]), bit = 0;
+    uint32_t bits = used ? ~word(lo) : word(lo);
 #pragma unroll
-  for (int e = 0; e < kEach; ++e) {
-    if (first + e >= p.n_pages) break;
-    if (p.refs[first + e] == 0) bits |= 1u << e;
-    else used |= 1u << e;
+    for (int half = 16; half > 0; half >>= 1) {  // its n-th bit
+      const int c = __popc(bits & ((1u << half) - 1));
+      if (n >= c) {
+        n -= c;
+        bits >>= half;
+        bit += half;
+      }
+    }
+    return 32 * lo + bit;
   }
-  *live = used;
-  return bits;
+};
+__device__ __forceinline__ void map_block(const Pages& p, int block, Block* b) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = block * kBlock + (int)threadIdx.x;
+  int count[32];
+#pragma unroll
+  for (int j = 0; j < 32; ++j)  // always loaded: a load for some lanes only would be waited for before the next
+    count[j] = p.refs[min(first + kBlockThreads * j, p.n_pages - 1)];
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    const uint64_t map = __ballot(count[j] == 0 && first + kBlockThreads * j < p.n_pages);
+    if (lane == 0) b->map[kBlockThreads / 64 * j + wave] = map;
+  }
+  __syncthreads();
+}
+// The counts of the words before; returns all of the block's free pages.
+__device__ __forceinline__ int scan_block(Block* b) {
+  int total;
+  b->before[threadIdx.x] = block_scan<kBlockThreads>(__popc(b->word(threadIdx.x)), &total);
+  __syncthreads();
+  return total;
 }
 
-// What growing takes.  need[i]: pages before sequence i's in the list of those
-// taken, need[n]: all; copied[i]: whether its last page is copied.
+// Free pages in the blocks before this one (blockIdx.x), and in the pool; counts: of a
+// pool of more than one block.
+__device__ __forceinline__ int free_before(const int32_t* counts, int mine, int* all) {
+  if (gridDim.x == 1) {
+    *all = mine;
+    return 0;
+  }
+  int before = 0, sum = 0;
+  for (int i = threadIdx.x; i < (int)gridDim.x; i += kBlockThreads) {
+    const int c = counts[i];
+    sum += c;
+    before += i < (int)blockIdx.x ? c : 0;
+  }
+  block_scan<kBlockThreads>(sum, all);
+  int b;
+  block_scan<kBlockThreads>(before, &b);
+  return b;
+}
+
+// What growing takes.  first[i]: pages before sequence i's in the order they are
+// taken, first[n]: all; old[i]: its last page, if that is copied, else -1.
 struct Need {
   int32_t first[kMaxPageList + 1];
-  int32_t copied[kMaxPageList];
+  int32_t old[kMaxPageList];
 };
 
-__global__ __launch_bounds__(kThreads) void count_kernel(Pages p, int32_t* counts, int32_t* pairs, int n_pairs) {
-  const int at = blockIdx.x * kThreads + threadIdx.x, all = gridDim.x * kThreads;
-  for (int i = at; i < 2 * n_pairs; i += all) pairs[i] = -1;
-  uint32_t live;
-  const uint32_t bits = free_bits(p, blockIdx.x, &live);
-  int total;
-  block_scan<kThreads>(__popc(bits), &total);
-  if (threadIdx.x == 0) counts[blockIdx.x] = total;
-}
-
-__global__ __launch_bounds__(kMaxPageList) void need_kernel(Pages p, PageList l, Need* need) {
-  __shared__ int32_t s_last[kMaxPageList];
+// By the first kMaxPageList threads of a workgroup of T (all come here).
+template <int T>
+__device__ __forceinline__ void find_need(const Pages& p, const PageList& l, Need* need) {
+  __shared__ __attribute__((aligned(16))) int32_t s_last[kMaxPageList];
   const int i = threadIdx.x;
-  int32_t last = -1;
+  int32_t last = -1, holders = 0;
   int fresh = 0;
   if (i < l.n && l.b[i] > l.a[i]) {
     fresh = pages_of(p, l.b[i]) - pages_of(p, l.a[i]);
     if (l.a[i] & ((1 << p.shift) - 1)) last = p.table[(int64_t)l.slot[i] * p.max_pages + (l.a[i] >> p.shift)];
     if (!in_pool(p, last)) last = -1;
+    if (last >= 0) holders = p.refs[last];
   }
-  s_last[i] = last;
+  if (i < kMaxPageList) s_last[i] = last;
   __syncthreads();
   int copied = 0;
-  if (last >= 0) {
+  if (holders > 1) {
     int rank = 0;  // of the call's sequences before this one that hold the page
-    for (int j = 0; j < i; ++j) rank += s_last[j] == last;
-    copied = rank < p.refs[last] - 1;  // the last holder keeps it
+    for (int j = 0; j < i; j += 4) {
+      const int4 v = *reinterpret_cast<const int4*>(&s_last[j]);
+      rank += (v.x == last) + (j + 1 < i && v.y == last) + (j + 2 < i && v.z == last) + (j + 3 < i && v.w == last);
+    }
+    copied = rank < holders - 1;  // the last holder keeps it
   }
   int total;
-  const int first = block_scan<kMaxPageList>(copied + fresh, &total);
+  const int first = block_scan<T>(copied + fresh, &total);
   if (i < l.n) {
     need->first[i] = first;
-    need->copied[i] = copied;
+    need->old[i] = copied ? last : -1;
   }
   if (i == 0) need->first[l.n] = total;
 }
 
-// Free pages before this block, and in the pool.
-__device__ __forceinline__ int free_before(const int32_t* counts, int blocks, int block, int* all) {
-  int before = 0, sum = 0;
-  for (int i = threadIdx.x; i < blocks; i += kThreads) {
-    const int c = counts[i];
-    sum += c;
-    before += i < block ? c : 0;
+// The blocks' free pages and maps, and (one workgroup more) what growing takes.
+__global__ __launch_bounds__(kBlockThreads) void count_kernel(Pages p, PageList l, int blocks, int32_t* counts,
+                                                              uint64_t* maps, Need* need, int32_t* pairs, int n_pairs) {
+  __shared__ Block s_block;
+  const int at = blockIdx.x * kBlockThreads + threadIdx.x, all = gridDim.x * kBlockThreads;
+  for (int64_t i = at; i < 2 * (int64_t)n_pairs; i += all) pairs[i] = -1;
+  if ((int)blockIdx.x == blocks) {
+    find_need<kBlockThreads>(p, l, need);
+    return;
   }
-  block_scan<kThreads>(sum, all);
-  int b;
-  block_scan<kThreads>(before, &b);
-  return b;
+  map_block(p, blockIdx.x, &s_block);
+  const int total = scan_block(&s_block);
+  if (threadIdx.x == 0) counts[blockIdx.x] = total;
+  if (maps && threadIdx.x < kBlock / 64) maps[(int64_t)blockIdx.x * (kBlock / 64) + threadIdx.x] = s_block.map[threadIdx.x];
 }
 
-// The list of the pages that are taken, and their counts.
-__global__ __launch_bounds__(kThreads) void take_kernel(Pages p, int n, const int32_t* counts, const Need* need,
-                                                        int32_t* list, int32_t* state) {
-  int all, total;
-  const int before = free_before(counts, gridDim.x, blockIdx.x, &all);
-  const int want = need->first[n];
-  if (blockIdx.x == 0 && threadIdx.x == 0) {
+// The last of n ascending values (the first of them 0) that is at most x.
+__device__ __forceinline__ int last_at_most(const int32_t* v, int n, int x) {
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (v[mid] <= x) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+
+// maps: NULL in the one launch of a pool of one block
+__global__ __launch_bounds__(kBlockThreads) void grow_kernel(Pages p, PageList l, const int32_t* counts,
+                                                             const uint64_t* maps, const Need* need, int32_t* pairs,
+                                                             int32_t* state) {
+  __shared__ Block s_block;
+  __shared__ Need s_need;
+  __shared__ PageList s_list;  // read at places that differ between threads
+  const int tid = threadIdx.x;
+  if (tid < l.n) {
+    s_list.slot[tid] = l.slot[tid];
+    s_list.a[tid] = l.a[tid];
+  }
+  if (!maps) {
+    find_need<kBlockThreads>(p, l, &s_need);
+    if (tid < 2 * l.n) pairs[tid] = -1;
+    map_block(p, blockIdx.x, &s_block);
+  } else {
+    if (tid <= l.n) s_need.first[tid] = need->first[tid];
+    if (tid < l.n) s_need.old[tid] = need->old[tid];
+    if (tid < kBlock / 64) s_block.map[tid] = maps[(int64_t)blockIdx.x * (kBlock / 64) + tid];
+    __syncthreads();
+  }
+  const int total = scan_block(&s_block);
+  int all;
+  const int before = free_before(counts, total, &all);
+  const int want = s_need.first[l.n];
+  if (blockIdx.x == 0 && blockIdx.y == 0 && tid == 0) {
     state[0] = want > all ? want - all : 0;
     state[1] = want > all ? all : all - want;
   }
-  if (want > all || before >= want) return;
-  uint32_t live, bits = free_bits(p, blockIdx.x, &live);
-  int at = before + block_scan<kThreads>(__popc(bits), &total);
-  for (; bits && at < want; bits &= bits - 1, ++at) {
-    const int page = blockIdx.x * kBlock + kEach * threadIdx.x + __ffs(bits) - 1;
-    list[at] = page;
+  if (want > all) return;
+  const int mine = min(total, want - before);
+  for (int k = blockIdx.y * kBlockThreads + tid; k < mine; k += gridDim.y * kBlockThreads) {
+    const int page = blockIdx.x * kBlock + s_block.free_page(k);
+    const int at = before + k, i = last_at_most(s_need.first, l.n, at), j = at - s_need.first[i];
+    const int old = s_need.old[i], now = s_list.a[i];
+    const bool copy = old >= 0 && j == 0;
+    p.table[(int64_t)s_list.slot[i] * p.max_pages + (copy ? now >> p.shift : pages_of(p, now) + j - (old >= 0))] = page;
     p.refs[page] = 1;
+    if (copy) {
+      pairs[2 * i] = old;
+      pairs[2 * i + 1] = page;
+      atomicSub(p.refs + old, 1);
+    }
   }
-}
-
-__global__ __launch_bounds__(kThreads) void assign_kernel(Pages p, PageList l, const Need* need, const int32_t* list,
-                                                          const int32_t* state, int32_t* pairs) {
-  if (state[0] > 0) return;  // too few: nothing happens
-  const int i = blockIdx.x, j = blockIdx.y * kThreads + threadIdx.x;
-  const int first = need->first[i], n = need->first[i + 1] - first, copied = need->copied[i];
-  if (j >= n) return;
-  const int32_t page = list[first + j];
-  const int at = copied && j == 0 ? l.a[i] >> p.shift : pages_of(p, l.a[i]) + j - copied;
-  int32_t* entry = p.table + (int64_t)l.slot[i] * p.max_pages + at;
-  if (copied && j == 0) {
-    pairs[2 * i] = *entry;
-    pairs[2 * i + 1] = page;
-    atomicSub(p.refs + *entry, 1);
-  }
-  *entry = page;
 }
 
 // The moves of compacting, pairs (from, to): the k-th free page from below takes
 // the k-th page in use from above.  Of L pages in use as many lie at L and above as
 // there are free ones below L; those are the moves there are.
-__global__ __launch_bounds__(kThreads) void moves_kernel(Pages p, const int32_t* counts, int most, int32_t* pairs,
-                                                         int32_t* state) {
-  int all, total;
-  const int before = free_before(counts, gridDim.x, blockIdx.x, &all);
-  const int first = blockIdx.x * kBlock, in_use = p.n_pages - all;
-  uint32_t live, bits = free_bits(p, blockIdx.x, &live);
-  const int free_at = before + block_scan<kThreads>(__popc(bits), &total);
-  const int mine = first + kEach * (int)threadIdx.x;
-  int holes = 0;
-  for (int e = 0, at = free_at, used = min(mine, p.n_pages) - free_at; e < kEach && mine + e < p.n_pages; ++e) {
-    if (bits >> e & 1) {
-      if (mine + e < in_use) {
-        ++holes;
-        if (at < most) pairs[2 * at + 1] = mine + e;
-      }
-      ++at;
-    } else {
-      const int k = in_use - 1 - used;  // from above
-      if (mine + e >= in_use && k < most) pairs[2 * k] = mine + e;
-      ++used;
-    }
+__global__ __launch_bounds__(kBlockThreads) void moves_kernel(Pages p, const int32_t* counts, int most, int32_t* pairs,
+                                                              int32_t* state) {
+  __shared__ Block s_block;
+  __shared__ int s_holes;
+  const int tid = threadIdx.x, first = blockIdx.x * kBlock;
+  map_block(p, blockIdx.x, &s_block);
+  const int total = scan_block(&s_block);
+  int all;
+  const int before = free_before(counts, total, &all), in_use = p.n_pages - all;
+  const int size = min(p.n_pages - first, kBlock), below = min(max(in_use - first, 0), size);  // pages below L
+  if (tid == 0) {
+    const uint32_t low = below & 31 ? s_block.word(below >> 5) & ((1u << (below & 31)) - 1) : 0;
+    s_holes = below == kBlock ? total : s_block.before[below >> 5] + __popc(low);
   }
-  block_scan<kThreads>(holes, &total);
-  // the block that the L-th page lies in (the last one, if no page is free)
-  if (threadIdx.x == 0 && min(in_use, p.n_pages - 1) / kBlock == (int)blockIdx.x) {
-    state[0] = all == 0 ? 0 : min(before + total, most);
+  __syncthreads();
+  const int holes = s_holes;
+  for (int i = tid; i < holes && before + i < most; i += kBlockThreads)
+    pairs[2 * (int64_t)(before + i) + 1] = first + s_block.free_page(i);
+  const int used_before = first - before;
+  for (int u = size - total - 1 - tid; u >= below - holes; u -= kBlockThreads) {  // the highest ones first
+    const int k = in_use - 1 - (used_before + u);
+    if (k < most) pairs[2 * (int64_t)k] = first + s_block.used_page(u);
+  }
+  // the block that page L lies in (the last one, if no page is free)
+  if (min(in_use, p.n_pages - 1) / kBlock != (int)blockIdx.x) return;
+  const int n = min(before + holes, most);
+  if (tid == 0) {
+    state[0] = n;
     state[1] = in_use;
   }
+  if (gridDim.x == 1)
+    for (int64_t i = 2 * (int64_t)n + tid; i < 2 * (int64_t)most; i += kBlockThreads) pairs[i] = -1;
 }
 
 // Counts and table entries of the pages that move.
@@ -285,22 +371,26 @@ hipError_t launch_pages_free(const Pages& p, const PageList& l, hipStream_t stre
   return hipGetLastError();
 }
 
-size_t pages_grow_workspace(const Pages& p, int64_t wanted) {
-  return round256(sizeof(Need)) + round256((size_t)pool_blocks(p) * 4) + round256((size_t)wanted * 4);
+size_t pages_grow_workspace(const Pages& p) {
+  return round256(sizeof(Need)) + round256((size_t)pool_blocks(p) * 4) + (size_t)pool_blocks(p) * (kBlock / 8);
 }
 
 hipError_t launch_pages_grow(const Pages& p, const PageList& l, int32_t* pairs, int32_t* state, void* workspace,
                              hipStream_t stream) {
-  uint8_t* ws = (uint8_t*)workspace;
-  Need* need = (Need*)ws;
-  int32_t* counts = (int32_t*)(ws + round256(sizeof(Need)));
-  int32_t* list = (int32_t*)((uint8_t*)counts + round256((size_t)pool_blocks(p) * 4));
-  const unsigned blocks = (unsigned)pool_blocks(p);
-  hipLaunchKernelGGL(count_kernel, dim3(blocks), dim3(kThreads), 0, stream, p, counts, pairs, l.n);
-  hipLaunchKernelGGL(need_kernel, dim3(1), dim3(kMaxPageList), 0, stream, p, l, need);
-  hipLaunchKernelGGL(take_kernel, dim3(blocks), dim3(kThreads), 0, stream, p, l.n, counts, need, list, state);
-  hipLaunchKernelGGL(assign_kernel, dim3((unsigned)l.n, blocks_of(std::max(0, most_pages(p, l, l.a, l.b)) + 1)),
-                     dim3(kThreads), 0, stream, p, l, need, list, state, pairs);
+  Need* need = (Need*)workspace;
+  int32_t* counts = (int32_t*)((uint8_t*)workspace + round256(sizeof(Need)));
+  const int blocks = pool_blocks(p);
+  uint64_t* maps = (uint64_t*)((uint8_t*)counts + round256((size_t)blocks * 4));
+  int64_t wanted = 0;
+  for (int i = 0; i < l.n; ++i) wanted += pages_of(p, l.b[i]) - pages_of(p, l.a[i]) + 1;
+  // workgroups that share a block: a round of bisections takes 2.5 us
+  const int parts = (int)std::min<int64_t>(std::min<int64_t>(wanted, kBlock) / kBlockThreads + 1, 8);
+  const bool one = blocks == 1 && parts <= 2;
+  if (!one)
+    hipLaunchKernelGGL(count_kernel, dim3((unsigned)blocks + 1), dim3(kBlockThreads), 0, stream, p, l, blocks, counts, maps,
+                       need, pairs, l.n);
+  hipLaunchKernelGGL(grow_kernel, dim3((unsigned)blocks, one ? 1u : (unsigned)parts), dim3(kBlockThreads), 0, stream, p, l,
+                     counts, one ? nullptr : maps, need, pairs, state);
   return hipGetLastError();
 }
 
@@ -308,10 +398,12 @@ size_t pages_compact_workspace(const Pages& p) { return round256((size_t)pool_bl
 
 hipError_t launch_pages_compact(const Pages& p, int32_t slots, int32_t most, int32_t* pairs, int32_t* state,
                                 void* workspace, hipStream_t stream) {
-  const unsigned blocks = (unsigned)pool_blocks(p);
+  const int blocks = pool_blocks(p);
   int32_t* counts = (int32_t*)workspace;
-  hipLaunchKernelGGL(count_kernel, dim3(blocks), dim3(kThreads), 0, stream, p, counts, pairs, most);
-  hipLaunchKernelGGL(moves_kernel, dim3(blocks), dim3(kThreads), 0, stream, p, counts, most, pairs, state);
+  if (blocks > 1)
+    hipLaunchKernelGGL(count_kernel, dim3((unsigned)blocks), dim3(kBlockThreads), 0, stream, p, PageList{}, blocks, counts,
+                       nullptr, nullptr, pairs, most);
+  hipLaunchKernelGGL(moves_kernel, dim3((unsigned)blocks), dim3(kBlockThreads), 0, stream, p, counts, most, pairs, state);
   const int64_t entries = (int64_t)slots * p.max_pages;
   hipLaunchKernelGGL(remap_kernel, dim3(blocks_of(std::max<int64_t>(entries, std::min(most, p.n_pages / 2 + 1)))),
                      dim3(kThreads), 0, stream, p, pairs, state, entries);

@@ -191,6 +191,20 @@ def test_list_refusals():
     assert L.pivot_pages_copy(p, 1, FAKE, 0, r, None) == BAD and L.pivot_pages_copy(p, 0, None, 1, r, None) == pv.PIVOT_OK
 
 
+@pytest.mark.parametrize("slots", [200, 1 << 15, 40000])
+def test_slots_that_come_twice(slots):
+    """Small tables look them up as bits, large ones sort."""
+    L, p = pv.lib(), ctypes.byref(pages(slots=slots))
+    for n in (2, 63, 64, 65, 200):
+        slot = list(range(slots - n, slots))
+        slot[-1] = slot[n // 2 - 1]
+        same = ints(*[5] * n)
+        assert L.pivot_pages_free(p, n, ints(*slot), same, same, None) == BAD and f"slot {slot[-1]} twice" in pv.last_error()
+        assert L.pivot_pages_fork(p, 1, ints(slot[0]), ints(slot[0]), ints(5), None) == BAD
+        assert L.pivot_pages_free(pages(slots=slots, refs=None), n, ints(*range(slots - n, slots)), same, same, None) == BAD
+        assert "refs" in pv.last_error()   # distinct slots come to the next check
+
+
 # ------------------------------------------------------------------ the binding
 def _pool():
     return pv.make_pages(torch.full((4, 8), -1, dtype=torch.int32), torch.zeros(20, dtype=torch.int32), 16)
