@@ -17,6 +17,7 @@ namespace {
 
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
 
 constexpr int kCus = 256;
 constexpr int kWaves = 8;
@@ -98,11 +99,39 @@ struct Ring {
 constexpr int kDirectRows = 4;  // up to here x is loaded straight into registers
 constexpr int64_t kMaxStride = 1 << 24;  // 64 rows so far apart have offsets of 32 bits
 
+// Four neighbouring outputs of row m from column n on.
+template <bool SCALED>
+__device__ __forceinline__ void put(const Linear4Args& a, int m, int n, v4f y) {
+  const float s = SCALED ? a.x_scale[m] : 1.f;
+  const int64_t at = m * a.ld_out + n;
+  if (a.out_fp32) {
+    float* to = (float*)a.out + at;
+    if (n + 4 <= a.n && ((uintptr_t)to & 15) == 0) {
+      *reinterpret_cast<v4f*>(to) = y * s;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (n + e < a.n) to[e] = y[e] * s;
+    }
+    return;
+  }
+  uint16_t* to = (uint16_t*)a.out + at;
+  const v4bf v = {(__bf16)(y[0] * s), (__bf16)(y[1] * s), (__bf16)(y[2] * s), (__bf16)(y[3] * s)};
+  if (n + 4 <= a.n && ((uintptr_t)to & 7) == 0) {
+    *reinterpret_cast<v4bf*>(to) = v;
+  } else {
+    const uint2 bits = __builtin_bit_cast(uint2, v);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (n + e < a.n) to[e] = (uint16_t)((e < 2 ? bits.x : bits.y) >> (16 * (e & 1)));
+  }
+}
+
 // What x holds.
 enum Rows : int { kRowsBf16, kRowsFp8, kRowsGroups };
 
 template <int MT, int KC, int X, bool WORDS>
-__global__ __launch_bounds__(64 * kWaves, 2) void linear4_kernel(Linear4Args a, Cut cut, float* parts) {
+__global__ __launch_bounds__(64 * kWaves, 2) void linear4_kernel(Linear4Args a, Cut cut, v4f* parts) {
   using R = Ring<MT, KC, WORDS>;
   constexpr bool GROUPS = X == kRowsGroups, FP8 = X != kRowsBf16;
   constexpr int PAIRED = KC / 2 * 2;  // chunks that come in pairs
@@ -343,36 +372,30 @@ __global__ __launch_bounds__(64 * kWaves, 2) void linear4_kernel(Linear4Args a, 
       v4f total = from[0];
       for (int j = 1; j < cut.kw; ++j) total += from[j * MT * 64];
       count(&s_added[at]);
-      const int m = row0 + 16 * t + r, n = 16 * (first + done * nw + tn) + 4 * g;
-      if (first + done * nw + tn >= last || m >= a.rows) continue;
-      if (parts) {
-        float* to = parts + ((int64_t)blockIdx.y * a.rows + m) * a.n;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (n + e < a.n) to[n + e] = total[e];
+      const int tile = first + done * nw + tn;
+      if (tile >= last) continue;
+      if (parts) {  // the registers as they lie: the joining kernel has the same lanes
+        parts[(((int64_t)blockIdx.y * gridDim.z + blockIdx.z) * MT + t) * cut.tiles * 64 + (int64_t)tile * 64 + lane] = total;
         continue;
       }
-      const float s = X == kRowsFp8 ? a.x_scale[m] : 1.f;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (n + e >= a.n) break;
-        const float y = total[e] * s;
-        if (a.out_fp32) ((float*)a.out)[m * a.ld_out + n + e] = y;
-        else ((uint16_t*)a.out)[m * a.ld_out + n + e] = bf16_rne(y);
-      }
+      const int m = row0 + 16 * t + r;
+      if (m < a.rows) put<X == kRowsFp8>(a, m, 16 * tile + 4 * g, total);
     }
   }
 }
 
-// The sums of the workgroups that share k, in their order.
-__global__ __launch_bounds__(256) void linear4_join_kernel(Linear4Args a, int splits, const float* parts) {
-  const int n = blockIdx.x * 256 + threadIdx.x, m = blockIdx.y;
-  if (n >= a.n) return;
-  float y = 0.f;
-  for (int s = 0; s < splits; ++s) y += parts[((int64_t)s * a.rows + m) * a.n + n];
-  if (a.x_fp8 && a.group == 0) y *= a.x_scale[m];
-  if (a.out_fp32) ((float*)a.out)[m * a.ld_out + n] = y;
-  else ((uint16_t*)a.out)[m * a.ld_out + n] = bf16_rne(y);
+// The sums of the workgroups that share k, in their order: a wave a tile of 16 rows x
+// 16 weight rows (blockIdx.y: 16 rows).
+__global__ __launch_bounds__(256) void linear4_join_kernel(Linear4Args a, int splits, int tiles, int64_t stride,
+                                                           const v4f* parts) {
+  const int lane = threadIdx.x & 63, tile = blockIdx.x * 4 + (threadIdx.x >> 6), m = 16 * blockIdx.y + (lane & 15);
+  if (tile >= tiles) return;
+  const v4f* from = parts + (int64_t)blockIdx.y * tiles * 64 + (int64_t)tile * 64 + lane;
+  v4f y = from[0];
+  for (int s = 1; s < splits; ++s) y += from[s * stride];
+  if (m >= a.rows) return;
+  if (a.x_fp8 && a.group == 0) put<true>(a, m, 16 * tile + 4 * (lane >> 4), y);
+  else put<false>(a, m, 16 * tile + 4 * (lane >> 4), y);
 }
 
 // Rows of 32 weights to codes and a scale, 8 values a lane (cache4.hip says how).
@@ -433,8 +456,14 @@ Plan plan_of(const Linear4Args& a) {
   return p;
 }
 
+// Sums of a workgroup's part of k, four a lane.
+int64_t part_of(const Linear4Args& a, const Plan& p) {
+  const int64_t blocks = (a.rows + 16 * p.mt - 1) / (16 * p.mt);
+  return blocks * p.mt * p.cut.tiles * 64;
+}
+
 template <int MT, int KC, int X>
-void launch_words(const Linear4Args& a, const Plan& p, float* parts, hipStream_t stream) {
+void launch_words(const Linear4Args& a, const Plan& p, v4f* parts, hipStream_t stream) {
   const dim3 grid((unsigned)p.cut.groups, (unsigned)p.cut.splits, (unsigned)((a.rows + 16 * MT - 1) / (16 * MT)));
   if (a.k % kChunk == 0 && ((uintptr_t)a.scales & 3) == 0)
     hipLaunchKernelGGL((linear4_kernel<MT, KC, X, true>), grid, dim3(64 * kWaves), 0, stream, a, p.cut, parts);
@@ -442,7 +471,7 @@ void launch_words(const Linear4Args& a, const Plan& p, float* parts, hipStream_t
     hipLaunchKernelGGL((linear4_kernel<MT, KC, X, false>), grid, dim3(64 * kWaves), 0, stream, a, p.cut, parts);
 }
 template <int MT, int KC>
-void launch(const Linear4Args& a, const Plan& p, float* parts, hipStream_t stream) {
+void launch(const Linear4Args& a, const Plan& p, v4f* parts, hipStream_t stream) {
   if (!a.x_fp8) launch_words<MT, KC, kRowsBf16>(a, p, parts, stream);
   else if (!a.group) launch_words<MT, KC, kRowsFp8>(a, p, parts, stream);
   else if constexpr (MT * KC <= 10) launch_words<MT, KC, kRowsGroups>(a, p, parts, stream);
@@ -452,12 +481,12 @@ void launch(const Linear4Args& a, const Plan& p, float* parts, hipStream_t strea
 
 size_t linear4_workspace(const Linear4Args& a) {
   const Plan p = plan_of(a);
-  return p.cut.splits > 1 ? (size_t)p.cut.splits * a.rows * a.n * 4 : 0;
+  return p.cut.splits > 1 ? (size_t)p.cut.splits * part_of(a, p) * sizeof(v4f) : 0;
 }
 
 hipError_t launch_linear4(const Linear4Args& a, void* workspace, hipStream_t stream) {
   const Plan p = plan_of(a);
-  float* parts = p.cut.splits > 1 ? (float*)workspace : nullptr;
+  v4f* parts = p.cut.splits > 1 ? (v4f*)workspace : nullptr;
   switch (10 * p.mt + p.kc) {
     case 11: launch<1, 1>(a, p, parts, stream); break;
     case 12: launch<1, 2>(a, p, parts, stream); break;
@@ -478,8 +507,8 @@ hipError_t launch_linear4(const Linear4Args& a, void* workspace, hipStream_t str
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !parts) return e;
-  hipLaunchKernelGGL(linear4_join_kernel, dim3((unsigned)((a.n + 255) / 256), (unsigned)a.rows), dim3(256), 0, stream, a,
-                     p.cut.splits, parts);
+  hipLaunchKernelGGL(linear4_join_kernel, dim3((unsigned)((p.cut.tiles + 3) / 4), (unsigned)((a.rows + 15) / 16)), dim3(256),
+                     0, stream, a, p.cut.splits, p.cut.tiles, part_of(a, p), parts);
   return hipGetLastError();
 }
 
