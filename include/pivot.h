@@ -578,7 +578,8 @@ pivot_status pivot_evict(const pivot_evict_args* a);
  *                            aligned
  *   scales  dev [n, k / 32]  E8M0: 2^(byte - 127) of each 32 values, 255 = NaN
  * as in the 4-bit cache (weights of 2^128 and more are infinite).  k is a multiple
- * of 32 (else PIVOT_ERR_UNSUPPORTED), at most PIVOT_LINEAR4_MAX_K; n is any.
+ * of 32, at most PIVOT_LINEAR4_MAX_K, n at most PIVOT_LINEAR4_MAX_N (else
+ * PIVOT_ERR_UNSUPPORTED).
  *   x       dev, rows ld_x >= k values apart: PIVOT_DT_BF16, or PIVOT_DT_FP8_E4M3
  *           with x_scale dev fp32 [n_rows, group ? ceil(k / 128) : 1], group 0 (one
  *           scale a row) or 128, as pivot_rmsnorm_fp8 writes them.  Pointers need
@@ -593,6 +594,7 @@ pivot_status pivot_evict(const pivot_evict_args* a);
  * invalid shapes or none needed).
  */
 #define PIVOT_LINEAR4_MAX_K (1 << 20)
+#define PIVOT_LINEAR4_MAX_N (1 << 30)
 typedef struct {
   int32_t x_dtype, out_dtype;
   int32_t n_rows, n, k;
@@ -669,7 +671,8 @@ pivot_status pivot_tree_accept(int32_t batch, int32_t n, const int32_t* path, co
  * page_size is a power of two in [16, 65536], n_pages * page_size and slots *
  * max_pages at most 2^31 - 1.  A pool starts with every entry -1 and every count 0.
  * Lists are host arrays of at most PIVOT_PAGES_MAX_LIST entries (else
- * UNSUPPORTED), slots in [0, slots), tokens in [0, max_pages * page_size].  Table
+ * UNSUPPORTED), slots in [0, slots), tokens in [0, max_pages * page_size] and at most
+ * PIVOT_MAX_KEYS (else UNSUPPORTED).  A call grows by at most 2^30 pages.  Table
  * entries that name no page of the pool are left alone.
  * Calls that change one pool run in the order of one stream.
  */

@@ -31,7 +31,7 @@ PIVOT_REFINE_AUTO, PIVOT_REFINE_FUSED, PIVOT_REFINE_SPLIT = 0, 1, 2
 H, D = 64, 128
 PIVOT_CACHE4_LATENT, PIVOT_CACHE4_ROPE = 512, 64
 PIVOT_ATTEND_MAX_HEADS, PIVOT_EVICT_MAX_ARRAYS = 128, 8
-PIVOT_LINEAR4_MAX_K, PIVOT_TREE_MAX_NODES, PIVOT_PAGES_MAX_LIST = 1 << 20, 1024, 256
+PIVOT_LINEAR4_MAX_K, PIVOT_LINEAR4_MAX_N, PIVOT_TREE_MAX_NODES, PIVOT_PAGES_MAX_LIST = 1 << 20, 1 << 30, 1024, 256
 
 EXPORTED = ["pivot_workspace_size", "pivot_dense_index", "pivot_group_index", "pivot_cand_width",
             "pivot_group_workspace_size", "pivot_group_index_opts", "pivot_dense_index_layout",

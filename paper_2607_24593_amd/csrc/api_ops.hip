@@ -372,7 +372,19 @@ pivot_status check_tokens(const pivot_pages* p, int n, const int32_t* low, const
       return fail(PIVOT_ERR_INVALID_ARG, "entry %d: %d and %d tokens", i, low ? low[i] : 0, high[i]);
     if (high[i] > (int64_t)p->max_pages * p->page_size)
       return fail(PIVOT_ERR_INVALID_ARG, "entry %d: %d tokens exceed max_pages*page_size", i, high[i]);
+    if (high[i] > PIVOT_MAX_KEYS)
+      return fail(PIVOT_ERR_UNSUPPORTED, "entry %d: %d tokens exceed PIVOT_MAX_KEYS=%d", i, high[i], PIVOT_MAX_KEYS);
   }
+  return PIVOT_OK;
+}
+
+// The pages that a growth takes are counted in 32 bits.
+pivot_status check_growth(const pivot_pages* p, int n, const int32_t* tokens, const int32_t* new_tokens) {
+  const pivot_status s = check_tokens(p, n, tokens, new_tokens);
+  if (s != PIVOT_OK) return s;
+  int64_t want = 0;
+  for (int i = 0; i < n; ++i) want += (int64_t)(new_tokens[i] - tokens[i]) / p->page_size + 2;
+  if (want > (1 << 30)) return fail(PIVOT_ERR_UNSUPPORTED, "growth by %lld pages", (long long)want);
   return PIVOT_OK;
 }
 
@@ -395,6 +407,7 @@ pivot_status check_linear4(const pivot_linear4_args* a) {
   if (a->out_dtype != PIVOT_DT_BF16 && a->out_dtype != PIVOT_DT_FP32)
     return fail(PIVOT_ERR_UNSUPPORTED, "out_dtype %d: bf16 or fp32", a->out_dtype);
   if (a->n_rows < 0 || a->n < 0) return fail(PIVOT_ERR_INVALID_ARG, "n_rows and n must be >= 0");
+  if (a->n > PIVOT_LINEAR4_MAX_N) return fail(PIVOT_ERR_UNSUPPORTED, "n=%d exceeds %d", a->n, PIVOT_LINEAR4_MAX_N);
   if (a->k < 1) return fail(PIVOT_ERR_INVALID_ARG, "k must be >= 1");
   if (a->k % kBlk || a->k > PIVOT_LINEAR4_MAX_K)
     return fail(PIVOT_ERR_UNSUPPORTED, "k=%d must be a multiple of %d up to %d", a->k, kBlk, PIVOT_LINEAR4_MAX_K);
@@ -699,7 +712,7 @@ pivot_status pivot_pages_free(const pivot_pages* p, int32_t n, const int32_t* sl
 }
 
 size_t pivot_pages_grow_workspace_size(const pivot_pages* p, int32_t n, const int32_t* tokens, const int32_t* new_tokens) {
-  if (check_list(p, n) != PIVOT_OK || n == 0 || !tokens || check_tokens(p, n, tokens, new_tokens) != PIVOT_OK) return 0;
+  if (check_list(p, n) != PIVOT_OK || n == 0 || !tokens || check_growth(p, n, tokens, new_tokens) != PIVOT_OK) return 0;
   return pages_grow_workspace(pages_at(p));
 }
 
@@ -712,7 +725,7 @@ pivot_status pivot_pages_grow(const pivot_pages* p, int32_t n, const int32_t* sl
   SlotSet slots;
   if ((s = check_slots(p, n, slot, &slots, "slot")) != PIVOT_OK) return s;
   if (!tokens) return fail(PIVOT_ERR_INVALID_ARG, "the numbers of tokens (host arrays) are required");
-  if ((s = check_tokens(p, n, tokens, new_tokens)) != PIVOT_OK) return s;
+  if ((s = check_growth(p, n, tokens, new_tokens)) != PIVOT_OK) return s;
   if ((s = check_pool(p)) != PIVOT_OK) return s;
   if (!copies || !state || !aligned(copies, 4) || !aligned(state, 4))
     return fail(PIVOT_ERR_INVALID_ARG, "copies and state are required, 4-byte aligned");

@@ -1183,45 +1183,50 @@ __global__ __launch_bounds__(256) void dense_weights_kernel(AttendArgs a, RunTab
   if (tid < kTileKeys && s < n) a.acc[(int64_t)b * a.acc_stride + s] += w;
 }
 
-// The same for trees, where a call has many rows: 32 rows at a time, each thread 4
+// The same for trees, where a call has many rows: T / 8 rows at a time, each thread 4
 // keys, four loads on their way.  Rows whose mask does not name a node are left out,
-// not added as zeros.  Bound by the scores' bytes: 192 rows x 196000 keys in 36 us,
-// 4.2 TB/s (one key a thread: 52).
-__global__ __launch_bounds__(256) void tree_weights_kernel(AttendArgs a, RunTable t, ScoreMap sm, TreeMask tree) {
-  __shared__ float red[4][kTileKeys];
+// not added as zeros.  T = 1024 from 1024 rows a sequence on: a short sequence has few
+// tiles.  Bound by the scores' bytes: 192 rows x 196000 keys in 25 us, 6 TB/s (one key
+// a thread: 52); 2940 rows x 375 keys: a call of 103 us with 256 threads and the masks
+// read row by row, 55 with 1024 and the masks beside the scores.
+template <int T>
+__global__ __launch_bounds__(T) void tree_weights_kernel(AttendArgs a, RunTable t, ScoreMap sm, TreeMask tree) {
+  constexpr int R = T / 8;  // rows at a time
+  __shared__ float red[T / 64][kTileKeys];
   const int b = blockIdx.y, tile = blockIdx.x, tid = threadIdx.x;
   const int n = t.n_k[b], rows = t.n_rows[b] * a.heads;
   if (rows == 0 || tile * kTileKeys >= n) return;
   const v4f* scores = reinterpret_cast<const v4f*>(sm.s2 + sm.base[b] + (int64_t)tile * rows * kTileKeys) + tid;
   const float2* stat = sm.stat + (int64_t)t.row0[b] * a.heads;
   v4f w = {0.f, 0.f, 0.f, 0.f};
-  if (tile * kTileKeys + kTileKeys <= tree.base[b]) {
-    for (int r = tid >> 3; r < rows; r += 128) {
-      v4f z[4];
-      float2 st[4];
+  // the tree's nodes that the thread's keys are (before it: negative), the two words of
+  // a mask that hold them
+  const int node = tile * kTileKeys + 4 * (tid & 7) - tree.base[b], word = max(node, 0) >> 5;
+  const bool drafts = tile * kTileKeys + kTileKeys > tree.base[b];
+  const int w0 = min(word, tree.words - 1), w1 = min(word + 1, tree.words - 1);
+  for (int r = tid >> 3; r < rows; r += 4 * R) {
+    v4f z[4];
+    float2 st[4];
+    uint32_t m0[4], m1[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int at = min(r + 32 * j, rows - 1);
-        z[j] = scores[(at - (tid >> 3)) * (kTileKeys / 4)];
-        st[j] = stat[at];
+    for (int j = 0; j < 4; ++j) {
+      const int at = min(r + R * j, rows - 1);
+      z[j] = scores[(at - (tid >> 3)) * (kTileKeys / 4)];
+      st[j] = stat[at];
+      if (drafts) {
+        const uint32_t* mask = tree.bits + (int64_t)(t.row0[b] + at / a.heads) * tree.words;
+        m0[j] = mask[w0];
+        m1[j] = mask[w1];
       }
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (r + 32 * j < rows) w[i] = fmaf(__builtin_amdgcn_exp2f(z[j][i] - st[j].x), st[j].y, w[i]);
     }
-  } else {
-    const int node = tile * kTileKeys + 4 * (tid & 7) - tree.base[b];
-    for (int r = tid >> 3; r < rows; r += 32) {
-      const uint32_t* mask = tree.bits + (int64_t)(t.row0[b] + r / a.heads) * tree.words;
-      const v4f z = scores[(r - (tid >> 3)) * (kTileKeys / 4)];
-      const float2 st = stat[r];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint64_t bits = (uint64_t)m1[j] << 32 | m0[j];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int at = node + i;
-        const bool seen = at < 0 || (at < n - tree.base[b] && (mask[at >> 5] >> (at & 31) & 1u));
-        if (seen) w[i] = fmaf(__builtin_amdgcn_exp2f(z[i] - st.x), st.y, w[i]);
+        bool seen = r + R * j < rows;
+        if (drafts && node + i >= 0) seen = seen && (bits >> (node + i - 32 * word) & 1) && node + i < n - tree.base[b];
+        if (seen) w[i] = fmaf(__builtin_amdgcn_exp2f(z[j][i] - st[j].x), st[j].y, w[i]);
       }
     }
   }
@@ -1233,8 +1238,12 @@ __global__ __launch_bounds__(256) void tree_weights_kernel(AttendArgs a, RunTabl
   }
   __syncthreads();
   const int s = tile * kTileKeys + tid;
-  if (tid < kTileKeys && s < n)
-    a.acc[(int64_t)b * a.acc_stride + s] += (red[0][tid] + red[1][tid]) + (red[2][tid] + red[3][tid]);
+  if (tid < kTileKeys && s < n) {
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < T / 64; ++j) sum += red[j][tid];
+    a.acc[(int64_t)b * a.acc_stride + s] += sum;
+  }
 }
 
 __global__ __launch_bounds__(256) void slot_weights_kernel(AttendArgs a, ScoreMap sm, float* __restrict__ slots,
@@ -1459,9 +1468,14 @@ hipError_t launch_call(const AttendArgs& a, const RunTable& t, const TreeOf<CALL
   if (e != hipSuccess || !a.acc || (a.idx && a.topk == 0)) return e;
   if (!a.idx) {
     const unsigned tiles = (unsigned)((p.max_n + kTileKeys - 1) / kTileKeys);
-    if constexpr (TREE)
-      hipLaunchKernelGGL(tree_weights_kernel, dim3(tiles, (unsigned)t.n), dim3(256), 0, stream, a, t, sm, tree);
-    else
+    if constexpr (TREE) {
+      int most = 0;
+      for (int b = 0; b < t.n; ++b) most = std::max(most, t.n_rows[b]);
+      if (most * a.heads >= 1024)
+        hipLaunchKernelGGL(tree_weights_kernel<1024>, dim3(tiles, (unsigned)t.n), dim3(1024), 0, stream, a, t, sm, tree);
+      else
+        hipLaunchKernelGGL(tree_weights_kernel<256>, dim3(tiles, (unsigned)t.n), dim3(256), 0, stream, a, t, sm, tree);
+    } else
       hipLaunchKernelGGL(dense_weights_kernel, dim3(tiles, (unsigned)t.n), dim3(256), 0, stream, a, t, sm);
     return hipGetLastError();
   }

@@ -197,8 +197,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void linear4_kernel(Linear4Args a, 
   if (steps > 0) load(0, 0);
   if (direct) {
 #pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int c = 0; c < KC; ++c)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[t][c][u] = uint4{0, 0, 0, 0};
+#pragma unroll
     for (int t = 0; t < MT; ++t) {
-      const int64_t m = min(row0 + 16 * t + r, a.rows - 1);
+      const int64_t m = row0 + 16 * t + r;
+      if (m >= a.rows) continue;  // a load takes as long as its lanes are many
 #pragma unroll
       for (int c = 0; c < KC; ++c)
 #pragma unroll

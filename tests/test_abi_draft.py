@@ -32,7 +32,7 @@ def linear(**kw):
 
 LINEAR = [
     (dict(x_dtype=2), UNS), (dict(x_dtype=-1), UNS), (dict(out_dtype=1), UNS), (dict(n_rows=-1), BAD), (dict(n=-1), BAD),
-    (dict(k=0), BAD), (dict(k=-32), BAD), (dict(k=48), UNS), (dict(k=(1 << 20) + 32, ld_x=1 << 21), UNS),
+    (dict(n=(1 << 30) + 1, ld_out=1 << 31), UNS), (dict(k=0), BAD), (dict(k=-32), BAD), (dict(k=48), UNS), (dict(k=(1 << 20) + 32, ld_x=1 << 21), UNS),
     (dict(group=128), UNS), (dict(x_dtype=1, group=64, x_scale=FAKE), UNS), (dict(ld_x=511), BAD), (dict(ld_out=99), BAD),
     (dict(x=None), BAD), (dict(codes=None), BAD), (dict(scales=None), BAD), (dict(out=None), BAD), (dict(x_dtype=1), BAD),
     (dict(codes=FAKE + 8), BAD), (dict(x=FAKE + 1), BAD), (dict(out=FAKE + 1), BAD), (dict(out_dtype=2, out=FAKE + 2), BAD),
@@ -165,6 +165,15 @@ def test_list_refusals():
     assert fork([0, 0], [1, 1], [5, 5]) == BAD and fork([0, 1], [1, 2], [5, 5]) == BAD and fork([3], [3], [5]) == BAD
     assert L.pivot_pages_fork(p, 1, None, ints(1), ints(5), None) == BAD
     assert L.pivot_pages_fork(p, 1, ints(0), ints(1), None, None) == BAD
+    long = ctypes.byref(pages(slots=2, max_pages=1 << 24))
+    assert L.pivot_pages_fork(long, 1, ints(0), ints(1), ints(pv.PIVOT_MAX_KEYS + 1), None) == UNS
+    assert L.pivot_pages_free(long, 1, ints(0), ints(pv.PIVOT_MAX_KEYS + 1), ints(1), None) == UNS
+    assert L.pivot_pages_grow(long, 1, ints(0), ints(0), ints(pv.PIVOT_MAX_KEYS + 1), FAKE, FAKE, FAKE, 1 << 40, None) == UNS
+    wide = ctypes.byref(pages(slots=200, max_pages=1 << 23))
+    most = ints(*[pv.PIVOT_MAX_KEYS] * 200)
+    none = ints(*[0] * 200)
+    assert L.pivot_pages_grow(wide, 200, ints(*range(200)), none, most, FAKE, FAKE, FAKE, 1 << 40, None) == UNS
+    assert L.pivot_pages_grow_workspace_size(wide, 200, none, most) == 0
     assert free([0, 0], [5, 5], [1, 1]) == BAD and free([0], [5], [6]) == BAD and free([0], [5], [-1]) == BAD
     assert free([8], [5], [1]) == BAD and free([0], [161], [1]) == BAD
     assert L.pivot_pages_free(p, 1, ints(0), ints(5), None, None) == BAD
