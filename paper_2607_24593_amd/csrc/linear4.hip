@@ -83,7 +83,7 @@ __device__ __forceinline__ void load_lds1(const void* base, uint32_t off, uint32
 // whose turn it is adds a tile's sums up kLag tiles later.
 // WORDS: the scales of a row's chunk are an aligned word (k a multiple of 128, the
 // array 4-byte aligned), else single bytes, each a word in LDS.
-constexpr int kLds = 160 * 1024 - 256;
+constexpr int kLds = 160 * 1024 - 512;
 template <int MT, int KC, bool WORDS>
 struct Ring {
   static constexpr int kSums = MT == 1 ? 4 : MT == 2 ? 3 : 2, kLag = kSums > 2 ? kSums - 2 : 1;
@@ -99,10 +99,8 @@ struct Ring {
 constexpr int kDirectRows = 4;  // up to here x is loaded straight into registers
 constexpr int64_t kMaxStride = 1 << 24;  // 64 rows so far apart have offsets of 32 bits
 
-// Four neighbouring outputs of row m from column n on.
-template <bool SCALED>
-__device__ __forceinline__ void put(const Linear4Args& a, int m, int n, v4f y) {
-  const float s = SCALED ? a.x_scale[m] : 1.f;
+// Four neighbouring outputs of row m from column n on, times s.
+__device__ __forceinline__ void put(const Linear4Args& a, int m, int n, v4f y, float s) {
   const int64_t at = m * a.ld_out + n;
   if (a.out_fp32) {
     float* to = (float*)a.out + at;
@@ -139,6 +137,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void linear4_kernel(Linear4Args a, 
   constexpr int CHAINS = MT == 1 ? 4 : MT == 2 ? 2 : 1;  // sums that do not wait for each other
   __shared__ __attribute__((aligned(16))) uint8_t s_lds[kLds];
   __shared__ uint32_t s_arrived[R::kSums], s_added[R::kSums];
+  __shared__ float s_row[16 * MT];  // the rows' scales: a load in the loop would wait for the weights on their way
   // slot 0 of all waves, the sums, the other slots
   constexpr int SUMS = kWaves * R::kTile;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -155,6 +154,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void linear4_kernel(Linear4Args a, 
   const int first = group * each + min(group, rest), last = first + each + (group < rest);
   const int steps = (last - first + nw - 1) / nw;
   if (threadIdx.x < R::kSums) s_arrived[threadIdx.x] = s_added[threadIdx.x] = 0;
+  if (X == kRowsFp8 && threadIdx.x < 16 * MT) s_row[threadIdx.x] = a.x_scale[min(row0 + (int)threadIdx.x, a.rows - 1)];
 
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)s_lds;
   auto slot_at = [&](int slot) { return (slot * kWaves + w) * R::kTile + (slot ? R::kSumBytes : 0); };
@@ -386,7 +386,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void linear4_kernel(Linear4Args a, 
         continue;
       }
       const int m = row0 + 16 * t + r;
-      if (m < a.rows) put<X == kRowsFp8>(a, m, 16 * tile + 4 * g, total);
+      if (m < a.rows) put(a, m, 16 * tile + 4 * g, total, X == kRowsFp8 ? s_row[16 * t + r] : 1.f);
     }
   }
 }
@@ -401,8 +401,7 @@ __global__ __launch_bounds__(256) void linear4_join_kernel(Linear4Args a, int sp
   v4f y = from[0];
   for (int s = 1; s < splits; ++s) y += from[s * stride];
   if (m >= a.rows) return;
-  if (a.x_fp8 && a.group == 0) put<true>(a, m, 16 * tile + 4 * (lane >> 4), y);
-  else put<false>(a, m, 16 * tile + 4 * (lane >> 4), y);
+  put(a, m, 16 * tile + 4 * (lane >> 4), y, a.x_fp8 && a.group == 0 ? a.x_scale[m] : 1.f);
 }
 
 // Rows of 32 weights to codes and a scale, 8 values a lane (cache4.hip says how).
