@@ -140,6 +140,44 @@ def test_scale_of_a_row_may_be_anything():
     _check(torch.from_numpy(y[2:]), x8[2:], codes, scales, False, "scales")
 
 
+@pytest.mark.parametrize("rows", [1, 6, 30, 64])
+def test_every_fp8_code(rows):
+    """Every code's value, subnormal ones and both zeros among them, as a sum and alone; a
+    NaN code makes its row NaN."""
+    k = 288
+    codes, scales = plain.quantise(np.ones((3, k)))
+    x = np.tile((np.arange(k) % 256).astype(np.uint8), (rows, 1))
+    x[:, (x[0] & 127) == 127] = 0
+    x[rows - 1, k - 1] = 0xFF
+    value = ref.e4m3_value(x)
+    say("linear4 fp8 codes", rows)
+    y = pv.pivot_linear4(dev(x), dev(codes), dev(scales), x_scale=torch.ones((rows, 1), device="cuda"), dtype=torch.float32)
+    assert np.isnan(host(y)[rows - 1]).all() and not np.isnan(host(y)[:rows - 1]).any()
+    if rows > 1:
+        _check(y[:rows - 1], value[:rows - 1], codes, scales, False, "codes")
+    eye = np.zeros((256, 256))
+    np.fill_diagonal(eye, 1)
+    codes, scales = plain.quantise(eye)
+    x = np.zeros((rows, 256), np.uint8)
+    x[0] = np.arange(256)
+    x[0, [127, 255]] = 0
+    y = pv.pivot_linear4(dev(x), dev(codes), dev(scales), x_scale=torch.full((rows, 1), 2.0, device="cuda"), dtype=torch.float32)
+    assert np.array_equal(host(y)[0], 2 * ref.e4m3_value(x[0]).astype(np.float32))
+
+
+def test_weights_past_32_bits():
+    """4.6 GB of codes: a sum over k cut into eight parts, columns at both ends."""
+    n, k = 140001, 65536
+    g = torch.Generator(device="cuda").manual_seed(2)
+    codes = torch.randint(0, 256, (n, k // 2), generator=g, device="cuda", dtype=torch.uint8)
+    scales = torch.randint(120, 124, (n, k // 32), generator=g, device="cuda", dtype=torch.uint8)
+    x = torch.randn((2, k), generator=g, device="cuda").bfloat16()
+    say("linear4 past 32 bits")
+    y = pv.pivot_linear4(x, codes, scales, dtype=torch.float32)
+    at = torch.tensor([0, 1, 65535, 131071, 131072, 139990, 140000], device="cuda")
+    _check(y[:, at], x.double().cpu().numpy(), host(codes[at]), host(scales[at]), False, "far")
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("n,k", [(1, 32), (3, 96), (70, 512), (129, 1056)])
 def test_pack(dtype, n, k):
