@@ -1026,7 +1026,7 @@ def _row_arrays(arrays, rows, device):
         n = x.shape[0]
         if n < rows or not x.is_contiguous():
             raise ValueError(f"array {i} must be contiguous, with {rows} rows")
-        words += (x.data_ptr(), x.element_size() * (x.numel() // n if n else 1))
+        words += (x.data_ptr(), x.nbytes // n if n else 4)
     return _ROWS.pack(*words, *(0,) * (2 * PIVOT_EVICT_MAX_ARRAYS - len(words)))
 
 
@@ -1062,17 +1062,23 @@ def make_pages(table, refs, page_size) -> pivot_pages:
     return p
 
 
-def _same_length(*lists):
-    if len({len(v) for v in lists}) != 1:
+def _same_length(a, b, c):
+    n = len(a)
+    if len(b) != n or len(c) != n:
         raise ValueError("the lists must have one entry per sequence")
-    return len(lists[0])
+    return n
+
+
+def _pool_on_gpu(pages):
+    if pages._device < 0:
+        raise ValueError("the pool's tensors must be on a GPU")
 
 
 def pivot_pages_fork(pages, src, dst, tokens, stream=None):
     """Slots dst[i], without pages until now, share the pages of the first tokens[i]
     tokens of slots src[i]."""
     n = _same_length(src, dst, tokens)
-    _on_gpu(pages._device)
+    _pool_on_gpu(pages)
     _check(lib().pivot_pages_fork(ctypes.byref(pages), n, _packed_ints(src), _packed_ints(dst), _packed_ints(tokens),
                                   _stream(stream)), "pivot_pages_fork")
 
@@ -1081,7 +1087,7 @@ def pivot_pages_free(pages, slots, tokens, keep, stream=None):
     """Slots go back from tokens[i] to keep[i] tokens; pages that no slot holds any
     more are free."""
     n = _same_length(slots, tokens, keep)
-    _on_gpu(pages._device)
+    _pool_on_gpu(pages)
     _check(lib().pivot_pages_free(ctypes.byref(pages), n, _packed_ints(slots), _packed_ints(tokens), _packed_ints(keep),
                                   _stream(stream)), "pivot_pages_free")
 

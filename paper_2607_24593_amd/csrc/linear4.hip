@@ -91,7 +91,7 @@ __device__ __forceinline__ void load_lds1(const void* base, uint32_t off, uint32
 constexpr int kLds = 160 * 1024 - 512;
 template <int MT, int KC, bool WORDS>
 struct Ring {
-  static constexpr int kSums = MT == 1 ? 4 : MT == 2 ? 3 : 2, kLag = kSums > 2 ? kSums - 2 : 1;
+  static constexpr int kSums = MT == 1 ? 4 : 3, kLag = kSums > 2 ? kSums - 2 : 1;
   static constexpr int kSumBytes = kSums * kWaves * MT * 1024;
   static constexpr int kScaleLoads = WORDS ? (KC + 3) / 4 : KC;
   static constexpr int kLoads = KC + kScaleLoads;  // of a tile
