@@ -382,7 +382,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void linear4_kernel(Linear4Args a, 
       const int tn = item / MT, t = item % MT;
       const v4f* from = s_sum + ((at * kWaves + tn * cut.kw) * MT + t) * 64 + lane;
       v4f total = from[0];
-      for (int j = 1; j < cut.kw; ++j) total += from[j * MT * 64];
+      if (cut.kw == kWaves) {  // all read before the first is added
+        v4f others[kWaves - 1];
+#pragma unroll
+        for (int j = 1; j < kWaves; ++j) others[j - 1] = from[j * MT * 64];
+#pragma unroll
+        for (int j = 1; j < kWaves; ++j) total += others[j - 1];
+      } else {
+        for (int j = 1; j < cut.kw; ++j) total += from[j * MT * 64];
+      }
       count(&s_added[at]);
       const int tile = first + done * nw + tn;
       if (tile >= last) continue;
