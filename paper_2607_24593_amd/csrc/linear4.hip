@@ -84,8 +84,8 @@ __device__ __forceinline__ void load_lds1(const void* base, uint32_t off, uint32
 // Few rows are bound by the weights' bytes: 2 rows x 4096 x 73728 in 31 us, 5.1 TB/s
 // (met at a barrier every tile 50 us, loaded as 16 rows x 64 bytes 34).  More rows
 // also by x, which every workgroup loads (64 rows, half of 6144 values: 3 us at 64
-// bytes a cycle), the waves' sums and the parts that are joined: 64 rows x 6144 x 24576 in 33
-// + 5 us.  One token x 4096 x 4096 takes 6 us, latency.
+// bytes a cycle), the waves' sums and the parts that are joined: 64 rows x 6144 x
+// 24576 in 31 + 5 us.  One token x 4096 x 4096 takes 6 us, latency.
 // WORDS: the scales of a row's chunk are an aligned word (k a multiple of 128, the
 // array 4-byte aligned), else single bytes, each a word in LDS.
 constexpr int kLds = 160 * 1024 - 512;
@@ -459,8 +459,8 @@ struct Plan {
 };
 
 // As few workgroups share k as have registers for its part of x (a part more costs 8
-// bytes a sum, written and read): 26 rows x 5024 x 8203 took 19 + 4 us in two parts
-// and 19 in one.  Then one workgroup a CU, which has the LDS to itself.
+// bytes a sum, written and read): 26 rows x 5024 x 8203 take 14 + 4 us in two parts
+// and 15 in one.  Then one workgroup a CU, which has the LDS to itself.
 Plan plan_of(const Linear4Args& a) {
   Plan p{};
   p.mt = a.rows <= 16 ? 1 : a.rows <= 32 ? 2 : 4;
