@@ -648,8 +648,9 @@ pivot_status pivot_cache4_attend_tree(const pivot_attend_args* a, const pivot_tr
  * it: row pos0[b] + path[b][j] of every array under `map` becomes row pos0[b] + j,
  * in place.
  *   path    dev int32 [batch, n]: the accepted nodes in ascending order, then -1.
- *           An entry that is not above the one before it, or past what the map can
- *           hold, ends the path as -1 does.
+ *           An entry that is not above the one before it, past what the map can
+ *           hold, or from or to a position whose block_table entry is outside the
+ *           pool, ends the path as -1 does.
  *   pos0    host [batch]: the tree's first position
  *   arrays  n_arrays (1 .. PIVOT_EVICT_MAX_ARRAYS) row arrays, rows of a multiple of
  *           4 bytes, 4-byte aligned

@@ -1033,7 +1033,8 @@ def _row_arrays(arrays, rows, device):
 def pivot_tree_accept(path, pos0, arrays, row_map, stream=None):
     """Move the accepted nodes of each sequence's tree to the positions that follow
     its prefix, in place in every row array: row pos0[b] + path[b, j] becomes row
-    pos0[b] + j.  path: int32 [B, n], ascending, -1 behind the last accepted node."""
+    pos0[b] + j.  path: int32 [B, n], ascending, -1 behind the last accepted node; it
+    ends too where the table has no page of the pool."""
     if path.dtype != torch.int32 or path.dim() != 2 or not path.is_contiguous() or path.shape[0] != len(pos0):
         raise ValueError("path must be a contiguous int32 [len(pos0), n] tensor")
     device = path.get_device()

@@ -300,3 +300,28 @@ def test_paths_that_are_none():
         say("accept, paths that end", page)
         pv.pivot_tree_accept(dev(path), pos0, [x], pool.map)
         assert torch.equal(x.cpu(), want)
+
+
+def test_paths_stop_at_pages_that_are_none():
+    """A position whose table entry names no page ends the path, read or written: no
+    row of another sequence's page changes."""
+    rng = np.random.default_rng(5)
+    page = 16
+    pool = Pool([96] * 5, page, rng)
+    n_pages = pool.rows // page
+    path = np.array([[1, 3, 20, 21], [1, 3, 20, 21], [2, 7, 8, 9], [0, 1, 2, 3], [1, 30, 50, 51]], np.int32)
+    pos0 = [14, 14, 30, 16, 0]
+    lengths = [2, 4, 0, 0, 1]
+    pool.table[0, 2] = -1  # of positions 32 .. 47: node 20 of the first tree
+    pool.table[2, 1] = n_pages  # 16 .. 31: the tree's first position
+    pool.table[3, 1] = -2**31
+    pool.table[4, 1] = 2**31 - 1  # 16 .. 31: node 30
+    pool.upload()
+    x = torch.from_numpy(rng.integers(0, 256, (pool.rows, 16), dtype=np.uint8)).cuda()
+    want = x.cpu().clone()
+    for b, k in enumerate(lengths):
+        for j in range(k):
+            want[int(pool.row(b, pos0[b] + j))] = want[int(pool.row(b, pos0[b] + path[b, j]))].clone()
+    say("accept, pages that are none")
+    pv.pivot_tree_accept(dev(path), pos0, [x], pool.map)
+    assert torch.equal(x.cpu(), want)
