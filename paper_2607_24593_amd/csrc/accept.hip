@@ -46,7 +46,7 @@ __global__ __launch_bounds__(kThreads) void accept_kernel(AcceptArgs a, RunTable
   const int64_t pos0 = t.pos0[b];
   // A row map leads entries outside the pool to some page of it.  Here that would
   // write rows of another sequence: a pool's table holds -1 where a sequence ends.
-  auto held = [&](int64_t pos) {
+  auto held = [&](int64_t pos) -> int {
     return !a.map.pages ||
            (uint32_t)a.map.pages[(int64_t)b * a.map.max_pages + (pos >> a.map.shift)] < (uint32_t)a.map.n_pages;
   };
@@ -55,7 +55,7 @@ __global__ __launch_bounds__(kThreads) void accept_kernel(AcceptArgs a, RunTable
   for (int j = tid; j < a.n; j += kThreads) {
     const int node = path[j], before = j > 0 ? path[j - 1] : -1;
     const bool ok = node >= j && node > before && node < a.limit - pos0 &&
-                    (held(pos0 + node) & held(pos0 + j));  // both loaded at once
+                    (held(pos0 + node) & held(pos0 + j)) != 0;  // both loaded at once
     if (!ok) atomicMin(&s_length, j);
     s_from[j] = ok ? a.map.row(b, pos0 + node) : 0;
     s_to[j] = ok ? a.map.row(b, pos0 + j) : 0;

@@ -82,7 +82,8 @@ hipError_t launch_attend(const AttendArgs& a, const RunTable& t, const TreeMask*
 
 // Rows of accepted nodes, moved within their arrays: row pos0[b] + path[b][j] of
 // sequence b to row pos0[b] + j, up to the first j whose entry is not in
-// [j, limit - pos0[b]) or not above the entry before it.
+// [j, limit - pos0[b]) or not above the entry before it, or where the map has no page
+// for either row.
 struct AcceptArgs {
   const int32_t* path;  // [sequences, n]
   int32_t n;
