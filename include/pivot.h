@@ -408,8 +408,10 @@ pivot_status pivot_rmsnorm_fp8(int32_t dtype, int32_t n_rows, int32_t dim, const
  *   block_table NULL: row b * seq_stride + s
  *   block_table dev int32 [B, max_pages]: row block_table[b * max_pages + s /
  *     page_size] * page_size + s % page_size; page_size is a power of two in
- *     [16, 65536], rows a multiple of it; entries outside the pool are clamped
- *     into it (no access leaves it, the result is then meaningless).
+ *     [16, 65536], rows a multiple of it.  Reads through entries outside the
+ *     pool (the -1 behind a slot's pages among them) are clamped into it: no
+ *     access leaves it, the result is then meaningless.  Rows are not written
+ *     through such entries.
  */
 typedef struct {
   const int32_t* block_table;
@@ -445,7 +447,8 @@ typedef struct {
  * Quantise new tokens into the cache.  Sequence b gets n_new rows, or rows
  * cu[b] .. cu[b+1]-1 (host [B+1], cu[0] = 0), of the packed latent (dev bf16,
  * rows ld_latent >= 512 values apart) and rope (dev bf16, ld_rope >= 64); they
- * become its positions pos0[b] (host [B]), pos0[b] + 1, ...
+ * become its positions pos0[b] (host [B]), pos0[b] + 1, ...  Rows of positions
+ * whose block_table entry is outside the pool are left out.
  * The scale of 32 values is the smallest power of two 2^e (e >= -127) with
  * max|x| / 2^e <= 6, their codes the nearest E2M1 values to x / 2^e, ties to
  * even; 32 zeros have scale byte 0, values with an infinity or a NaN among

@@ -778,7 +778,8 @@ def _check_batch(row_map, batch, what="block_table"):
 def pivot_cache4_write(latent, rope, cache, pos0, n_new=None, cu=None, stream=None):
     """Quantise packed tokens (latent [T, 512], rope [T, 64], bf16; rows may be
     strided) into the cache: n_new for each of len(pos0) sequences, or the runs
-    of cu (host ints [B+1]), from position pos0[b] on."""
+    of cu (host ints [B+1]), from position pos0[b] on.  Rows of positions for which
+    the block table has no page of the pool are left out."""
     if latent.dtype != torch.bfloat16 or rope.dtype != torch.bfloat16:
         raise ValueError("latent and rope must be bfloat16")
     batch = len(pos0)

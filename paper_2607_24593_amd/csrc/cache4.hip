@@ -37,7 +37,7 @@ __global__ __launch_bounds__(256) void cache4_write_kernel(Cache4Write a, RunTab
   const int r = blockIdx.x * kWavesPerWg + (threadIdx.x >> 6);
   if (r >= a.rows) return;
   const int b = run_of(t, r);
-  const int64_t row = a.map.row(b, (int64_t)t.pos0[b] + (r - t.row0[b]));
+  const int64_t row = a.map.held_row(b, (int64_t)t.pos0[b] + (r - t.row0[b]));
   const Bf8 v = *reinterpret_cast<const Bf8*>(a.latent + r * a.ld_latent + 8 * lane);
   const uint16_t rope = a.rope[r * a.ld_rope + lane];
   // |x| of bf16 orders as its bits do, infinities and NaN last
@@ -56,6 +56,7 @@ __global__ __launch_bounds__(256) void cache4_write_kernel(Cache4Write a, RunTab
   code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(v2bf, v.w[2]), s, 2);
   code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(v2bf, v.w[3]), s, 3);
   if (byte == 255u) code = 0;
+  if (row < 0) return;
   *reinterpret_cast<uint32_t*>(a.cache.codes + row * kCodeBytes + 4 * lane) = code;
   if ((lane & 3) == 0) a.cache.scales[row * kScaleBytes + (lane >> 2)] = (uint8_t)byte;
   a.cache.rope[row * kRope + lane] = rope;

@@ -78,6 +78,13 @@ struct KeyMap {
     const int32_t pg = min(max(pages[(int64_t)b * max_pages + (s >> shift)], 0), n_pages - 1);
     return ((int64_t)pg << shift) | (s & ((1 << shift) - 1));
   }
+  // The same for a row that is written: -1 where the entry names no page of the pool.
+  // Clamped it would be a row of whoever holds that page.
+  __device__ __forceinline__ int64_t held_row(int b, int64_t s) const {
+    if (!pages) return (int64_t)b * stride + s;
+    const int32_t pg = pages[(int64_t)b * max_pages + (s >> shift)];
+    return (uint32_t)pg < (uint32_t)n_pages ? ((int64_t)pg << shift) | (s & ((1 << shift) - 1)) : -1;
+  }
 };
 
 // Order-preserving map of a float onto uint32 (larger float -> larger key);
