@@ -541,7 +541,8 @@ pivot_status pivot_cache4_attend(const pivot_attend_args* a);
  *             multiple of 4, the pointers are 4-byte aligned.  No row that is
  *             written may be one that is read: dst is another array, or the
  *             same one with `to` naming other pages (pages shared with other
- *             sequences stay as they are).
+ *             sequences stay as they are).  Rows j for which `to` has no page
+ *             of the pool are left out.
  * Workspace as above, pivot_evict_workspace_size(a) bytes.
  */
 #define PIVOT_EVICT_MAX_ARRAYS 8

@@ -354,8 +354,9 @@ __global__ __launch_bounds__(256) void move_kernel(MoveArrays m, KeyMap from, Ke
   const int b = b0 + (int)(blockIdx.x / groups), j = (int)(blockIdx.x % groups) * kMoveRows + threadIdx.x;
   if (threadIdx.x < kMoveRows) {
     const int32_t pos = j < keep ? kept[(int64_t)b * keep + j] : -1;
-    s_from[threadIdx.x] = pos < 0 ? -1 : from.row(b, pos);
-    s_to[threadIdx.x] = pos < 0 ? -1 : to.row(b, j);
+    const int64_t row = pos < 0 ? -1 : to.held_row(b, j);
+    s_from[threadIdx.x] = row < 0 ? -1 : from.row(b, pos);
+    s_to[threadIdx.x] = row;
   }
   __syncthreads();
   for (int arr = 0; arr < m.n; ++arr) {

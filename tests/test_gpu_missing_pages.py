@@ -82,3 +82,39 @@ def test_a_growth_without_pages_and_the_write_behind_it():
     for now, old in zip(parts, before):
         assert torch.equal(now[rest], old[rest])
     assert torch.equal(parts[2][torch.from_numpy(own).cuda()], rows[:12, 512:])
+
+
+@pytest.mark.parametrize("lens,keep,page,share", [([300, 37, 200], 64, 16, 0.5), ([500] * 5, 490, 64, 0.3), ([40] * 70, 33, 16, 0.4)])
+def test_kept_rows_without_a_page_are_not_moved(lens, keep, page, share):
+    """Rows move to pages of another table; those whose new place has no page are left
+    out, the list of the kept positions is whole."""
+    rng = np.random.default_rng(keep)
+    pool = Pool(lens, page, rng, spare=0)
+    b, per = len(lens), -(-keep // page)
+    n = pool.rows // page
+    fresh = Pool.__new__(Pool)
+    fresh.page, fresh.rows = page, 2 * pool.rows
+    fresh.table = (n + rng.permutation(n)[:b * per].reshape(b, per)).astype(np.int32)
+    fresh.table[rng.random(fresh.table.shape) < share] = -1
+    fresh.table[0, 0] = rng.choice([-2**31, 2**31 - 1, 2 * n])
+    first = rng.integers(0, 256, (2 * pool.rows, 20), dtype=np.uint8)
+    second = rng.standard_normal((2 * pool.rows, 32)).astype(np.float32)
+    arrays = [dev(first), dev(second)]
+    acc = rng.random((b, max(lens))).astype(np.float32)
+    table = dev(fresh.table)
+    frm = pv.make_row_map(rows=2 * pool.rows, block_table=pool.bt, page_size=page)
+    to = pv.make_row_map(rows=2 * pool.rows, block_table=table, page_size=page)
+    say("evict, pages that are none", lens[:3], keep, page)
+    kept, _ = pv.pivot_evict(dev(acc), lens, keep, [(x, x) for x in arrays], frm, to, sink=2, recent=3)
+    want = [first.copy(), second.copy()]
+    left = 0
+    for i, m in enumerate(lens):
+        mine = np.array(ref.evict(acc[i], m, keep, 2, 3))
+        assert host(kept)[i, :len(mine)].tolist() == mine.tolist()
+        ok, at = _held(fresh, i, np.arange(len(mine)))
+        left += (~ok).sum()
+        for w, old in zip(want, (first, second)):
+            w[at[ok]] = old[pool.row(i, mine[ok])]
+    assert left > 0
+    for x, w in zip(arrays, want):
+        assert np.array_equal(host(x), w)
