@@ -43,14 +43,15 @@ def tree_masks(parents, words, device="cuda"):
 
 
 class Layer:
-    """The samples' lengths are host numbers; slot s of the table is sample s."""
+    """The samples' lengths are host numbers; slot s of the table is sample s.  n_pages:
+    the pool's pages, fewer than samples times room where samples share a prompt."""
 
-    def __init__(self, samples, room, dim=512, heads=128, page=64, device="cuda", seed=0):
+    def __init__(self, samples, room, dim=512, heads=128, page=64, device="cuda", seed=0, n_pages=None):
         g = torch.Generator(device=device).manual_seed(seed)
         self.samples, self.dim, self.heads, self.page = samples, dim, heads, page
         new = lambda *s, **k: torch.zeros(s, device=device, **k)  # noqa: E731
         per = -(-room // page)
-        n_pages = samples * per
+        n_pages = samples * per if n_pages is None else n_pages
         self.table = torch.full((samples, per), -1, dtype=torch.int32, device=device)
         self.refs = new(n_pages, dtype=torch.int32)
         self.pages = pv.make_pages(self.table, self.refs, page)
@@ -68,9 +69,12 @@ class Layer:
         self.length = [0] * samples
 
     def grow(self, slots, new):
-        """Room for new[i] more tokens of slots[i]."""
+        """Room for new[i] more tokens of slots[i].  Only the device knows whether the pool had
+        the pages: this waits for it."""
         now = [self.length[s] for s in slots]
         copies, self.state = pv.pivot_pages_grow(self.pages, slots, now, [n + m for n, m in zip(now, new)])
+        if missing := int(self.state[0]):
+            raise RuntimeError(f"the pool lacks {missing} pages")
         pv.pivot_pages_copy(self.pages, copies, self.arrays)
 
     def project(self, hidden, residual, weight, dtype=torch.bfloat16):

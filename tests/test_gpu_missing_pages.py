@@ -1,6 +1,9 @@
 """GPU tests of operators that write rows through a block table in which entries name
 no page of the pool, as a slot's do behind its pages and after a growth for which
 pages were missing: nothing is written there, and nothing else changes."""
+import importlib.util
+import os
+
 import numpy as np
 import pytest
 import torch
@@ -118,3 +121,23 @@ def test_kept_rows_without_a_page_are_not_moved(lens, keep, page, share):
     assert left > 0
     for x, w in zip(arrays, want):
         assert np.array_equal(host(x), w)
+
+
+def test_the_example_stops_where_pages_are_missing():
+    spec = importlib.util.spec_from_file_location(
+        "draft_step", os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "draft_step.py"))
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    layer = ex.Layer(2, 200, dim=128, heads=4, page=16, n_pages=9)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    layer.append(0, torch.randn((100, 128), generator=g, device="cuda").bfloat16())  # 7 pages
+    layer.fork(0, 1)
+    before = [t.clone() for t in (layer.table, layer.refs, *layer.arrays)]
+    say("a step that lacks pages")
+    hidden = torch.randn((2, 20, 128), generator=g, device="cuda").bfloat16()
+    masks = torch.stack([ex.tree_masks(list(range(-1, 19)), 1)] * 2)
+    with pytest.raises(RuntimeError, match="lacks 1 "):  # 100 + 20 tokens: a copy, and one more each
+        layer.step(hidden, torch.zeros_like(hidden), masks)
+    assert layer.length == [100, 100]
+    for now, old in zip((layer.table, layer.refs, *layer.arrays), before):
+        assert torch.equal(now, old)
