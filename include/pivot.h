@@ -659,6 +659,8 @@ pivot_status pivot_cache4_attend_tree(const pivot_attend_args* a, const pivot_tr
  *   arrays  n_arrays (1 .. PIVOT_EVICT_MAX_ARRAYS) row arrays, rows of a multiple of
  *           4 bytes, 4-byte aligned
  * The rows from pos0[b] to its last node must not be shared with another sequence.
+ * Weights that pivot_cache4_attend_tree added up by position do not move with them:
+ * pivot_tree_accept_acc does both.
  */
 typedef struct {
   void* rows;
@@ -666,6 +668,21 @@ typedef struct {
 } pivot_rows;
 pivot_status pivot_tree_accept(int32_t batch, int32_t n, const int32_t* path, const int32_t* pos0, int32_t n_arrays,
                                const pivot_rows* arrays, const pivot_row_map* map, void* stream);
+
+/*
+ * The same, and the accepted nodes' weights with them: acc[b][pos0[b] + path[b][j]]
+ * becomes acc[b][pos0[b] + j], and the weights of the tree's other positions, up to
+ * pos0[b] + nodes[b] - 1, become 0, for the tokens that come there next.  Weights that
+ * rows of rejected nodes gave to tokens that stay are not taken back.
+ *   nodes   host [batch]: each tree's nodes, at most PIVOT_TREE_MAX_NODES (else
+ *           UNSUPPORTED); an entry of path that is none of them ends the path, too
+ *   acc     dev fp32 [batch, acc_stride], as pivot_cache4_attend has it; acc_stride
+ *           >= every pos0[b] + nodes[b]
+ * With n = 0 (path may be NULL) every node is rejected.
+ */
+pivot_status pivot_tree_accept_acc(int32_t batch, int32_t n, const int32_t* path, const int32_t* pos0,
+                                   const int32_t* nodes, int32_t n_arrays, const pivot_rows* arrays,
+                                   const pivot_row_map* map, float* acc, int64_t acc_stride, void* stream);
 
 /*
  * Pages that sequences share.

@@ -44,6 +44,7 @@ EXPORTED = ["pivot_workspace_size", "pivot_dense_index", "pivot_group_index", "p
             "pivot_cache4_attend_workspace_size", "pivot_evict", "pivot_evict_workspace_size",
             "pivot_linear4", "pivot_linear4_workspace_size", "pivot_linear4_pack",
             "pivot_cache4_attend_tree", "pivot_cache4_attend_tree_workspace_size", "pivot_tree_accept",
+            "pivot_tree_accept_acc",
             "pivot_pages_fork", "pivot_pages_free", "pivot_pages_grow", "pivot_pages_grow_workspace_size",
             "pivot_pages_compact", "pivot_pages_compact_workspace_size", "pivot_pages_copy",
             "pivot_profile_end", "pivot_status_string", "pivot_last_error", "pivot_version"]
@@ -260,6 +261,8 @@ def lib():
         L.pivot_cache4_attend_tree.argtypes = [ctypes.POINTER(pivot_attend_args), T]
         L.pivot_tree_accept.restype = I32
         L.pivot_tree_accept.argtypes = [I32, I32, P, P, I32, P, ctypes.POINTER(pivot_row_map), P]
+        L.pivot_tree_accept_acc.restype = I32
+        L.pivot_tree_accept_acc.argtypes = [I32, I32, P, P, P, I32, P, ctypes.POINTER(pivot_row_map), P, I64, P]
         PG = ctypes.POINTER(pivot_pages)
         L.pivot_pages_fork.restype = I32
         L.pivot_pages_fork.argtypes = [PG, I32, P, P, P, P]
@@ -1031,17 +1034,32 @@ def _row_arrays(arrays, rows, device):
     return _ROWS.pack(*words, *(0,) * (2 * PIVOT_EVICT_MAX_ARRAYS - len(words)))
 
 
-def pivot_tree_accept(path, pos0, arrays, row_map, stream=None):
+def pivot_tree_accept(path, pos0, arrays, row_map, stream=None, acc=None, nodes=None):
     """Move the accepted nodes of each sequence's tree to the positions that follow
     its prefix, in place in every row array: row pos0[b] + path[b, j] becomes row
     pos0[b] + j.  path: int32 [B, n], ascending, -1 behind the last accepted node; it
-    ends too where the table has no page of the pool."""
+    ends too where the table has no page of the pool.  acc: fp32 [B, >= max pos0 +
+    nodes], the weights that pivot_cache4_attend added up, with nodes, each tree's
+    number of nodes (host ints): those of the accepted nodes move too, the other
+    nodes' become 0."""
     if path.dtype != torch.int32 or path.dim() != 2 or not path.is_contiguous() or path.shape[0] != len(pos0):
         raise ValueError("path must be a contiguous int32 [len(pos0), n] tensor")
+    if (acc is None) != (nodes is None):
+        raise ValueError("acc and nodes come together")
     device = path.get_device()
     _check_batch(row_map, len(pos0))
     _on_gpu(device, getattr(row_map, "_bt", None))
     c = _row_arrays(arrays, row_map.rows, device)
+    if acc is not None:
+        if acc.dtype != torch.float32 or acc.dim() != 2 or acc.shape[0] < len(pos0) or not acc.is_contiguous():
+            raise ValueError("acc must be a contiguous float32 [B, tokens] tensor")
+        if len(nodes) != len(pos0):
+            raise ValueError("nodes must have one entry per sequence")
+        _on_gpu(device, acc)
+        _check(lib().pivot_tree_accept_acc(len(pos0), path.shape[1], _ptr(path), _packed_ints(pos0), _packed_ints(nodes),
+                                           len(arrays), c, ctypes.byref(row_map), _ptr(acc), acc.shape[1],
+                                           _stream(stream)), "pivot_tree_accept_acc")
+        return
     _check(lib().pivot_tree_accept(len(pos0), path.shape[1], _ptr(path), _packed_ints(pos0), len(arrays), c,
                                    ctypes.byref(row_map), _stream(stream)), "pivot_tree_accept")
 

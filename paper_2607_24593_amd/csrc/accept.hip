@@ -54,14 +54,23 @@ __global__ __launch_bounds__(kThreads) void accept_kernel(AcceptArgs a, RunTable
   __syncthreads();
   for (int j = tid; j < a.n; j += kThreads) {
     const int node = path[j], before = j > 0 ? path[j - 1] : -1;
-    const bool ok = node >= j && node > before && node < a.limit - pos0 &&
+    const bool ok = node >= j && node > before && node < a.limit - pos0 && node < t.n_rows[b] &&
                     (held(pos0 + node) & held(pos0 + j)) != 0;  // both loaded at once
     if (!ok) atomicMin(&s_length, j);
     s_from[j] = ok ? a.map.row(b, pos0 + node) : 0;
     s_to[j] = ok ? a.map.row(b, pos0 + j) : 0;
   }
   __syncthreads();
-  const int n = s_length, bytes = a.row_bytes[arr];
+  const int n = s_length;
+  if (arr == a.n_arrays) {  // the nodes' weights, by positions of the sequence
+    __shared__ float s_acc[PIVOT_TREE_MAX_NODES];
+    float* acc = a.acc + b * a.acc_stride + pos0;
+    for (int j = tid; j < n; j += kThreads) s_acc[j] = acc[path[j]];
+    __syncthreads();
+    for (int j = tid; j < t.n_rows[b]; j += kThreads) acc[j] = j < n ? s_acc[j] : 0.f;
+    return;
+  }
+  const int bytes = a.row_bytes[arr];
   if (((bytes | (uintptr_t)a.rows[arr]) & 15) == 0) move_path<uint4>(a.rows[arr], bytes, s_from, s_to, n);
   else move_path<uint32_t>(a.rows[arr], bytes, s_from, s_to, n);
 }
@@ -69,7 +78,8 @@ __global__ __launch_bounds__(kThreads) void accept_kernel(AcceptArgs a, RunTable
 }  // namespace
 
 hipError_t launch_accept(const AcceptArgs& a, const RunTable& t, hipStream_t stream) {
-  hipLaunchKernelGGL(accept_kernel, dim3((unsigned)t.n, (unsigned)a.n_arrays), dim3(kThreads), 0, stream, a, t);
+  const unsigned parts = (unsigned)a.n_arrays + (a.acc ? 1 : 0);
+  hipLaunchKernelGGL(accept_kernel, dim3((unsigned)t.n, parts), dim3(kThreads), 0, stream, a, t);
   return hipGetLastError();
 }
 

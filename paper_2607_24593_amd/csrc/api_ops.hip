@@ -300,6 +300,56 @@ pivot_status check_rows(int n_arrays, const pivot_rows* arrays) {
   return PIVOT_OK;
 }
 
+// nodes: of each tree, where the call has acc, else NULL.
+pivot_status accept(int32_t batch, int32_t n, const int32_t* path, const int32_t* pos0, const int32_t* nodes,
+                    int32_t n_arrays, const pivot_rows* arrays, const pivot_row_map* map, float* acc, int64_t acc_stride,
+                    void* stream) {
+  if (batch < 1 || n < 0) return fail(PIVOT_ERR_INVALID_ARG, "batch must be >= 1 and n >= 0");
+  if (n > PIVOT_TREE_MAX_NODES) return fail(PIVOT_ERR_UNSUPPORTED, "n=%d exceeds %d nodes", n, PIVOT_TREE_MAX_NODES);
+  if (!pos0 || !map) return fail(PIVOT_ERR_INVALID_ARG, "pos0 (host array) and map are required");
+  int64_t longest = 0;
+  for (int b = 0; b < batch; ++b) {
+    if (pos0[b] < 0) return fail(PIVOT_ERR_INVALID_ARG, "position %d of sequence %d is negative", pos0[b], b);
+    if (nodes && nodes[b] < 0) return fail(PIVOT_ERR_INVALID_ARG, "%d nodes of sequence %d", nodes[b], b);
+    if (nodes && nodes[b] > PIVOT_TREE_MAX_NODES)
+      return fail(PIVOT_ERR_UNSUPPORTED, "%d nodes of sequence %d exceed %d", nodes[b], b, PIVOT_TREE_MAX_NODES);
+    const int64_t end = (int64_t)pos0[b] + (nodes ? nodes[b] : 0);
+    if (end > PIVOT_MAX_KEYS) return fail(PIVOT_ERR_UNSUPPORTED, "sequence %d exceeds PIVOT_MAX_KEYS=%d", b, PIVOT_MAX_KEYS);
+    longest = std::max(longest, end);
+  }
+  if (acc && acc_stride < longest)
+    return fail(PIVOT_ERR_INVALID_ARG, "acc_stride=%lld < %lld tokens", (long long)acc_stride, (long long)longest);
+  pivot_status s = check_map(*map, batch, longest, "map");
+  if (s != PIVOT_OK) return s;
+  s = check_rows(n_arrays, arrays);
+  if (s != PIVOT_OK || (n == 0 && !acc)) return s;
+  if (n > 0 && (!path || !aligned(path, 4))) return fail(PIVOT_ERR_INVALID_ARG, "path is required, 4-byte aligned");
+  for (int b0 = 0; b0 < batch; b0 += kMaxSeq) {
+    RunTable t{};
+    t.n = std::min(kMaxSeq, batch - b0);
+    for (int u = 0; u < t.n; ++u) {
+      t.pos0[u] = pos0[b0 + u];
+      t.n_rows[u] = nodes ? nodes[b0 + u] : 0x7FFFFFFF;
+    }
+    AcceptArgs k{};
+    int64_t first;
+    k.path = path + (int64_t)b0 * n;
+    k.n = n;
+    k.limit = capacity(*map);
+    k.map = key_map(*map, b0, &first);
+    k.n_arrays = n_arrays;
+    for (int i = 0; i < n_arrays; ++i) {
+      k.rows[i] = (uint8_t*)arrays[i].rows + first * arrays[i].row_bytes;
+      k.row_bytes[i] = arrays[i].row_bytes;
+    }
+    k.acc = acc ? acc + (int64_t)b0 * acc_stride : nullptr;
+    k.acc_stride = acc_stride;
+    s = hip_check(launch_accept(k, t, (hipStream_t)stream), "accept kernel");
+    if (s != PIVOT_OK) return s;
+  }
+  return PIVOT_OK;
+}
+
 pivot_status check_pages(const pivot_pages* p) {
   if (!p) return fail(PIVOT_ERR_INVALID_ARG, "pages is NULL");
   const int P = p->page_size;
@@ -536,39 +586,15 @@ pivot_status pivot_cache4_attend_tree(const pivot_attend_args* a, const pivot_tr
 
 pivot_status pivot_tree_accept(int32_t batch, int32_t n, const int32_t* path, const int32_t* pos0, int32_t n_arrays,
                                const pivot_rows* arrays, const pivot_row_map* map, void* stream) {
-  if (batch < 1 || n < 0) return fail(PIVOT_ERR_INVALID_ARG, "batch must be >= 1 and n >= 0");
-  if (n > PIVOT_TREE_MAX_NODES) return fail(PIVOT_ERR_UNSUPPORTED, "n=%d exceeds %d nodes", n, PIVOT_TREE_MAX_NODES);
-  if (!pos0 || !map) return fail(PIVOT_ERR_INVALID_ARG, "pos0 (host array) and map are required");
-  int64_t longest = 0;
-  for (int b = 0; b < batch; ++b) {
-    if (pos0[b] < 0) return fail(PIVOT_ERR_INVALID_ARG, "position %d of sequence %d is negative", pos0[b], b);
-    if (pos0[b] > PIVOT_MAX_KEYS) return fail(PIVOT_ERR_UNSUPPORTED, "sequence %d exceeds PIVOT_MAX_KEYS=%d", b, PIVOT_MAX_KEYS);
-    longest = std::max<int64_t>(longest, pos0[b]);
-  }
-  pivot_status s = check_map(*map, batch, longest, "map");
-  if (s != PIVOT_OK) return s;
-  s = check_rows(n_arrays, arrays);
-  if (s != PIVOT_OK || n == 0) return s;
-  if (!path || !aligned(path, 4)) return fail(PIVOT_ERR_INVALID_ARG, "path is required, 4-byte aligned");
-  for (int b0 = 0; b0 < batch; b0 += kMaxSeq) {
-    RunTable t{};
-    t.n = std::min(kMaxSeq, batch - b0);
-    for (int u = 0; u < t.n; ++u) t.pos0[u] = pos0[b0 + u];
-    AcceptArgs k{};
-    int64_t first;
-    k.path = path + (int64_t)b0 * n;
-    k.n = n;
-    k.limit = capacity(*map);
-    k.map = key_map(*map, b0, &first);
-    k.n_arrays = n_arrays;
-    for (int i = 0; i < n_arrays; ++i) {
-      k.rows[i] = (uint8_t*)arrays[i].rows + first * arrays[i].row_bytes;
-      k.row_bytes[i] = arrays[i].row_bytes;
-    }
-    s = hip_check(launch_accept(k, t, (hipStream_t)stream), "accept kernel");
-    if (s != PIVOT_OK) return s;
-  }
-  return PIVOT_OK;
+  return accept(batch, n, path, pos0, nullptr, n_arrays, arrays, map, nullptr, 0, stream);
+}
+
+pivot_status pivot_tree_accept_acc(int32_t batch, int32_t n, const int32_t* path, const int32_t* pos0,
+                                   const int32_t* nodes, int32_t n_arrays, const pivot_rows* arrays,
+                                   const pivot_row_map* map, float* acc, int64_t acc_stride, void* stream) {
+  if (!nodes) return fail(PIVOT_ERR_INVALID_ARG, "nodes (host array) is required");
+  if (!acc || !aligned(acc, 4)) return fail(PIVOT_ERR_INVALID_ARG, "acc is required, 4-byte aligned");
+  return accept(batch, n, path, pos0, nodes, n_arrays, arrays, map, acc, acc_stride, stream);
 }
 
 size_t pivot_evict_workspace_size(const pivot_evict_args* a) {

@@ -82,8 +82,9 @@ hipError_t launch_attend(const AttendArgs& a, const RunTable& t, const TreeMask*
 
 // Rows of accepted nodes, moved within their arrays: row pos0[b] + path[b][j] of
 // sequence b to row pos0[b] + j, up to the first j whose entry is not in
-// [j, limit - pos0[b]) or not above the entry before it, or where the map has no page
-// for either row.
+// [j, min(limit - pos0[b], n_rows[b])) or not above the entry before it, or where the
+// map has no page for either row.  With acc the weights of the tree's n_rows[b] nodes
+// move alike, and those behind the path become 0.
 struct AcceptArgs {
   const int32_t* path;  // [sequences, n]
   int32_t n;
@@ -92,6 +93,8 @@ struct AcceptArgs {
   int32_t n_arrays;
   uint8_t* rows[PIVOT_EVICT_MAX_ARRAYS];
   int32_t row_bytes[PIVOT_EVICT_MAX_ARRAYS];
+  float* acc;           // [sequences, acc_stride], or NULL
+  int64_t acc_stride;
 };
 hipError_t launch_accept(const AcceptArgs& a, const RunTable& t, hipStream_t stream);
 
