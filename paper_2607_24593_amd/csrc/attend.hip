@@ -207,8 +207,10 @@ __host__ __device__ inline int splits_of(const RunTable& t, int b, int tiles_per
 }
 
 // What a kernel is compiled for: causal calls of both kinds, trees over the prefix,
-// trees over index sets (with one kernel for both, three registers of its tile loop
-// are spilled, which costs 20%).
+// trees over index sets.  At 128 rows both kernels of trees spill three registers, one
+// of which every tile reloads (the causal one spills none); one kernel for both kinds
+// spills as many, and takes 2 to 4% longer (64 nodes x 128 heads x 131072 keys 3.27
+// instead of 3.16 ms).
 enum Call : int { kCausal, kTreePrefix, kTreeSets };
 struct NoTree {};
 template <bool TREE>
@@ -245,7 +247,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a, Ru
   __shared__ float s_alpha[2][ROWS], s_max[ROWS], s_sum[ROWS];
   // of a tree: the word that a row's mask starts at (prefix calls), the mask of the
   // unit's query (index sets), the masks and their words; here, and not in registers,
-  // because few tiles need them (held in registers they cost the tile loop 20%)
+  // because few tiles need them (masks held in registers cost the tile loop 20%)
   __shared__ int s_tree[TREE ? ROWS : 1];
   __shared__ uint32_t s_mask[TREE ? kTreeWords : 1];
   __shared__ const uint32_t* s_bits;
@@ -1185,10 +1187,15 @@ __global__ __launch_bounds__(256) void dense_weights_kernel(AttendArgs a, RunTab
 
 // The same for trees, where a call has many rows: T / 8 rows at a time, each thread 4
 // keys, four loads on their way.  Rows whose mask does not name a node are left out,
-// not added as zeros.  T = 1024 from 1024 rows a sequence on: a short sequence has few
-// tiles.  Bound by the scores' bytes: 192 rows x 196000 keys in 25 us, 6 TB/s (one key
-// a thread: 52); 2940 rows x 375 keys: a call of 103 us with 256 threads and the masks
-// read row by row, 55 with 1024 and the masks beside the scores.
+// not added as zeros.  Bound by the scores' bytes: 192 rows x 196000 keys in 25 us, 6
+// TB/s (one key a thread: 52).  T = 1024 from 1024 rows a sequence on, where a
+// workgroup of 256 threads passes a tile in many rounds, 32 rows each; below, 1024
+// threads have too few rows to share.  Calls with 256 and 1024 threads, us: 3328 rows a
+// sequence x 1026 keys 91, 68; x 6026 keys 145, 123; x 40026 keys 610, 599; 32 x 3328
+// rows x 1026 keys 626, 617; 8192 rows x 16064 keys 613, 583; 2048 rows x 100064 keys
+// 879, 869; 38400 rows x 2300 keys 1010, 694; 4 x 1024 rows x 20008 keys 371, 364; 32 x
+// 896 rows x 1507 keys 203, 202; 8 x 640 rows x 3040 keys 101, 102; 8 x 192 rows x 24012
+// keys 212, 233; 64 x 128 rows x 2008 keys 104, 121.
 template <int T>
 __global__ __launch_bounds__(T) void tree_weights_kernel(AttendArgs a, RunTable t, ScoreMap sm, TreeMask tree) {
   constexpr int R = T / 8;  // rows at a time

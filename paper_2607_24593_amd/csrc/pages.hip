@@ -17,8 +17,8 @@
 // before writes the blocks' maps and counts (the second one changes refs, and several
 // workgroups share a block).
 // Bound by latency, a chain of dependent loads and bisections: 160 slots of a pool of
-// 4800 pages grow in 12 us; two slots by 4096 pages each in a pool of 87000 in 5 + 6 us
-// (by one workgroup a block 27).
+// 4800 pages grow in 11.5 us; two slots by 4096 pages each in a pool of 87000 in 5.3 +
+// 7.5 us (by one workgroup a block 27).
 #include <algorithm>
 
 #include "cache4.h"
