@@ -693,9 +693,10 @@ pivot_status pivot_tree_accept_acc(int32_t batch, int32_t n, const int32_t* path
  * page_size is a power of two in [16, 65536], n_pages * page_size and slots *
  * max_pages at most 2^31 - 1.  A pool starts with every entry -1 and every count 0.
  * Lists are host arrays of at most PIVOT_PAGES_MAX_LIST entries (else
- * UNSUPPORTED), slots in [0, slots), tokens in [0, max_pages * page_size] and at most
- * PIVOT_MAX_KEYS (else UNSUPPORTED).  A call grows by at most 2^30 pages.  Table
- * entries that name no page of the pool are left alone.
+ * UNSUPPORTED; a growth takes at least one), slots in [0, slots), tokens in [0,
+ * max_pages * page_size] and at most PIVOT_MAX_KEYS (else UNSUPPORTED).  A call
+ * grows by at most 2^30 pages.  Table entries that name no page of the pool are left
+ * alone.
  * Calls that change one pool run in the order of one stream.
  */
 #define PIVOT_PAGES_MAX_LIST 256
@@ -707,7 +708,9 @@ typedef struct {
 } pivot_pages;
 
 /* Slot dst[i], without pages until now, gets the pages of slot src[i]'s first
- * tokens[i] tokens, counted once more.  No dst may come twice or be a src. */
+ * tokens[i] tokens, counted once more.  No dst may come twice or be a src.  What lies
+ * by sequence and under no table (weights of pivot_cache4_attend) is the caller's to
+ * copy. */
 pivot_status pivot_pages_fork(const pivot_pages* p, int32_t n, const int32_t* src, const int32_t* dst,
                               const int32_t* tokens, void* stream);
 
@@ -728,7 +731,9 @@ pivot_status pivot_pages_free(const pivot_pages* p, int32_t n, const int32_t* sl
  *   copies  dev int32 [n, 2]: (old page, new page) of the first kind, else (-1, -1):
  *           their contents are to be copied (pivot_pages_copy) before they are used
  *   state   dev int32 [2]: pages that were missing, pages that are free afterwards.
- *           If any is missing nothing is changed, and copies are all -1.
+ *           If any is missing nothing is changed, and copies are all -1: the slots
+ *           have no pages for their new tokens, and rows written there are left
+ *           out.  Only the device knows; a caller that may run short reads it.
  * Workspace: pivot_pages_grow_workspace_size bytes (device, 256-byte aligned; 0 for
  * invalid arguments).
  */
